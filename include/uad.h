@@ -290,6 +290,129 @@ int uad_linear_check(const void* x, const void* w_tiled, const float* bias, floa
 int uad_linear_static_scratch(const void* x, const void* w_tiled, const float* bias, float* out,
                               int32_t M, int32_t N, int32_t K, void* stream);
 
+/* ---- A paged key-value cache on caller buffers: append, attention ---------------------------
+ * The paper has no counterpart: its prefix is one cached buffer a robot (App. D). A program that runs the
+ * vision-language model on the same GPU keeps that model's keys and values in pages shared by all robots, extends
+ * them by the tokens of an instruction, an answer or a draft, and binds them to the expert (uad_set_prefix_paged).
+ * The calls below do so for one layer and a batch of sequences of different lengths. They are asynchronous on
+ * `stream` (a cudaStream_t, NULL = legacy stream) and in its order, allocate nothing, keep nothing between calls,
+ * and may be captured into CUDA graphs: what changes from step to step (tables, lengths, rows) is read on the
+ * device when the graph runs. All pointers in the structures are device memory of the current device.
+ *
+ * Page p, slot s, head h, dimension d of the keys is at k + p * page_stride + s * slot_stride + h * head_stride + d
+ * (in elements), of the values at the same place of v: pages of [slot][head][dim], [head][slot][dim] or of keys and
+ * values in turn. */
+typedef struct uad_kv_pages {
+  void *k, *v;           /* 16-byte aligned */
+  int64_t page_stride, slot_stride, head_stride;   /* > 0, multiples of 16 bytes */
+  int32_t dtype;         /* UAD_DTYPE_F32 or UAD_DTYPE_BF16 */
+  int32_t n_pages;       /* >= 1 */
+  int32_t page_size;     /* tokens of a page, 1..65536, any number */
+  int32_t n_kv_heads;    /* 1..1024 */
+  int32_t head_dim;      /* 64, 128 or 256 */
+  int32_t pad;
+} uad_kv_pages;
+
+/* A batch of sequences. Token i of sequence b is in page table[b * table_stride + i / page_size], slot i % page_size.
+ * Rows start[b] .. start[b + 1] - 1 of the token tensors are its newest tokens, in order: row t is the token at position
+ * len[b] - (start[b + 1] - t). Rows from start[n_seqs] on belong to nobody and are neither read nor written. A page may
+ * stand in the tables of several sequences (a shared prefix); no two rows of one append may name the same slot. */
+typedef struct uad_kv_seqs {
+  const int32_t* table;  /* [n_seqs][table_stride], the first table_width entries of a row; entries past a sequence's last
+                            token, or before what its window sees, are not looked at */
+  const int32_t* len;    /* [n_seqs] tokens in the cache, the new ones included; 0 is allowed */
+  const int32_t* start;  /* [n_seqs + 1], ascending from 0 or more; NULL: row b is the one new token of sequence b */
+  int64_t table_stride;
+  int32_t n_seqs;        /* 0..65535 */
+  int32_t table_width;   /* >= 1; table_width * page_size < 2^31 */
+  int32_t max_new;       /* at least the largest number of new tokens of a sequence, >= 1 */
+  int32_t max_len;       /* attention: about the longest len, from which the work is split (0: table_width * page_size). A
+                            longer sequence is served too, less evenly */
+} uad_kv_seqs;
+
+/* What the kernels find wrong on the device is added to the caller's status word (a device int32 that the caller
+ * clears; NULL: not reported), and never followed: */
+#define UAD_KV_BAD_PAGE 1 /* a page outside 0..n_pages-1 where a token is written or seen: it is left out */
+#define UAD_KV_BAD_SEQ 2  /* len outside 0..table_width * page_size, fewer tokens than new ones, more new ones than max_new, or
+                             start not ascending within the rows: the sequence is left out, its rows stay as they were */
+
+/* Rotation of a head's first `dim` dimensions by its token's position: pair (i, i + dim / 2) by the angle
+ * position * theta^(-2 i / dim). The frequencies are kept as 64-bit fractions of a turn, so that far positions
+ * lose nothing. Plain memory of the caller, set by uad_rope_init (host only). */
+typedef struct uad_rope {
+  int32_t dim, pad;
+  uint64_t turn[128];
+} uad_rope;
+/* dim: a multiple of 16, 16..256; theta > 0, finite. Returns UAD_OK or UAD_EINVAL. */
+int uad_rope_init(double theta, int32_t dim, uad_rope* out);
+
+/* The new tokens' rows of an append. Head h of row t of q is at q + t * q_stride + h * head_dim, and so on: the three may
+ * be parts of one fused projection. Strides in elements; addresses and strides are multiples of 16 bytes. */
+typedef struct uad_kv_rows {
+  const void *q, *k, *v; /* q: NULL = no queries; k, v: both or NULL = only queries are rotated */
+  int64_t q_stride, k_stride, v_stride;
+  void* q_out;           /* rotated queries in the cache's type, head h of row t at t * q_out_stride + h * head_dim; may be q */
+  int64_t q_out_stride;
+  int32_t dtype;         /* type of q, k and v: UAD_DTYPE_F32 (such as uad_linear's output) or UAD_DTYPE_BF16 */
+  int32_t n_heads;       /* query heads; 0 without q */
+  int32_t n_rows;        /* rows that the tensors hold; start stays within them */
+  int32_t pad;
+} uad_kv_rows;
+
+/* Rotate the new tokens' queries and keys (rope NULL: no rotation) and write keys and values into their pages, in fp32
+ * arithmetic rounded once to the cache's type. Values are not rotated. Slots of other tokens stay as they were.
+ * Errors: UAD_EINVAL (arguments), UAD_ECUDA. */
+int uad_kv_append(const uad_kv_pages* pages, const uad_kv_seqs* seqs, const uad_kv_rows* rows, const uad_rope* rope,
+                  int32_t* status, void* stream);
+
+/* Attention of the new tokens over their sequences' pages. Query head h reads key/value head h / (n_heads / n_kv_heads).
+ * A token at position p sees the keys j < len with j <= p (causal), j > p - window (window > 0) and
+ * key_mask[b * mask_stride + j] != 0 (key_mask != NULL): out = softmax(scale q k) v over them. What it does not see has no
+ * influence, whatever it holds. Where it sees nothing, out is 0 and lse is -infinity. Products and softmax in fp32
+ * (bf16 caches: exact products of bf16 keys and queries, probabilities as the sum of two bf16), rounded once to the
+ * cache's type. Meant for one to a few new tokens a sequence: each 8 to 32 rows (n_heads / n_kv_heads times new tokens)
+ * read the keys once. */
+typedef struct uad_attn {
+  const void* q;         /* cache's type, head h of row t at t * q_stride + h * head_dim, 16-byte aligned */
+  void* out;             /* the same with out_stride; must not overlap q */
+  float* lse;            /* [n_rows][n_heads] natural logarithm of the softmax's denominator; NULL: not wanted */
+  const uint8_t* key_mask;
+  int64_t q_stride, out_stride, mask_stride;
+  float scale;           /* 0: 1 / sqrt(head_dim) */
+  int32_t n_heads;       /* a multiple of n_kv_heads, at most 64 times it */
+  int32_t n_rows;
+  int32_t causal;        /* 0 or 1 */
+  int32_t window;        /* 0: no limit */
+  int32_t pad;
+} uad_attn;
+
+/* Bytes of device memory that uad_paged_attention needs for these arguments (0 is possible): host only, the same for
+ * the same sizes. table, len and start may be NULL here. Returns UAD_EINVAL (negative) for bad arguments. */
+int64_t uad_paged_attention_workspace(const uad_kv_pages* pages, const uad_kv_seqs* seqs, const uad_attn* attn);
+
+/* workspace: 16-byte aligned, in use until the call's work is done: calls that may run at the same time (other streams,
+ * graphs) need one each. It needs no preparation and carries nothing from call to call.
+ * Errors: UAD_EINVAL (arguments, workspace too small), UAD_ECUDA. */
+int uad_paged_attention(const uad_kv_pages* pages, const uad_kv_seqs* seqs, const uad_attn* attn, void* workspace,
+                        size_t workspace_bytes, int32_t* status, void* stream);
+
+/* ---- The projection of few tokens with 4-bit weights ------------------------------------------------------
+ * out[M][N] = x[M][K] w^T + bias with w[n][k] = (q[n][k] - zero[n][k / group]) * scale[n][k / group]: for the tokens of a
+ * decoding step, whose time is that of reading the weights. x: device bf16; q: device [N][K / 2], k even in the low
+ * four bits of byte k / 2; scale: device bf16 [N][K / group]; zero: device uint8 [N][K / group], 0..15 (only the low four
+ * bits are read), or NULL: 8; bias: device fp32 [N] or NULL; out: device fp32 [M][N]. Products of x and q - zero are exact
+ * and summed in fp32 over a group, then scaled. x and q 16-byte aligned. 1 <= M <= UAD_W4_MAX_ROWS, N >= 1, K % group == 0,
+ * group 32, 64 or 128, N * K < 2^40. Asynchronous on `stream` and in its order; allocates nothing; may be captured.
+ * Errors: UAD_EINVAL, UAD_ETOOBIG (M: dequantise and use uad_linear), UAD_ECUDA. */
+#define UAD_W4_MAX_ROWS 64
+int uad_linear_w4(const void* x, const uint8_t* q, const uint16_t* scale, const uint8_t* zero, const float* bias,
+                  float* out, int32_t M, int32_t N, int32_t K, int32_t group, void* stream);
+
+/* Round a linear weight to that form (host only). w: host fp32 [K][N] (y = x w), finite; q, scale (bf16 bits) and zero
+ * as above, host. zero NULL: symmetric, scale = max |w| / 7, values -7..7 (stored plus 8); else over [min(w, 0), max(w, 0)].
+ * scale is rounded to bf16 first and q to the nearest for it. Returns UAD_OK or UAD_EINVAL. */
+int uad_quantize_w4(const float* w, int32_t K, int32_t N, int32_t group, uint8_t* q, uint16_t* scale, uint8_t* zero);
+
 #ifdef __cplusplus
 }
 #endif

@@ -46,6 +46,31 @@ class uad_kernel_stat(C.Structure):
                 ("bytes", C.c_double), ("flops", C.c_double)]
 
 
+class uad_kv_pages(C.Structure):
+    _fields_ = [("k", _P), ("v", _P), ("page_stride", C.c_int64), ("slot_stride", C.c_int64), ("head_stride", C.c_int64)] + \
+               [(n, _I32) for n in ("dtype", "n_pages", "page_size", "n_kv_heads", "head_dim", "pad")]
+
+
+class uad_kv_seqs(C.Structure):
+    _fields_ = [("table", _P), ("len", _P), ("start", _P), ("table_stride", C.c_int64)] + \
+               [(n, _I32) for n in ("n_seqs", "table_width", "max_new", "max_len")]
+
+
+class uad_rope(C.Structure):
+    _fields_ = [("dim", _I32), ("pad", _I32), ("turn", C.c_uint64 * 128)]
+
+
+class uad_kv_rows(C.Structure):
+    _fields_ = [("q", _P), ("k", _P), ("v", _P), ("q_stride", C.c_int64), ("k_stride", C.c_int64), ("v_stride", C.c_int64),
+                ("q_out", _P), ("q_out_stride", C.c_int64), ("dtype", _I32), ("n_heads", _I32), ("n_rows", _I32), ("pad", _I32)]
+
+
+class uad_attn(C.Structure):
+    _fields_ = [("q", _P), ("out", _P), ("lse", _P), ("key_mask", _P), ("q_stride", C.c_int64), ("out_stride", C.c_int64),
+                ("mask_stride", C.c_int64), ("scale", C.c_float), ("n_heads", _I32), ("n_rows", _I32), ("causal", _I32),
+                ("window", _I32), ("pad", _I32)]
+
+
 def _fn(name, res, *args):
     f = getattr(_lib, name)
     f.restype = res
@@ -73,13 +98,23 @@ uad_linear_status = _fn("uad_linear_status", C.c_int)
 uad_linear_check = _fn("uad_linear_check", C.c_int, _P, _P, _P, _P, _I32, _I32, _I32, _P)
 uad_set_wait_limit = _fn("uad_set_wait_limit", C.c_int, _P, C.c_int64, _I32)
 uad_so3_check = _fn("uad_so3_check", C.c_int, _P, _I32, _P, _P)
+uad_rope_init = _fn("uad_rope_init", C.c_int, C.c_double, _I32, C.POINTER(uad_rope))
+_PAGES, _SEQS = C.POINTER(uad_kv_pages), C.POINTER(uad_kv_seqs)
+uad_kv_append = _fn("uad_kv_append", C.c_int, _PAGES, _SEQS, C.POINTER(uad_kv_rows), C.POINTER(uad_rope), _P, _P)
+uad_paged_attention_workspace = _fn("uad_paged_attention_workspace", C.c_int64, _PAGES, _SEQS, C.POINTER(uad_attn))
+uad_paged_attention = _fn("uad_paged_attention", C.c_int, _PAGES, _SEQS, C.POINTER(uad_attn), _P, C.c_size_t, _P, _P)
+uad_linear_w4 = _fn("uad_linear_w4", C.c_int, _P, _P, _P, _P, _P, _P, _I32, _I32, _I32, _I32, _P)
+uad_quantize_w4 = _fn("uad_quantize_w4", C.c_int, _P, _I32, _I32, _I32, _P, _P, _P)
 UAD_ETOOBIG = -7
+UAD_KV_BAD_PAGE, UAD_KV_BAD_SEQ = 1, 2
+UAD_W4_MAX_ROWS = 64
 
 EXPORTS = ["uad_version", "uad_last_error", "uad_init", "uad_set_prefix_kv", "uad_prepare_times",
            "uad_denoise", "uad_poll_released", "uad_finish", "uad_step_times",
            "uad_launches_per_chunk", "uad_destroy", "uad_plan_step", "uad_profile_chunk",
            "uad_tile_weight", "uad_linear", "uad_linear_static_scratch", "uad_set_wait_limit",
-           "uad_linear_status", "uad_linear_check", "uad_so3_check"]
+           "uad_linear_status", "uad_linear_check", "uad_so3_check", "uad_rope_init", "uad_kv_append",
+           "uad_paged_attention_workspace", "uad_paged_attention", "uad_linear_w4", "uad_quantize_w4"]
 
 
 def tile_weight(w):
@@ -161,6 +196,188 @@ def plan_step(budgets, k, tr=True):
     if ns < 0:
         raise UADError(ns, "invalid plan arguments")
     return ns, f, tn, td
+
+
+def _tensor(t, what, dtype, shape, device=None, rows=False):
+    """The address of a torch tensor that a kernel reads or writes: element type(s), shape (None: any size), contiguous
+    (rows: its rows alone, which may be apart) and on `device` (the GPU of the tensors beside it)."""
+    if str(t.dtype)[6:] not in dtype:
+        raise ValueError(f"{what}: expected {' or '.join(dtype)} elements, got {t.dtype}")
+    if t.dim() != len(shape) or any(a is not None and a != b for a, b in zip(shape, t.shape)):
+        raise ValueError(f"{what}: expected shape {list(shape)}, got {list(t.shape)}")
+    if not t.is_contiguous() and not (rows and t.dim() == 2 and t.stride(1) == 1 and t.stride(0) >= t.shape[1]):
+        raise ValueError(f"{what}: buffer must be contiguous" + (" along its rows" if rows else ""))
+    if t.device.type != "cuda" or (device is not None and t.device != device):
+        raise ValueError(f"{what}: must be on {'the GPU' if device is None else device}, is on {t.device}")
+    return t.data_ptr()
+
+
+def rope(theta, dim):
+    """Rotation of a head's first `dim` dimensions by its token's position: pair (i, i + dim / 2) by the angle
+    position * theta^(-2 i / dim). To be kept by the caller and given to PagedCache.append."""
+    r = uad_rope()
+    rc = uad_rope_init(theta, dim, C.byref(r))
+    if rc:
+        raise UADError(rc, "rope: dim must be a multiple of 16 up to 256, theta positive and finite")
+    return r
+
+
+class Sequences:
+    """A batch of sequences in a paged cache, as GPU tensors that the kernels read when they run: table int32
+    [n][pages of the longest], length int32 [n] (tokens in the cache, new ones included), start int32 [n + 1] (rows
+    start[b] .. start[b + 1] - 1 of the token tensors are the newest tokens of sequence b; None: row b is). max_new: at
+    least the largest number of new tokens of a sequence; max_len: about the longest length, from which attention splits
+    its work (0: what the table holds)."""
+
+    def __init__(self, table, length, start=None, max_len=0, max_new=1):
+        n = length.shape[0] if length.dim() else -1
+        self.n = n
+        tp = _tensor(table, "table", ("int32",), (n, None), rows=True)
+        lp = _tensor(length, "length", ("int32",), (n,), table.device)
+        sp = None if start is None else _tensor(start, "start", ("int32",), (n + 1,), table.device)
+        self.device = table.device
+        self._keep = table, length, start
+        self.seqs = uad_kv_seqs(table=tp, len=lp, start=sp, table_stride=table.stride(0) if n > 1 else max(1, table.shape[1]), n_seqs=n,
+                                table_width=table.shape[1], max_new=max_new, max_len=max_len)
+        self._ref = C.byref(self.seqs)
+
+
+class PagedCache:
+    """One layer's paged key-value cache on the GPU: k and v [n_pages][page_size][n_kv_heads][head_dim], float32 or
+    bfloat16, the last dimension contiguous, the others in any order (a view of [pages][heads][slots][dim], or of keys and
+    values in one tensor), both with the same strides. The tensors stay the caller's. Calls are asynchronous on `stream`
+    (None: the legacy default stream); `status`: an int32 tensor of one element that device-side findings
+    (UAD_KV_BAD_PAGE, UAD_KV_BAD_SEQ) are added to."""
+
+    def __init__(self, k, v):
+        if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.stride() != v.stride() or k.device != v.device:
+            raise ValueError("pages: k and v must be [n_pages][page_size][n_kv_heads][head_dim] of one type, device and strides")
+        self.dtype = str(k.dtype)[6:]
+        if self.dtype not in ("float32", "bfloat16"):
+            raise ValueError(f"pages: expected float32 or bfloat16 elements, got {k.dtype}")
+        if k.stride(3) != 1 or min(k.stride()) < 1:
+            raise ValueError("pages: the last dimension must be contiguous")
+        if k.device.type != "cuda":
+            raise ValueError(f"pages: must be on the GPU, is on {k.device}")
+        self.k, self.v, self.device = k, v, k.device
+        self.n_kv_heads, self.head_dim = k.shape[2], k.shape[3]
+        self.pages = uad_kv_pages(k=k.data_ptr(), v=v.data_ptr(), page_stride=k.stride(0), slot_stride=k.stride(1),
+                                  head_stride=k.stride(2), dtype=DTYPE["f32" if self.dtype == "float32" else "bf16"],
+                                  n_pages=k.shape[0], page_size=k.shape[1], n_kv_heads=k.shape[2], head_dim=k.shape[3])
+        self._ref = C.byref(self.pages)
+
+    def _status(self, status):
+        return None if status is None else _tensor(status, "status", ("int32",), (1,), self.device)
+
+    def _here(self, seqs):
+        if seqs.device != self.device:
+            raise ValueError(f"sequences: must be on {self.device}, are on {seqs.device}")
+
+    def _refused(self, rc, what):
+        raise UADError(rc, f"{what}: the arguments break a rule of include/uad.h, or the pages are not on the current device"
+                       if rc == UAD_EINVAL else what)
+
+    def append(self, seqs, k=None, v=None, q=None, q_out=None, rope=None, status=None, stream=None):
+        """Write the new tokens' keys and values [rows][n_kv_heads * head_dim] into their pages and their queries
+        [rows][n_heads * head_dim] into q_out, keys and queries rotated by `rope` (None: not). float32 or bfloat16 rows,
+        which may be parts of a fused projection; q_out in the cache's type."""
+        self._here(seqs)
+        first = q if k is None else k
+        if first is None:
+            raise ValueError("append: neither keys nor queries")
+        kind, n = (str(first.dtype)[6:],), first.shape[0] if first.dim() else 0
+        if kind[0] not in ("float32", "bfloat16"):
+            raise ValueError(f"append: expected float32 or bfloat16 rows, got {first.dtype}")
+        r = uad_kv_rows(dtype=DTYPE["f32" if kind[0] == "float32" else "bf16"], n_rows=n)
+        width = self.n_kv_heads * self.head_dim
+        if (k is None) != (v is None) or (q is None) != (q_out is None):
+            raise ValueError("append: k goes with v, q with q_out")
+        if k is not None:
+            r.k, r.k_stride = _tensor(k, "k", kind, (n, width), self.device, True), k.stride(0)
+            r.v, r.v_stride = _tensor(v, "v", kind, (n, width), self.device, True), v.stride(0)
+        if q is not None:
+            r.q, r.q_stride = _tensor(q, "q", kind, (n, None), self.device, True), q.stride(0)
+            r.q_out, r.q_out_stride = _tensor(q_out, "q_out", (self.dtype,), tuple(q.shape), self.device, True), q_out.stride(0)
+            r.n_heads, rest = divmod(q.shape[1], self.head_dim)
+            if rest:
+                raise ValueError(f"q: expected a multiple of {self.head_dim} columns, got {q.shape[1]}")
+        rc = uad_kv_append(self._ref, seqs._ref, C.byref(r), None if rope is None else C.byref(rope), self._status(status),
+                           _stream_handle(stream))
+        if rc:
+            self._refused(rc, "append")
+
+    def _attn(self, rows, n_heads, scale=None, causal=True, window=0):
+        return uad_attn(scale=scale or 0.0, n_heads=n_heads, n_rows=rows, causal=int(causal), window=window)
+
+    def attention_workspace(self, seqs, rows, n_heads, window=0):
+        """Bytes of the workspace that attention of these sizes needs (0 is possible)."""
+        n = uad_paged_attention_workspace(self._ref, seqs._ref, C.byref(self._attn(rows, n_heads, window=window)))
+        if n < 0:
+            self._refused(n, "attention_workspace")
+        return n
+
+    def attention(self, seqs, q, out, workspace=None, scale=None, causal=True, window=0, key_mask=None, lse=None, status=None,
+                  stream=None):
+        """out = softmax(scale q k) v of the new tokens' queries [rows][n_heads * head_dim] over their sequences' pages
+        (scale None: 1 / sqrt(head_dim)). causal: a token sees the keys up to its own; window > 0: no more than so many; key_mask
+        uint8 [sequences][>= longest length]: only where it is not 0. Where a token sees nothing, out is 0 and lse
+        (float32 [rows][n_heads]) -inf. workspace: a uint8 tensor of attention_workspace bytes, not shared by calls that may
+        run at the same time."""
+        self._here(seqs)
+        n = q.shape[0] if q.dim() else 0
+        qp = _tensor(q, "q", (self.dtype,), (n, None), self.device, True)
+        heads, rest = divmod(q.shape[1], self.head_dim)
+        if rest:
+            raise ValueError(f"q: expected a multiple of {self.head_dim} columns, got {q.shape[1]}")
+        a = self._attn(n, heads, scale, causal, window)
+        a.q, a.q_stride = qp, q.stride(0)
+        a.out, a.out_stride = _tensor(out, "out", (self.dtype,), tuple(q.shape), self.device, True), out.stride(0)
+        if lse is not None:
+            a.lse = _tensor(lse, "lse", ("float32",), (n, heads), self.device)
+        if key_mask is not None:
+            a.key_mask = _tensor(key_mask, "key_mask", ("uint8",), (seqs.n, None), self.device, True)
+            a.mask_stride = key_mask.stride(0)
+            if key_mask.shape[1] < seqs.seqs.table_width * self.pages.page_size:
+                raise ValueError(f"key_mask: expected {seqs.seqs.table_width * self.pages.page_size} columns, what the table holds")
+        wp, wn = (None, 0) if workspace is None else (_tensor(workspace, "workspace", ("uint8",), (None,), self.device), workspace.numel())
+        rc = uad_paged_attention(self._ref, seqs._ref, C.byref(a), wp, wn, self._status(status), _stream_handle(stream))
+        if rc:
+            self._refused(rc, "attention")
+
+
+def quantize_w4(w, group=64, symmetric=False):
+    """fp32 [K][N] -> (q uint8 [N][K / 2], scale [N][K / group] as uint16 bf16 bits, zero uint8 [N][K / group] or None) for
+    linear_w4 (host only)."""
+    w = np.ascontiguousarray(w, dtype=np.float32)
+    K, N = w.shape
+    g = K // group if group > 0 else 0
+    q, scale = np.empty((N, K // 2), np.uint8), np.empty((N, g), np.uint16)
+    zero = None if symmetric else np.empty((N, g), np.uint8)
+    rc = uad_quantize_w4(_ptr(w), K, N, group, _ptr(q), _ptr(scale), _ptr(zero))
+    if rc:
+        raise UADError(rc, "quantize_w4: needs finite weights, group 32, 64 or 128 and K % group == 0")
+    return q, scale, zero
+
+
+def linear_w4(x, q, scale, out, zero=None, bias=None, stream=None):
+    """out [M][N] = x [M][K] w^T + bias with w = (q - zero) * scale, 4 bits a weight (zero None: 8): x bfloat16, q uint8
+    [N][K / 2] (the even k in the low bits), scale bfloat16 and zero uint8 [N][K / group], bias and out float32; group 32, 64 or
+    128, M up to UAD_W4_MAX_ROWS. Asynchronous on `stream` (None: the legacy default stream)."""
+    M, K = x.shape if x.dim() == 2 else (0, 0)
+    N, groups = scale.shape if scale.dim() == 2 else (0, 0)
+    xp = _tensor(x, "x", ("bfloat16",), (M, K))
+    d = x.device
+    qp = _tensor(q, "q", ("uint8",), (N, K // 2), d)
+    sp = _tensor(scale, "scale", ("bfloat16",), (N, groups), d)
+    zp = None if zero is None else _tensor(zero, "zero", ("uint8",), (N, groups), d)
+    bp = None if bias is None else _tensor(bias, "bias", ("float32",), (N,), d)
+    op = _tensor(out, "out", ("float32",), (M, N), d)
+    if groups < 1 or K % groups:
+        raise ValueError(f"scale: {groups} groups do not divide {K} columns")
+    rc = uad_linear_w4(xp, qp, sp, zp, bp, op, M, N, K, K // groups, _stream_handle(stream))
+    if rc:
+        raise UADError(rc, "linear_w4: group must be 32, 64 or 128, x and q 16-byte aligned and on the current device, at most "
+                       f"{UAD_W4_MAX_ROWS} rows")
 
 
 class Expert:

@@ -1,0 +1,212 @@
+// The paged key-value cache: argument checks, the rotation's frequencies and the append of new tokens.
+#include "kv_pages.cuh"
+
+#include <cmath>
+
+using namespace uad;
+
+namespace {
+
+constexpr int kItem = 16;   // dimensions that a thread takes of a head: 8 pairs, or 16 that are not rotated
+
+struct AppendArgs {
+  PagedArgs p;
+  const void *q, *k, *v;
+  int64_t q_stride, k_stride, v_stride, q_out_stride;
+  void* q_out;
+  int n_heads, rot;
+};
+
+// cos and sin of position * turn / 2^64 turns. The product wraps at whole turns, which is exact; what is left is
+// taken to the nearest quarter, so that its rounding to fp32 is below 2^-28 of a turn.
+__device__ __forceinline__ void rotation(uint32_t pos, uint64_t turn, float* c, float* s) {
+  const uint64_t ph = (uint64_t)pos * turn + (1ull << 61);
+  const int quarter = (int)(ph >> 62);
+  const int64_t rest = (int64_t)(ph & ((1ull << 62) - 1)) - (1ll << 61);   // within an eighth of a turn
+  float cr, sr;
+  sincospif((float)(int32_t)(rest >> 32) * 4.656612873077393e-10f, &sr, &cr);   // 2^-31: half turns of 2^-32 turns
+  const float a = quarter & 1 ? -sr : cr, b = quarter & 1 ? cr : sr;
+  *c = quarter & 2 ? -a : a;
+  *s = quarter & 2 ? -b : b;
+}
+
+template <int T>
+__device__ __forceinline__ void load8(const void* base, int64_t e, float* x) {
+  if constexpr (T == F32) {
+    const float4* f = reinterpret_cast<const float4*>(static_cast<const float*>(base) + e);
+    const float4 a = f[0], b = f[1];
+    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+  } else {
+    const uint4 u = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(base) + e);
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = __uint_as_float(w[i] << 16);
+      x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+  }
+}
+template <int T>
+__device__ __forceinline__ void store8(void* base, int64_t e, const float* x) {
+  if constexpr (T == F32) {
+    float4* f = reinterpret_cast<float4*>(static_cast<float*>(base) + e);
+    f[0] = make_float4(x[0], x[1], x[2], x[3]);
+    f[1] = make_float4(x[4], x[5], x[6], x[7]);
+  } else {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+      w[i] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+    *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(base) + e) = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+}
+
+// One thread: 16 dimensions (8 pairs) of one head of one row.
+template <int IN, int CACHE>
+__global__ void __launch_bounds__(256) append_kernel(const AppendArgs a, const __grid_constant__ uad_rope rope) {
+  pdl_wait();
+  pdl_trigger();
+  const PagedArgs& p = a.p;
+  const int b = blockIdx.y;
+  const SeqRows s = seq_rows(p, b);
+  if (s.n < 0) {
+    if (blockIdx.x == 0 && threadIdx.x == 0) kv_report(p, UAD_KV_BAD_SEQ);
+    return;
+  }
+  const int per_head = p.dh / kItem, heads = a.n_heads + (a.k ? 2 * p.n_kv : 0), per_row = heads * per_head;
+  const int64_t item = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+  const int j = (int)(item / per_row), r = (int)(item - (int64_t)j * per_row), head = r / per_head, c = r - head * per_head;
+  if (j >= s.n) return;
+  const int row = s.first + j, pos = s.len - s.n + j;
+  const bool is_q = head < a.n_heads;
+  const int kv = head - a.n_heads;
+  const bool is_v = !is_q && kv >= p.n_kv;
+  const int h = is_q ? head : is_v ? kv - p.n_kv : kv;
+  int64_t dst;
+  if (is_q) {
+    dst = row * a.q_out_stride + (int64_t)h * p.dh;
+  } else {
+    dst = token_at(p, p.table + b * p.table_stride, pos);
+    if (dst < 0) {
+      kv_report(p, UAD_KV_BAD_PAGE);
+      return;
+    }
+    dst += h * p.head_stride;
+  }
+  const void* from = is_q ? a.q : is_v ? a.v : a.k;
+  void* to = is_q ? a.q_out : is_v ? p.v : p.k;
+  const int64_t src = row * (is_q ? a.q_stride : is_v ? a.v_stride : a.k_stride) + (int64_t)h * p.dh;
+  const int half = a.rot / 2;
+  const bool turned = !is_v && c * 8 < half;
+  // pairs (lo + i, hi + i); past the rotated dimensions, 16 neighbours
+  const int lo = turned ? c * 8 : c * kItem, hi = turned ? lo + half : lo + 8;
+  float x[8], y[8];
+  load8<IN>(from, src + lo, x);
+  load8<IN>(from, src + hi, y);
+  if (turned) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      float cs, sn;
+      rotation((uint32_t)pos, rope.turn[lo + i], &cs, &sn);
+      const float u = x[i] * cs - y[i] * sn, w = y[i] * cs + x[i] * sn;
+      x[i] = u;
+      y[i] = w;
+    }
+  }
+  store8<CACHE>(to, dst + lo, x);
+  store8<CACHE>(to, dst + hi, y);
+}
+
+bool bad_address(const void* p, int64_t stride, int es) {
+  return reinterpret_cast<uintptr_t>(p) % 16 != 0 || stride < 0 || (stride * es) % 16 != 0;
+}
+
+}  // namespace
+
+bool uad::on_current_device(const void* p) {
+  int dev = 0;
+  cudaPointerAttributes at{};
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaPointerGetAttributes(&at, p) != cudaSuccess) {
+    cudaGetLastError();
+    return false;
+  }
+  return (at.type == cudaMemoryTypeDevice && at.device == dev) || at.type == cudaMemoryTypeManaged;
+}
+
+int uad::paged_args(const uad_kv_pages* g, const uad_kv_seqs* s, int n_rows, bool device, PagedArgs* p) {
+  if (!g || !s || !g->k || !g->v) return UAD_EINVAL;
+  if (g->dtype != UAD_DTYPE_F32 && g->dtype != UAD_DTYPE_BF16) return UAD_EINVAL;
+  const int es = g->dtype == UAD_DTYPE_F32 ? 4 : 2;
+  if (g->head_dim != 64 && g->head_dim != 128 && g->head_dim != 256) return UAD_EINVAL;
+  if (g->n_pages < 1 || g->page_size < 1 || g->page_size > 65536 || g->n_kv_heads < 1 || g->n_kv_heads > 1024) return UAD_EINVAL;
+  if (g->page_stride < 1 || g->slot_stride < 1 || g->head_stride < 1) return UAD_EINVAL;
+  if (bad_address(g->k, g->page_stride, es) || bad_address(g->v, g->slot_stride, es) || bad_address(nullptr, g->head_stride, es))
+    return UAD_EINVAL;
+  if (s->n_seqs < 0 || s->n_seqs > 65535 || s->max_new < 1 || s->max_len < 0 || s->table_width < 1) return UAD_EINVAL;
+  if ((int64_t)s->table_width * g->page_size >= (1ll << 31) || s->table_stride < s->table_width) return UAD_EINVAL;
+  if (n_rows < 0 || (!s->start && n_rows < s->n_seqs)) return UAD_EINVAL;
+  if (device && s->n_seqs > 0 && n_rows > 0) {
+    if (!s->table || !s->len) return UAD_EINVAL;
+    if (!on_current_device(g->k)) return UAD_EINVAL;
+  }
+  p->k = g->k; p->v = g->v;
+  p->page_stride = g->page_stride; p->slot_stride = g->slot_stride; p->head_stride = g->head_stride;
+  p->table = s->table; p->len = s->len; p->start = s->start; p->table_stride = s->table_stride;
+  p->page = FastDiv((uint32_t)g->page_size);
+  p->n_pages = g->n_pages; p->n_kv = g->n_kv_heads; p->dh = g->head_dim; p->dtype = g->dtype == UAD_DTYPE_F32 ? F32 : BF16;
+  p->n_seqs = s->n_seqs; p->n_rows = n_rows; p->max_new = s->max_new < n_rows ? s->max_new : (n_rows > 0 ? n_rows : 1);
+  p->capacity = s->table_width * g->page_size;
+  return UAD_OK;
+}
+
+extern "C" {
+
+int uad_rope_init(double theta, int32_t dim, uad_rope* out) {
+  if (!out || dim < 16 || dim > 256 || dim % 16 || !(theta > 0) || !std::isfinite(theta)) return UAD_EINVAL;
+  *out = uad_rope{};
+  out->dim = dim;
+  for (int i = 0; i < dim / 2; ++i) {
+    // turns a position; whole ones drop out. In long double (64 bits of mantissa and more): a double's last bit is
+    // 2e-7 rad of the first angles at 2^31 tokens
+    const long double t = std::pow((long double)theta, -2.0L * i / dim) * 0.159154943091895335768883763372514362L;
+    out->turn[i] = (uint64_t)std::ldexp(t - std::floor(t), 64);
+  }
+  return UAD_OK;
+}
+
+int uad_kv_append(const uad_kv_pages* pages, const uad_kv_seqs* seqs, const uad_kv_rows* rows, const uad_rope* rope,
+                  int32_t* status, void* stream) {
+  if (!rows) return UAD_EINVAL;
+  AppendArgs a{};
+  const int rc = paged_args(pages, seqs, rows->n_rows, true, &a.p);
+  if (rc) return rc;
+  if (rows->dtype != UAD_DTYPE_F32 && rows->dtype != UAD_DTYPE_BF16) return UAD_EINVAL;
+  const int es = rows->dtype == UAD_DTYPE_F32 ? 4 : 2, ces = a.p.dtype == F32 ? 4 : 2;
+  if (!rows->k != !rows->v || (!rows->q && !rows->k)) return UAD_EINVAL;
+  if (rows->q ? rows->n_heads < 1 || rows->n_heads > 65536 || !rows->q_out : rows->n_heads != 0) return UAD_EINVAL;
+  if (bad_address(rows->q, rows->q_stride, es) || bad_address(rows->k, rows->k_stride, es) || bad_address(rows->v, rows->v_stride, es) ||
+      bad_address(rows->q_out, rows->q_out_stride, ces))
+    return UAD_EINVAL;
+  if (rope && (rope->dim < 16 || rope->dim > a.p.dh || rope->dim % 16)) return UAD_EINVAL;
+  if (a.p.n_seqs == 0 || a.p.n_rows == 0) return UAD_OK;
+  a.p.status = status;
+  a.q = rows->q; a.k = rows->k; a.v = rows->v;
+  a.q_stride = rows->q_stride; a.k_stride = rows->k_stride; a.v_stride = rows->v_stride;
+  a.q_out = rows->q_out; a.q_out_stride = rows->q_out_stride;
+  a.n_heads = rows->n_heads; a.rot = rope ? rope->dim : 0;
+  const uad_rope none{};
+  const int64_t items = (int64_t)a.p.max_new * (a.n_heads + (a.k ? 2 * a.p.n_kv : 0)) * (a.p.dh / kItem);
+  const int64_t blocks = (items + 255) / 256;
+  if (blocks > 0x7fffffff) return UAD_EINVAL;
+  const dim3 grid((unsigned)blocks, (unsigned)a.p.n_seqs);
+  const uad_rope& r = rope ? *rope : none;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  const bool in32 = rows->dtype == UAD_DTYPE_F32, out32 = a.p.dtype == F32;
+  const cudaError_t e = in32 ? (out32 ? launch_k(append_kernel<F32, F32>, grid, 256, 0, s, a, r) : launch_k(append_kernel<F32, BF16>, grid, 256, 0, s, a, r))
+                             : (out32 ? launch_k(append_kernel<BF16, F32>, grid, 256, 0, s, a, r) : launch_k(append_kernel<BF16, BF16>, grid, 256, 0, s, a, r));
+  return e == cudaSuccess ? UAD_OK : UAD_ECUDA;
+}
+
+}  // extern "C"

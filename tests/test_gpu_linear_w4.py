@@ -1,0 +1,139 @@
+"""GPU parity of the 4-bit projection against its 64-bit reference.
+
+Tolerance: products of bf16 and whole numbers up to 15 are exact; a group's sum of at most 128 of them is off by an ulp a
+step (the tensor cores truncate), 2^-23 of the sum of magnitudes each, as is every group that is added: (group + groups + 2)
+2^-23 sum |x w|, and the output's own half step 2^-24.
+"""
+import numpy as np
+import pytest
+import torch
+
+import paper_2609_37772_gb300 as uad
+from oracle import paged
+
+pytestmark = pytest.mark.gpu
+
+
+def operands(M, N, K, group, zero, seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    q = torch.randint(0, 256, (N, K // 2), generator=g, device="cuda", dtype=torch.uint8)
+    scale = (torch.rand((N, K // group), generator=g, device="cuda") * 0.01 - 0.002).bfloat16()
+    z = torch.randint(0, 256, (N, K // group), generator=g, device="cuda", dtype=torch.uint8) if zero else None
+    x = torch.randn((M, K), generator=g, device="cuda").bfloat16()
+    return x, q, scale, z, torch.randn(N, generator=g, device="cuda")
+
+
+def reference(x, q, scale, z, bias):
+    w = paged.dequantize(q.cpu().numpy(), scale.float().cpu().numpy(), None if z is None else z.cpu().numpy())
+    xn = x.double().cpu().numpy()
+    with np.errstate(all="ignore"):
+        return xn @ w.T + (0 if bias is None else bias.double().cpu().numpy()), np.abs(xn) @ np.abs(w).T
+
+
+def check(out, want, size, K, group, bias):
+    tol = (group + K // group + 2) * 2.0 ** -23 * size + 2.0 ** -23 * (np.abs(want) + (0 if bias is None else np.abs(bias.double().cpu().numpy()))) + 1e-30
+    err = np.abs(out.double().cpu().numpy() - want)
+    assert np.all(err <= tol), float((err / tol).max())
+
+
+SHAPES = [(1, 1, 32, 32), (1, 16, 64, 64), (1, 17, 128, 128), (1, 2560, 1024, 64), (1, 100, 4096, 128), (2, 33, 96, 32), (3, 1000, 256, 128),
+          (5, 2048, 8192, 32), (7, 15, 384, 128), (8, 64, 2048, 64), (9, 640, 160, 32), (16, 129, 512, 64), (17, 77, 704, 64), (24, 4608, 1536, 128),
+          (31, 31, 992, 32), (32, 256, 1024, 128), (33, 513, 320, 64), (40, 1409, 4096, 64), (63, 48, 640, 128), (64, 1024, 2048, 32), (64, 7, 12288, 128)]
+
+
+@pytest.mark.parametrize("M,N,K,group", SHAPES)
+@pytest.mark.parametrize("zero", [False, True])
+def test_linear_w4_matches_reference(M, N, K, group, zero):
+    x, q, scale, z, bias = operands(M, N, K, group, zero, M + N + K)
+    bias = bias if zero else None
+    room = torch.full((M + 2, N), 7.5, device="cuda")
+    uad.linear_w4(x, q, scale, room[1:M + 1], zero=z, bias=bias)
+    torch.cuda.synchronize()
+    want, size = reference(x, q, scale, z, bias)
+    check(room[1:M + 1], want, size, K, group, bias)
+    assert bool((room[0] == 7.5).all()) and bool((room[M + 1] == 7.5).all())
+
+
+@pytest.mark.parametrize("M", [1, 2, 4, 8, 12, 20, 36, 50, 64])
+def test_rows_do_not_depend_on_each_other(M):
+    """A row's values are its own whatever is beside it: NaN and infinities stay in their rows."""
+    x, q, scale, z, bias = operands(M, 96, 512, 64, True, M)
+    clean = torch.empty(M, 96, device="cuda")
+    uad.linear_w4(x, q, scale, clean, zero=z, bias=bias)
+    x2 = x.clone()
+    x2[M // 2, 5] = float("nan")
+    x2[M - 1, 500] = float("inf")
+    out = torch.empty(M, 96, device="cuda")
+    uad.linear_w4(x2, q, scale, out, zero=z, bias=bias)
+    torch.cuda.synchronize()
+    same = [m for m in range(M) if m not in (M // 2, M - 1)]
+    assert torch.equal(out[same], clean[same])
+    assert bool(torch.isnan(out[M // 2]).all()) and not bool(torch.isfinite(out[M - 1]).any() and M > 1 and M // 2 != M - 1 and
+                                                             bool(((out[M - 1] != clean[M - 1]) & torch.isfinite(out[M - 1])).any()))
+
+
+def test_quantized_weights_give_what_they_stand_for():
+    rng = np.random.default_rng(3)
+    w = (rng.normal(size=(512, 200)) * 0.02).astype(np.float32)
+    x = torch.from_numpy(rng.normal(size=(3, 512)).astype(np.float32)).cuda().bfloat16()
+    for symmetric in (False, True):
+        q, s, z = uad.quantize_w4(w, 64, symmetric)
+        scale = torch.from_numpy(s.view(np.int16)).cuda().view(torch.bfloat16)
+        zt = None if z is None else torch.from_numpy(z).cuda()
+        out = torch.empty(3, 200, device="cuda")
+        uad.linear_w4(x, torch.from_numpy(q).cuda(), scale, out, zero=zt)
+        torch.cuda.synchronize()
+        want, size = reference(x, torch.from_numpy(q), scale, zt, None)
+        check(out, want, size, 512, 64, None)
+        full = x.double().cpu().numpy() @ w.astype(np.float64)
+        step = float(scale.float().max())
+        assert np.abs(want - full).max() <= step * 1.06 * np.abs(x.double().cpu().numpy()).sum(axis=1).max()
+
+
+def test_linear_w4_is_the_same_every_time_on_streams_and_in_graphs():
+    """In stream order with its weights' and inputs' writers; replayed with other inputs; the same bits every time."""
+    x, q, scale, z, bias = operands(5, 2048, 4096, 64, True, 1)
+    xs = [torch.randn(5, 4096, device="cuda").bfloat16() for _ in range(4)]
+    st, out = torch.cuda.Stream(), torch.empty(5, 2048, device="cuda")
+    alone = []
+    for v in xs:
+        o = torch.empty(5, 2048, device="cuda")
+        uad.linear_w4(v, q, scale, o, zero=z, bias=bias)
+        alone.append(o)
+    torch.cuda.synchronize()
+    got = []
+    with torch.cuda.stream(st):
+        for v in xs * 3:
+            x.copy_(v)
+            uad.linear_w4(x, q, scale, out, zero=z, bias=bias, stream=st)
+            got.append(out.clone())
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, alone[i % 4]) for i, o in enumerate(got))
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=st):
+        uad.linear_w4(x, q, scale, out, zero=z, bias=bias, stream=st)
+    for i, v in enumerate(xs):
+        x.copy_(v)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, alone[i])
+
+
+@pytest.mark.parametrize("M", [1, 7, 40])
+def test_unaligned_outputs_scales_and_biases(M):
+    """Outputs, bias, scales and zeros at any element address; nothing around the output is written."""
+    N, K = 75, 320
+    x, q, scale, z, bias = operands(M, N, K, 64, True, M)
+    room = torch.full((M * N + 3,), 7.5, device="cuda")
+    s1, z1 = torch.zeros(scale.numel() + 1, device="cuda", dtype=torch.bfloat16), torch.zeros(z.numel() + 1, device="cuda", dtype=torch.uint8)
+    s1[1:] = scale.reshape(-1)
+    z1[1:] = z.reshape(-1)
+    b1 = torch.cat([bias[:1], bias])
+    out = room[1:1 + M * N].view(M, N)
+    uad.linear_w4(x, q, s1[1:].view(N, -1), out, zero=z1[1:].view(N, -1), bias=b1[1:])
+    torch.cuda.synchronize()
+    want, size = reference(x, q, scale, z, bias)
+    check(out, want, size, K, 64, bias)
+    assert float(room[0]) == 7.5 and bool((room[1 + M * N:] == 7.5).all())
