@@ -324,7 +324,7 @@ typedef struct uad_kv_seqs {
   const int32_t* start;  /* [n_seqs + 1], ascending from 0 or more; NULL: row b is the one new token of sequence b */
   int64_t table_stride;
   int32_t n_seqs;        /* 0..65535 */
-  int32_t table_width;   /* >= 1; table_width * page_size < 2^31 */
+  int32_t table_width;   /* >= 1; table_width * page_size <= 2^31 - 2^17 */
   int32_t max_new;       /* at least the largest number of new tokens of a sequence, >= 1 */
   int32_t max_len;       /* attention: about the longest len, from which the work is split (0: table_width * page_size). A
                             longer sequence is served too, less evenly */

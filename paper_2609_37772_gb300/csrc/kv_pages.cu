@@ -145,7 +145,7 @@ int uad::paged_args(const uad_kv_pages* g, const uad_kv_seqs* s, int n_rows, boo
   if (bad_address(g->k, g->page_stride, es) || bad_address(g->v, g->slot_stride, es) || bad_address(nullptr, g->head_stride, es))
     return UAD_EINVAL;
   if (s->n_seqs < 0 || s->n_seqs > 65535 || s->max_new < 1 || s->max_len < 0 || s->table_width < 1) return UAD_EINVAL;
-  if ((int64_t)s->table_width * g->page_size >= (1ll << 31) || s->table_stride < s->table_width) return UAD_EINVAL;
+  if ((int64_t)s->table_width * g->page_size > (1ll << 31) - (1 << 17) || s->table_stride < s->table_width) return UAD_EINVAL;
   if (n_rows < 0 || (!s->start && n_rows < s->n_seqs)) return UAD_EINVAL;
   if (device && s->n_seqs > 0 && n_rows > 0) {
     if (!s->table || !s->len) return UAD_EINVAL;
