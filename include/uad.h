@@ -376,7 +376,7 @@ typedef struct uad_attn {
   const void* q;         /* cache's type, head h of row t at t * q_stride + h * head_dim, 16-byte aligned */
   void* out;             /* the same with out_stride; must not overlap q */
   float* lse;            /* [n_rows][n_heads] natural logarithm of the softmax's denominator; NULL: not wanted */
-  const uint8_t* key_mask;
+  const uint8_t* key_mask;   /* rows of table_width * page_size bytes, mask_stride apart */
   int64_t q_stride, out_stride, mask_stride;
   float scale;           /* 0: 1 / sqrt(head_dim) */
   int32_t n_heads;       /* a multiple of n_kv_heads, at most 64 times it */
