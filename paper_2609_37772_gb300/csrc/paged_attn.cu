@@ -33,19 +33,21 @@ struct PagedAttnArgs {
 };
 
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
-constexpr int kMaxCluster = 8;
+constexpr int kMaxCluster = 16;   // more than 8 need the opt-in of non-portable sizes
 // A seen key's score is at least this, a hidden one's -infinity: a row that sees nothing (0) and one whose every score
 // is -infinity (undefined) stay apart.
 constexpr float kLeast = -3.402823466e38f;
 
-// The final division: what a row is from the sum of weighted values `x`, their weights' sum and the scores' maximum.
-__device__ __forceinline__ float attn_value(float x, float m, float l) {
-  return m == -INFINITY && l == 0.f ? 0.f : m == kLeast ? NAN : x / l;
+// 1 / l: what a row's weighted values are multiplied by in the end, from their weights' sum and the scores' maximum.
+__device__ __forceinline__ float row_factor(float m, float l) {
+  const float f = 1.f / l;
+  return m == -INFINITY && l == 0.f ? 0.f : m == kLeast ? NAN : f;
 }
-__device__ __forceinline__ float attn_lse(float m, float l) {
+__device__ __forceinline__ float row_lse(float m, float l) {
   return m == -INFINITY && l == 0.f ? -INFINITY : m == kLeast ? NAN : (m + log2f(l)) * 0.6931471805599453f;
 }
-__device__ __forceinline__ float weight(float m, float top) { return m == top ? 1.f : exp2f(m - top); }
+// 2^(m - top), 1 also where both are infinite. Without a branch: a CTA's end is a chain of such steps.
+__device__ __forceinline__ float weight(float m, float top) { return ex2_approx(m == top ? 0.f : m - top); }
 
 // The rows and keys of a warp: rows r0 .. r0 + rows - 1 of (new token, head of the group), keys k0 .. k1 - 1, of which it
 // takes the slices kw, kw + wk, ...
@@ -76,9 +78,10 @@ __device__ __forceinline__ int64_t key_at(const PagedAttnArgs& a, const Piece& c
   }
   return f.page * a.p.page_stride + (f.key - (int)(a.p.page.div(f.key) * a.p.page.d)) * a.p.slot_stride + c.kvh * a.p.head_stride;
 }
-// What this warp has to do; `first`: the warp's first slice's keys (one a lane of `slice` lanes), already on their way.
+// What this warp has to do; found[N]: the keys of its first N slices (one a lane of `slice` lanes), already on their way.
 // False: the whole CTA (and cluster) has nothing to do.
-__device__ __forceinline__ bool find_piece(const PagedAttnArgs& a, int block_rows, int slice, Piece* c, Found* first) {
+template <int N>
+__device__ __forceinline__ bool find_piece(const PagedAttnArgs& a, int block_rows, int slice, Piece* c, Found* found) {
   const PagedArgs& p = a.p;
   const int b = blockIdx.z, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int x = (int)a.by_x.div(blockIdx.x), rest = blockIdx.x - x * (int)a.by_x.d;
@@ -95,7 +98,8 @@ __device__ __forceinline__ bool find_piece(const PagedAttnArgs& a, int block_row
   if (a.window > 0) lo = max(0, before + (int)a.by_group.div(c->r0) - a.window + 1);
   const int64_t from = lo + (int64_t)c->piece * a.piece_keys;
   c->k0 = (int)(from < p.capacity ? from : p.capacity);
-  *first = find_key(a, c->k0 + c->kw * slice + lane % slice);
+#pragma unroll
+  for (int i = 0; i < N; ++i) found[i] = find_key(a, c->k0 + (i * c->wk + c->kw) * slice + lane % slice);
   if (c->s.n < 0) {
     if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) kv_report(p, UAD_KV_BAD_SEQ);
     return false;
@@ -133,23 +137,18 @@ template <int N>
 __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 
-__device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ uint32_t peer(uint32_t s, uint32_t rank) {
   uint32_t r;
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(s), "r"(rank));
   return r;
 }
-__device__ __forceinline__ float4 peer_f4(uint32_t s) {
-  float4 v;
-  asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(s) : "memory");
-  return v;
+__device__ __forceinline__ void put_peer(uint32_t s, float4 v) {
+  asm volatile("st.shared::cluster.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(s), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
 }
-__device__ __forceinline__ float2 peer_f2(uint32_t s) {
-  float2 v;
-  asm volatile("ld.shared::cluster.v2.f32 {%0,%1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(s) : "memory");
-  return v;
+__device__ __forceinline__ void put_peer(uint32_t s, float2 v) {
+  asm volatile("st.shared::cluster.v2.f32 [%0], {%1,%2};" ::"r"(s), "f"(v.x), "f"(v.y) : "memory");
 }
 
 // A piece that has no keys says so and is done (in a cluster it takes part in the joining). True: it was one.
@@ -160,311 +159,298 @@ __device__ __forceinline__ bool no_keys(const PagedAttnArgs& a, const Piece& c) 
   return true;
 }
 
-// CNT dimensions from d of row r, final or as a piece.
-template <int T, int CNT>
-__device__ __forceinline__ void put_row(const PagedAttnArgs& a, const Piece& c, int r, int d, const float* x, float m, float l, bool joined) {
+// Four dimensions from d of row r, final or as a piece.
+template <int T>
+__device__ __forceinline__ void put_row(const PagedAttnArgs& a, const Piece& c, int r, int d, float4 x, float m, float l, bool joined) {
   if (!joined) {
     const int64_t at = row_at(a, c, r, a.n_heads, 1) * a.pieces + c.piece;
-    float* o = a.part_o + at * a.p.dh + d;
-    if constexpr (CNT == 2) *reinterpret_cast<float2*>(o) = make_float2(x[0], x[1]);
-#pragma unroll
-    for (int i = 0; i + 4 <= CNT; i += 4) *reinterpret_cast<float4*>(o + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+    *reinterpret_cast<float4*>(a.part_o + at * a.p.dh + d) = x;
     if (d == 0) a.part_ml[at] = make_float2(m, l);
     return;
   }
-  float y[CNT];
-#pragma unroll
-  for (int i = 0; i < CNT; ++i) y[i] = attn_value(x[i], m, l);
+  const float f = row_factor(m, l);
   const int64_t e = row_at(a, c, r, a.out_stride, a.p.dh) + d;
-  if constexpr (T == F32) {
-    float* o = static_cast<float*>(a.out) + e;
-#pragma unroll
-    for (int i = 0; i < CNT; i += 4) *reinterpret_cast<float4*>(o + i) = make_float4(y[i], y[i + 1], y[i + 2], y[i + 3]);
-  } else {
-    uint32_t w[CNT / 2];
-#pragma unroll
-    for (int i = 0; i < CNT / 2; ++i) w[i] = pack_bf16(y[2 * i], y[2 * i + 1]);
-    __nv_bfloat16* o = static_cast<__nv_bfloat16*>(a.out) + e;
-    if constexpr (CNT == 8) *reinterpret_cast<uint4*>(o) = make_uint4(w[0], w[1], w[2], w[3]);
-    else *reinterpret_cast<uint32_t*>(o) = w[0];
-  }
-  if (a.lse && d == 0) a.lse[row_at(a, c, r, a.n_heads, 1)] = attn_lse(m, l);
+  if constexpr (T == F32) *reinterpret_cast<float4*>(static_cast<float*>(a.out) + e) = make_float4(x.x * f, x.y * f, x.z * f, x.w * f);
+  else *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.out) + e) = make_uint2(pack_bf16(x.x * f, x.y * f), pack_bf16(x.z * f, x.w * f));
+  if (a.lse && d == 0) a.lse[row_at(a, c, r, a.n_heads, 1)] = row_lse(m, l);
 }
 
-// How a warp's sums lie in shared memory, in float4. FRAG (bf16): the accumulators' own order: [dims / 64][rows / 8][4][lane], lane
-// (g, t) with dims 64 x + 8 g + 2 j, + 1 of rows 8 n + 2 t, + 1. Else (fp32): [row][dims / 4].
-template <bool FRAG, int DH, int ROWS>
+// A warp's sums lie in shared memory as [row][dim], rows DH + 4 floats apart (so that the accumulators of mma.sync go there
+// without bank conflicts). They are handled in groups of 32 float4: 128 dims of a row, or two rows of 64.
+template <int DH, int ROWS>
 struct Sums {
-  static constexpr int kItems = ROWS * DH / 4;
-  __device__ static int row(int i) { return FRAG ? (i / 128 % (ROWS / 8)) * 8 + 2 * (i & 3) : i / (DH / 4); }
-  __device__ static int dim(int i) { return FRAG ? i / 128 / (ROWS / 8) * 64 + (i >> 2 & 7) * 8 + (i >> 5 & 3) * 2 : i % (DH / 4) * 4; }
+  static constexpr int kGroups = ROWS * DH / 128, kPitch = DH + 4, kBytes = ROWS * kPitch * 4;
+  __device__ static int row(int gr, int lane) { return (gr * 32 + lane) / (DH / 4); }
+  __device__ static int dim(int gr, int lane) { return (gr * 32 + lane) % (DH / 4) * 4; }
 };
+// Shared memory of a CTA's end: the maxima and sums of its warps' rows, and what the cluster's CTAs send it: their
+// maxima and sums, and their sums of its share of the groups (which lie in the ring, behind the warps' sums, where they fit).
+template <int ROWS>
+struct EndShared {
+  float m[kWarps][ROWS], l[kWarps][ROWS];
+  float2 ml[ROWS], ml_of[kMaxCluster][ROWS];
+};
+template <int DH, int ROWS>
+constexpr int receive_bytes() { return (Sums<DH, ROWS>::kGroups + kMaxCluster - 1) * 512; }
+template <int DH, int ROWS>
+constexpr int receive_extra(int ring) { return kWarps * Sums<DH, ROWS>::kBytes + receive_bytes<DH, ROWS>() <= ring ? 0 : receive_bytes<DH, ROWS>(); }
 
-// The warps' rows become the CTA's, and those the cluster's or a piece. so [kWarps][items], sm, sl [kWarps][ROWS]: what the
-// warps found; ml [ROWS]. Called by all threads after a barrier. Where a CTA's warps have a head each, every warp ends alone.
-template <int T, bool FRAG, int DH, int ROWS>
-__device__ __forceinline__ void finish(const PagedAttnArgs& a, const Piece& c, float4* so, const float* sm, const float* sl, float2* ml) {
-  using S = Sums<FRAG, DH, ROWS>;
+// A CTA's four sets of sums, which its warps have scaled to the rows' common maxima e->ml[row].x, become the CTA's, and
+// those the cluster's or a piece. so [kWarps]: the sums; receive: where the cluster's share arrives. By all threads, after a
+// barrier; in a cluster, each of its CTAs has arrived at the cluster's barrier once its ring was free.
+template <int T, int DH, int ROWS>
+__device__ __forceinline__ void finish(const PagedAttnArgs& a, const Piece& c, const float* so, EndShared<ROWS>* e, float4* receive) {
+  using S = Sums<DH, ROWS>;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int from = a.warp_heads ? warp : 0, n = a.warp_heads ? 1 : kWarps;
-  constexpr int kJ = FRAG ? 4 : 1;   // items of a thread that go together: 8 dims of two rows, or 4 of one
-  constexpr int kR = FRAG ? 2 : 1;
-  for (int i = a.warp_heads ? lane : threadIdx.x; i < S::kItems / kJ; i += 32 * n) {
-    const int at = FRAG ? (i >> 5) * 128 + (i & 31) : i, r = S::row(at), d = S::dim(at);
-    float top[kR], sum[kR];
+  if (a.clustered) cluster_wait();   // every CTA's receiving place is free
+  const int share = a.clustered ? (S::kGroups + a.pieces - 1) / a.pieces : 0;
+#pragma unroll 2
+  for (int gr = warp; gr < S::kGroups; gr += kWarps) {
+    const int r = S::row(gr, lane), d = S::dim(gr, lane);
+    const float* at = so + r * S::kPitch + d;
+    float4 x = *reinterpret_cast<const float4*>(at);
 #pragma unroll
-    for (int e = 0; e < kR; ++e) {
-      top[e] = sm[from * ROWS + r + e];
-      for (int w = 1; w < n; ++w) top[e] = fmaxf(top[e], sm[(from + w) * ROWS + r + e]);
-      sum[e] = 0.f;
+    for (int w = 1; w < kWarps; ++w) {
+      const float4 y = *reinterpret_cast<const float4*>(at + w * (S::kBytes / 4));
+      x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
     }
-    float4 x[kJ];
-#pragma unroll
-    for (int j = 0; j < kJ; ++j) x[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int w = from; w < from + n; ++w) {
-      float f[kR];
-#pragma unroll
-      for (int e = 0; e < kR; ++e) {
-        f[e] = weight(sm[w * ROWS + r + e], top[e]);
-        sum[e] += sl[w * ROWS + r + e] * f[e];
-      }
-#pragma unroll
-      for (int j = 0; j < kJ; ++j) {
-        const float4 y = so[w * S::kItems + at + 32 * j];
-        x[j].x += y.x * f[0];
-        x[j].y += y.y * f[FRAG ? 1 : 0];
-        x[j].z += y.z * f[0];
-        x[j].w += y.w * f[FRAG ? 1 : 0];
-      }
-    }
-    if (a.clustered) {   // in place of the first warp's, which nobody else reads
-#pragma unroll
-      for (int j = 0; j < kJ; ++j) so[at + 32 * j] = x[j];
-      if (d == 0) {
-#pragma unroll
-        for (int e = 0; e < kR; ++e) ml[r + e] = make_float2(top[e], sum[e]);
-      }
-    } else if constexpr (FRAG) {
-      const float y0[8] = {x[0].x, x[0].z, x[1].x, x[1].z, x[2].x, x[2].z, x[3].x, x[3].z};
-      const float y1[8] = {x[0].y, x[0].w, x[1].y, x[1].w, x[2].y, x[2].w, x[3].y, x[3].w};
-      if (r < c.rows) put_row<T, 8>(a, c, r, d, y0, top[0], sum[0], a.pieces == 1);
-      if (r + 1 < c.rows) put_row<T, 8>(a, c, r + 1, d, y1, top[kR - 1], sum[kR - 1], a.pieces == 1);
-    } else {
-      const float y[4] = {x[0].x, x[0].y, x[0].z, x[0].w};
-      if (r < c.rows) put_row<T, 4>(a, c, r, d, y, top[0], sum[0], a.pieces == 1);
+    if (a.clustered) {   // group i goes to CTA i % pieces, [from][i / pieces]
+      put_peer(peer(su32(receive + (c.piece * share + gr / a.pieces) * 32 + lane), gr % a.pieces), x);
+    } else if (r < c.rows) {
+      const float2 ml = e->ml[r];
+      put_row<T>(a, c, r, d, x, ml.x, ml.y, a.pieces == 1);
     }
   }
   if (!a.clustered) return;
-  cluster_sync();
-  const uint32_t o = su32(so), s = su32(ml);
-  for (int i = c.piece * kThreads + threadIdx.x; i < S::kItems; i += a.pieces * kThreads) {   // a share of the items
-    const int r = S::row(i), d = S::dim(i);
-    if (r >= c.rows) continue;
-    float2 q[kMaxCluster][kR];
-    float4 y[kMaxCluster];
-#pragma unroll
-    for (int k = 0; k < kMaxCluster; ++k)
-      if (k < a.pieces) {
-        y[k] = peer_f4(peer(o + i * 16, k));
-#pragma unroll
-        for (int e = 0; e < kR; ++e) q[k][e] = peer_f2(peer(s + (r + e) * 8, k));
-      }
-    float top[kR], sum[kR];
-#pragma unroll
-    for (int e = 0; e < kR; ++e) {
-      top[e] = q[0][e].x;
-      sum[e] = 0.f;
-#pragma unroll
-      for (int k = 1; k < kMaxCluster; ++k)
-        if (k < a.pieces) top[e] = fmaxf(top[e], q[k][e].x);
-    }
+  for (int i = threadIdx.x; i < ROWS * a.pieces; i += kThreads) put_peer(peer(su32(&e->ml_of[c.piece][i % ROWS]), i / ROWS), e->ml[i % ROWS]);
+  cluster_arrive();
+  cluster_wait();   // everybody's share is here; nothing is sent after this
+  for (int i = warp; i < share; i += kWarps) {
+    const int gr = i * a.pieces + c.piece;
+    if (gr >= S::kGroups) break;
+    const int r = S::row(gr, lane), d = S::dim(gr, lane);
+    float top = -INFINITY, sum = 0.f;
+    for (int k = 0; k < a.pieces; ++k) top = fmaxf(top, e->ml_of[k][r].x);
     float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-    for (int k = 0; k < kMaxCluster; ++k)
-      if (k < a.pieces) {
-        float f[kR];
-#pragma unroll
-        for (int e = 0; e < kR; ++e) {
-          f[e] = weight(q[k][e].x, top[e]);
-          sum[e] += q[k][e].y * f[e];
-        }
-        x.x += y[k].x * f[0];
-        x.y += y[k].y * f[FRAG ? 1 : 0];
-        x.z += y[k].z * f[0];
-        x.w += y[k].w * f[FRAG ? 1 : 0];
-      }
-    if constexpr (FRAG) {
-      const float y0[2] = {x.x, x.z}, y1[2] = {x.y, x.w};
-      put_row<T, 2>(a, c, r, d, y0, top[0], sum[0], true);
-      if (r + 1 < c.rows) put_row<T, 2>(a, c, r + 1, d, y1, top[kR - 1], sum[kR - 1], true);
-    } else {
-      const float y0[4] = {x.x, x.y, x.z, x.w};
-      put_row<T, 4>(a, c, r, d, y0, top[0], sum[0], true);
+#pragma unroll 4
+    for (int k = 0; k < a.pieces; ++k) {
+      const float4 y = receive[(k * share + i) * 32 + lane];
+      const float2 q = e->ml_of[k][r];
+      const float f = weight(q.x, top);
+      sum += q.y * f;
+      x.x += y.x * f; x.y += y.y * f; x.z += y.z * f; x.w += y.w * f;
     }
+    if (r < c.rows) put_row<T>(a, c, r, d, x, top, sum, true);
   }
-  cluster_sync();   // nobody leaves while another CTA reads its shared memory
+}
+// The rows' common maxima and sums, by the first ROWS threads, after a barrier behind the writes of e->m and e->l.
+template <int ROWS>
+__device__ __forceinline__ float common_max(const EndShared<ROWS>* e, int r) {
+  return fmaxf(fmaxf(e->m[0][r], e->m[1][r]), fmaxf(e->m[2][r], e->m[3][r]));
+}
+template <int ROWS>
+__device__ __forceinline__ void common_rows(EndShared<ROWS>* e) {
+  const int r = threadIdx.x;
+  if (r >= ROWS) return;
+  const float top = common_max(e, r);
+  float sum = 0.f;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) sum += e->l[w][r] * weight(e->m[w][r], top);
+  e->ml[r] = make_float2(top, sum);
 }
 
 // ---- bf16 -------------------------------------------------------------------------------------------------------
 //
-// mma.sync m16n8k16: a warp takes 16 keys at a time by itself, with no barrier in the loop. Both products take their
-// contraction in an order that suits the loads, so that every thread needs exactly the 16-byte pieces that it
-// copies itself (cp.async, in a ring of its own in shared memory, lanes side by side: no bank conflict, no exchange):
-//   S = Q K^T, A = Q (16 rows), B = 8 keys: lane (g, t) has key g, dims 32 c + 8 t .. + 7, two k-steps' worth;
-//   O^T = V^T P^T, A = V^T (16 dims x 16 keys): lane (g, t) has keys 2t, 2t + 1, 2t + 8, 2t + 9, dims 64 c + 8 g .. + 7;
-//   a k pair is two keys' halves put together, and B = P^T is S's own register layout.
-// P goes in as two bf16 (the cut value and the rest): a second MMA where the pipe idles, for an error of 2^-16
-// and not 2^-9. The tensor cores' own form (tcgen05) would need 128 rows where there are 8 to 32.
-
-constexpr int kSlice = 16;
+// mma.sync m16n8k16: a warp takes a slice of 16 or 32 keys at a time by itself, with no barrier in the loop, out of a ring of
+// its own in shared memory that it fills with cp.async (rows 16 bytes further apart than they are long: ldmatrix reads eight of
+// them without a conflict). S = Q K^T has 16 query rows as A and 8 keys as B; O^T = V^T P^T has V^T as A (16 dims by 16 keys,
+// transposed by ldmatrix) and P^T as B, which is S's own register layout: 8 query rows are one tile there, so the few
+// rows of a decoding step waste nothing where most of the work is. P goes in as two bf16 (the cut value and the
+// rest): a second MMA where the pipe idles, for an error of 2^-16 and not 2^-9. The tensor cores' own form (tcgen05)
+// would need 128 rows where there are 8 to 32.
 
 __device__ __forceinline__ void mma16816(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void ldm4(uint32_t* r, uint32_t s) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(s) : "memory");
+}
+__device__ __forceinline__ void ldm4t(uint32_t* r, uint32_t s) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(s) : "memory");
+}
+__device__ __forceinline__ uint32_t lds2(uint32_t s) {
+  uint16_t v;
+  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(s) : "memory");
+  return v;
 }
 // Two bf16: ones in the halves that are infinite or NaN.
 __device__ __forceinline__ uint32_t nonfinite2(uint32_t w) {
   return ((w & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((w & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
 }
 
-template <int DH, int NR>   // K and V slices in turn, 32 DH bytes each
-constexpr int ring_slots() { return DH == 256 ? (NR == 1 ? 2 : 3) : DH == 128 ? 4 : 6; }
-template <int DH, int NR>   // a head's queries
-constexpr int tc_q_bytes() { return ((NR + 1) / 2) * (NR > 1 ? 2 : 1) * 16 * DH; }
+// Keys of a slice, in sixteens: two where registers and shared memory bear it, for more independent work in a warp.
 template <int DH, int NR>
-constexpr size_t tc_smem(int heads) { return (size_t)kWarps * ring_slots<DH, NR>() * 32 * DH + heads * tc_q_bytes<DH, NR>() + 8 * NR * (2 * kWarps * 4 + 8); }
+constexpr int slice_steps() { return DH == 256 || NR == 4 ? 1 : 2; }
+template <int DH, int NR>   // K and V slices in turn
+constexpr int ring_slots() { return DH == 256 ? 3 : DH == 128 ? (NR == 4 ? 4 : 2) : NR == 4 ? 6 : 2; }
+template <int DH>
+constexpr int row_pitch() { return 2 * DH + 16; }
 template <int DH, int NR>
-constexpr int tc_ctas() { return NR == 4 || (DH == 256 && NR == 2) ? 2 : DH == 64 && NR == 1 ? 4 : 3; }
+constexpr int tc_ring() { return kWarps * ring_slots<DH, NR>() * slice_steps<DH, NR>() * 16 * row_pitch<DH>(); }
+template <int DH, int NR>
+constexpr size_t tc_smem(int heads) { return (size_t)tc_ring<DH, NR>() + receive_extra<DH, 8 * NR>(tc_ring<DH, NR>()) + sizeof(EndShared<8 * NR>) + heads * 8 * NR * row_pitch<DH>(); }
+template <int DH, int NR>
+constexpr int tc_ctas() { return NR == 4 || DH == 256 ? 2 : DH == 64 && NR == 1 ? 4 : 3; }
 
 template <int DH, int NR>   // head dim; 8 NR query rows
 __global__ void __launch_bounds__(kThreads, tc_ctas<DH, NR>()) paged_attn_tc_kernel(const PagedAttnArgs a) {
-  constexpr int SLOTS = ring_slots<DH, NR>(), AHEAD = (SLOTS + 1) / 2, MT = (NR + 1) / 2, C = DH / 32, D = DH / 64, SLOT = 32 * DH;
-  constexpr int QH = NR > 1 ? 2 : 1, QB = tc_q_bytes<DH, NR>();
-  static_assert(SLOTS >= NR, "the warps' sums fit the ring");
+  constexpr int KT = slice_steps<DH, NR>(), KEYS = 16 * KT, SLOTS = ring_slots<DH, NR>(), AHEAD = (SLOTS + 1) / 2;
+  constexpr int MT = (NR + 1) / 2, PITCH = row_pitch<DH>(), SLOT = KEYS * PITCH, STEPS = DH / 16;
+  constexpr int RING = tc_ring<DH, NR>(), EXTRA = receive_extra<DH, 8 * NR>(RING);
+  using S = Sums<DH, 8 * NR>;
+  static_assert(kWarps * S::kBytes <= RING, "the warps' sums fit the ring");
+  static_assert(AHEAD * KEYS <= 64, "the bits of the keys ahead");
   extern __shared__ __align__(16) unsigned char smem[];
   const uint32_t base = su32(smem);
-  float* sm = reinterpret_cast<float*>(smem + kWarps * SLOTS * SLOT);   // [warp][row]
-  float* sl = sm + kWarps * 8 * NR;
-  float2* ml = reinterpret_cast<float2*>(sl + kWarps * 8 * NR);
+  EndShared<8 * NR>* end = reinterpret_cast<EndShared<8 * NR>*>(smem + RING + EXTRA);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const uint32_t sq = base + kWarps * SLOTS * SLOT + 8 * NR * (2 * kWarps * 4 + 8) + (a.warp_heads ? warp * QB : 0);
+  const uint32_t sq = base + RING + EXTRA + sizeof(EndShared<8 * NR>) + (a.warp_heads ? warp * 8 * NR * PITCH : 0);   // queries [row][dim]
   pdl_wait();
   pdl_trigger();
   Piece c;
-  Found found;
-  if (!find_piece(a, 8 * NR, kSlice, &c, &found) || no_keys(a, c)) return;
-  // the queries, in the order of the A operand
-  for (int i = a.warp_heads ? lane : threadIdx.x; i < MT * C * QH * 32; i += a.warp_heads ? 32 : kThreads) {
-    const int ln = i & 31, half = QH == 2 ? i >> 5 & 1 : 0, x = i / (32 * QH) % C, mt = i / (32 * QH * C), r = mt * 16 + half * 8 + (ln >> 2);
+  Found first[AHEAD + 1], found;
+  if (!find_piece<AHEAD + 1>(a, 8 * NR, KEYS, &c, first) || no_keys(a, c)) return;
+  for (int i = a.warp_heads ? lane : threadIdx.x; i < 8 * NR * (DH / 8); i += a.warp_heads ? 32 : kThreads) {
+    const int r = i / (DH / 8), x = i % (DH / 8);
     const bool ok = r < c.rows;
-    cp16_or_zero(sq + i * 16, static_cast<const __nv_bfloat16*>(a.q) + (ok ? row_at(a, c, r, a.q_stride, DH) + 32 * x + 8 * (ln & 3) : 0), ok);
+    cp16_or_zero(sq + r * PITCH + x * 16, static_cast<const __nv_bfloat16*>(a.q) + (ok ? row_at(a, c, r, a.q_stride, DH) + 8 * x : 0), ok);
   }
-  const uint32_t ring = base + warp * (SLOTS * SLOT) + lane * 16;
-  const __nv_bfloat16 *kp = static_cast<const __nv_bfloat16*>(a.p.k), *vp = static_cast<const __nv_bfloat16*>(a.p.v);
-  const int slices = (c.k1 - c.k0 + kSlice - 1) / kSlice, mine = (slices - c.kw + c.wk - 1) / c.wk;
-  const auto slice_key = [&](int i) { return c.k0 + (i * c.wk + c.kw) * kSlice; };
+  const uint32_t ring = base + warp * (SLOTS * SLOT);
+  const int slices = (c.k1 - c.k0 + KEYS - 1) / KEYS, mine = (slices - c.kw + c.wk - 1) / c.wk;
+  const auto slice_key = [&](int i) { return c.k0 + (i * c.wk + c.kw) * KEYS; };
 
-  uint64_t seen = 0;   // 16 bits a slice, the next one lowest
-  int64_t cur = -1;
+  // Copies: eight lanes 128 bytes of a key, four keys at a time. Lane l (and, of 16 keys, l + 16) has looked up key l; at: where
+  // this lane's keys are, for the keys and then the values.
+  uint64_t seen = 0;   // KEYS bits a slice, the next one lowest
+  int64_t at[KEYS / 4];
   int slot = 0;
-  const auto copy_k = [&](int i, int at) {   // lanes l and l + 16 have looked up key l
-    cur = i < mine ? key_at(a, c, found) : -1;
-    seen |= (uint64_t)(__ballot_sync(0xffffffffu, cur >= 0) & 0xffffu) << (16 * at);
+  const uint32_t to = ring + (lane >> 3) * PITCH + (lane & 7) * 16;
+  const auto copy = [&](int i, const void* pool) {
     if (i < mine) {
 #pragma unroll
-      for (int n = 0; n < 2; ++n) {
-        const int64_t e = __shfl_sync(0xffffffffu, cur, 8 * n + g);
-        const __nv_bfloat16* src = kp + (e < 0 ? 0 : e) + 8 * t;
+      for (int h = 0; h < KEYS / 4; ++h) {
+        const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(pool) + (at[h] < 0 ? 0 : at[h]) + 8 * (lane & 7);
 #pragma unroll
-        for (int x = 0; x < C; ++x) cp16_or_zero(ring + slot * SLOT + (n * C + x) * 512, src + 32 * x, e >= 0);
-      }
-    }
-    cp_commit();
-    slot = slot + 1 == SLOTS ? 0 : slot + 1;
-    if (i + 1 < mine) found = find_key(a, slice_key(i + 1) + (lane & 15));
-  };
-  const auto copy_v = [&](int i) {
-    if (i < mine) {
-#pragma unroll
-      for (int n = 0; n < 4; ++n) {
-        const int64_t e = __shfl_sync(0xffffffffu, cur, 2 * t + (n & 1) + 8 * (n >> 1));
-        const __nv_bfloat16* src = vp + (e < 0 ? 0 : e) + 8 * g;
-#pragma unroll
-        for (int x = 0; x < D; ++x) cp16_or_zero(ring + slot * SLOT + (n * D + x) * 512, src + 64 * x, e >= 0);
+        for (int x = 0; x < DH / 64; ++x) cp16_or_zero(to + slot * SLOT + 4 * h * PITCH + x * 128, src + 64 * x, at[h] >= 0);
       }
     }
     cp_commit();
     slot = slot + 1 == SLOTS ? 0 : slot + 1;
   };
+  const auto copy_k = [&](int i, int ahead, const Found& fnd) {
+    const int64_t e = i < mine ? key_at(a, c, fnd) : -1;
+    seen |= (uint64_t)(__ballot_sync(0xffffffffu, e >= 0) & (0xffffffffu >> (32 - KEYS))) << (KEYS * ahead);
+#pragma unroll
+    for (int h = 0; h < KEYS / 4; ++h) at[h] = __shfl_sync(0xffffffffu, e, 4 * h + (lane >> 3));
+    copy(i, a.p.k);
+  };
+  const auto next_k = [&](int i) {
+    copy_k(i, AHEAD - 1, found);
+    if (i + 1 < mine) found = find_key(a, slice_key(i + 1) + (lane & (KEYS - 1)));
+  };
+  const auto copy_v = [&](int i) { copy(i, a.p.v); };
 #pragma unroll
   for (int i = 0; i < SLOTS; ++i) {
     if (i & 1) copy_v(i / 2);
-    else copy_k(i / 2, i / 2);
+    else copy_k(i / 2, i / 2, first[i / 2]);
   }
-  float o[DH / 16][NR][4] = {}, m[2 * MT], l[2 * MT];
+  found = first[AHEAD];
+  float o[STEPS][NR][4] = {}, m[2 * MT], l[2 * MT];
 #pragma unroll
   for (int i = 0; i < 2 * MT; ++i) m[i] = -INFINITY, l[i] = 0.f;
   cp_wait<SLOTS - 1>();
   __syncthreads();   // the queries are there
+  // one tile of rows stays in registers
+  uint32_t q[NR == 1 ? STEPS : 1][4];
+  const uint32_t qa = sq + ((lane & 7) + (NR > 1 ? 8 * (lane >> 3 & 1) : 0)) * PITCH + (NR > 1 ? lane >> 4 : lane >> 3 & 1) * 16;
+  if constexpr (NR == 1) {
+#pragma unroll
+    for (int x = 0; x < STEPS; x += 2) {
+      uint32_t r[4];   // dims 16 x .. + 31 of rows 0..7
+      ldm4(r, sq + (lane & 7) * PITCH + (lane >> 3) * 16 + x * 32);
+      q[x][0] = r[0]; q[x][2] = r[1]; q[x + 1][0] = r[2]; q[x + 1][2] = r[3];
+      q[x][1] = q[x][3] = q[x + 1][1] = q[x + 1][3] = 0;
+    }
+  }
+  const uint32_t ka = ring + (lane & 7) * PITCH + (lane >> 3) * 16;                                    // 8 keys, 32 dims
+  const uint32_t va = ring + ((lane & 7) + 8 * (lane >> 4)) * PITCH + (lane >> 3 & 1) * 16;            // 16 keys, 16 dims
   int use = 0;       // slot of the slice at hand
   for (int i = 0; i < mine; ++i) {
     cp_wait<SLOTS - 1>();
-    float s[MT][2][4] = {};
+    __syncwarp();
+    float s[MT][2 * KT][4] = {};
 #pragma unroll
-    for (int x = 0; x < C; ++x) {
-      uint4 kk[2];
+    for (int x = 0; x < STEPS; x += 2) {
+      uint32_t kk[2 * KT][4];
 #pragma unroll
-      for (int n = 0; n < 2; ++n) kk[n] = lds16(ring + use * SLOT + (n * C + x) * 512);
+      for (int n = 0; n < 2 * KT; ++n) ldm4(kk[n], ka + use * SLOT + n * 8 * PITCH + x * 32);
 #pragma unroll
-      for (int mt = 0; mt < MT; ++mt) {
-        const uint4 q0 = lds16(sq + ((mt * C + x) * QH) * 512 + lane * 16);
-        const uint4 q1 = QH > 1 ? lds16(sq + ((mt * C + x) * QH + 1) * 512 + lane * 16) : make_uint4(0, 0, 0, 0);
-        const uint32_t a0[4] = {q0.x, q1.x, q0.y, q1.y}, a1[4] = {q0.z, q1.z, q0.w, q1.w};
+      for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-        for (int n = 0; n < 2; ++n) {
-          mma16816(s[mt][n], a0, kk[n].x, kk[n].y);
-          mma16816(s[mt][n], a1, kk[n].z, kk[n].w);
+        for (int y = 0; y < 2; ++y) {
+          uint32_t qq[4];
+          if constexpr (NR > 1) ldm4(qq, qa + mt * 16 * PITCH + (x + y) * 32);
+#pragma unroll
+          for (int n = 0; n < 2 * KT; ++n) mma16816(s[mt][n], NR > 1 ? qq : q[NR == 1 ? x + y : 0], kk[n][2 * y], kk[n][2 * y + 1]);
         }
-      }
     }
     use = use + 1 == SLOTS ? 0 : use + 1;
-    const uint32_t bits = (uint32_t)seen & 0xffffu;
-    seen >>= 16;
+    const uint32_t bits = (uint32_t)seen & (0xffffffffu >> (32 - KEYS));
+    seen >>= KEYS;
+    __syncwarp();   // read by all: the slot may be filled again
     if constexpr (SLOTS & 1) copy_v(i + AHEAD - 1);
-    else copy_k(i + AHEAD, AHEAD - 1);
+    else next_k(i + AHEAD);
 
     // scores, base 2; hidden keys
     const int key = slice_key(i);
-    const bool mixed = (a.causal && key + kSlice - 1 > c.first_pos) || (a.window > 0 && key <= c.last_pos - a.window);
+    const bool mixed = (a.causal && key + KEYS - 1 > c.first_pos) || (a.window > 0 && key <= c.last_pos - a.window);
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-      for (int n = 0; n < 2; ++n)
+      for (int n = 0; n < 2 * KT; ++n)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const float v = s[mt][n][e] * a.scale_log2;
           s[mt][n][e] = v < kLeast ? kLeast : v;
         }
-    if (mixed || bits != 0xffffu) {
+    if (mixed || bits != (0xffffffffu >> (32 - KEYS))) {
 #pragma unroll
-      for (int mt = 0; mt < MT; ++mt)
+      for (int j = 0; j < (NR > 1 ? 2 * MT : 1); ++j) {   // rows g + 8 j
+        int from = 0, end_key = c.k1;
+        if (mixed) {
+          const int pos = c.s.len - c.s.n + (int)a.by_group.div(c.r0 + 8 * j + g);
+          if (a.causal) end_key = pos + 1;
+          if (a.window > 0) from = pos - a.window + 1;
+        }
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
+        for (int n = 0; n < 2 * KT; ++n)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int k = 8 * n + 2 * t + (e & 1);
-            if (!(bits >> k & 1) || (mixed && !row_sees(a, c, mt * 16 + g + 8 * (e >> 1), key + k))) s[mt][n][e] = -INFINITY;
+          for (int e = 0; e < 2; ++e) {
+            const int k = 8 * n + 2 * t + e;
+            if (!(bits >> k & 1) || key + k < from || key + k >= end_key) s[j >> 1][n][2 * (j & 1) + e] = -INFINITY;
           }
+      }
     }
     // running maxima: kept until a score passes them by 2^8, which fp32 sums and bf16 weights bear
     float f[2 * MT];
     bool grew = false;
 #pragma unroll
     for (int j = 0; j < (NR > 1 ? 2 * MT : 1); ++j) {
-      float* v0 = s[j >> 1][0] + 2 * (j & 1);
-      float* v1 = s[j >> 1][1] + 2 * (j & 1);
-      float top = fmaxf(fmaxf(v0[0], v0[1]), fmaxf(v1[0], v1[1]));
+      float top = -INFINITY;
+#pragma unroll
+      for (int n = 0; n < 2 * KT; ++n) top = fmaxf(top, fmaxf(s[j >> 1][n][2 * (j & 1)], s[j >> 1][n][2 * (j & 1) + 1]));
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
       f[j] = 1.f;
@@ -474,18 +460,22 @@ __global__ void __launch_bounds__(kThreads, tc_ctas<DH, NR>()) paged_attn_tc_ker
         grew = true;
       }
       const float mm = m[j] == -INFINITY ? 0.f : m[j];
-      v0[0] = ex2_approx(v0[0] - mm);
-      v0[1] = ex2_approx(v0[1] - mm);
-      v1[0] = ex2_approx(v1[0] - mm);
-      v1[1] = ex2_approx(v1[1] - mm);
-      l[j] = l[j] * f[j] + ((v0[0] + v0[1]) + (v1[0] + v1[1]));
+      float sum = 0.f;
+#pragma unroll
+      for (int n = 0; n < 2 * KT; ++n) {
+        float* v = s[j >> 1][n] + 2 * (j & 1);
+        v[0] = ex2_approx(v[0] - mm);
+        v[1] = ex2_approx(v[1] - mm);
+        sum += v[0] + v[1];
+      }
+      l[j] = l[j] * f[j] + sum;
     }
     if (i > 0 && __any_sync(0xffffffffu, grew)) {
 #pragma unroll
       for (int n = 0; n < NR; ++n) {
         const float f0 = __shfl_sync(0xffffffffu, f[n], 8 * t), f1 = __shfl_sync(0xffffffffu, f[n], 8 * t + 4);
 #pragma unroll
-        for (int y = 0; y < DH / 16; ++y) {
+        for (int y = 0; y < STEPS; ++y) {
           o[y][n][0] *= f0;
           o[y][n][1] *= f1;
           o[y][n][2] *= f0;
@@ -495,11 +485,11 @@ __global__ void __launch_bounds__(kThreads, tc_ctas<DH, NR>()) paged_attn_tc_ker
     }
     // weights as two bf16: cut to the upper half, and the rest (above 0 wherever the weight is, so that a weight times an
     // infinite value is no NaN)
-    uint32_t hi[NR][2], lo[NR][2];
+    uint32_t hi[NR][2 * KT], lo[NR][2 * KT];
 #pragma unroll
     for (int n = 0; n < NR; ++n)
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
+      for (int k = 0; k < 2 * KT; ++k) {
         const float p0 = s[n >> 1][k][2 * (n & 1)], p1 = s[n >> 1][k][2 * (n & 1) + 1];
         const uint32_t u0 = __float_as_uint(p0), u1 = __float_as_uint(p1);
         hi[n][k] = __byte_perm(u0, u1, 0x7632);
@@ -508,100 +498,108 @@ __global__ void __launch_bounds__(kThreads, tc_ctas<DH, NR>()) paged_attn_tc_ker
       }
 
     cp_wait<SLOTS - 1>();
-    const uint32_t vs = ring + use * SLOT;
+    __syncwarp();
+    const uint32_t vs = va + use * SLOT;
     // Where rows see different keys, a value that one of them does not see must not reach it, not even as 0 times NaN:
     // infinite and NaN values of such a slice are left out here and added row by row below.
     bool odd = false;
     if (mixed) {
-#pragma unroll 1
-      for (int x = 0; x < 4 * D; ++x) {
-        const uint4 w = lds16(vs + x * 512);
-        odd |= (nonfinite2(w.x) | nonfinite2(w.y) | nonfinite2(w.z) | nonfinite2(w.w)) != 0;
+      const __nv_bfloat162 none = __floats2bfloat162_rn(0.f, 0.f);
+      __nv_bfloat162 any = none;
+#pragma unroll 4
+      for (int x = 0; x < STEPS * KT; ++x) {
+        uint32_t u[4];
+        ldm4t(u, vs + (x % KT) * 16 * PITCH + x / KT * 32);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) any = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&u[j]), none, any);   // 0 times it: 0 or NaN
       }
-      odd = __any_sync(0xffffffffu, odd);
+      odd = __any_sync(0xffffffffu, !(__low2float(any) == 0.f && __high2float(any) == 0.f));
     }
 #pragma unroll
-    for (int x = 0; x < D; ++x) {
-      uint32_t w[4][4];
+    for (int x = 0; x < STEPS; ++x)
 #pragma unroll
-      for (int n = 0; n < 4; ++n) {
-        const uint4 v = lds16(vs + (n * D + x) * 512);
-        w[n][0] = v.x; w[n][1] = v.y; w[n][2] = v.z; w[n][3] = v.w;
-      }
-      if (odd) {
+      for (int u = 0; u < KT; ++u) {
+        uint32_t v[4];
+        ldm4t(v, vs + u * 16 * PITCH + x * 32);
+        if (odd) {
 #pragma unroll
-        for (int n = 0; n < 4; ++n)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) w[n][j] &= ~nonfinite2(w[n][j]);
-      }
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint32_t v[4] = {__byte_perm(w[0][j], w[1][j], 0x5410), __byte_perm(w[0][j], w[1][j], 0x7632),
-                               __byte_perm(w[2][j], w[3][j], 0x5410), __byte_perm(w[2][j], w[3][j], 0x7632)};
+          for (int j = 0; j < 4; ++j) v[j] &= ~nonfinite2(v[j]);
+        }
 #pragma unroll
         for (int n = 0; n < NR; ++n) {
-          mma16816(o[4 * x + j][n], v, hi[n][0], hi[n][1]);
-          mma16816(o[4 * x + j][n], v, lo[n][0], lo[n][1]);
+          mma16816(o[x][n], v, hi[n][2 * u], hi[n][2 * u + 1]);
+          mma16816(o[x][n], v, lo[n][2 * u], lo[n][2 * u + 1]);
         }
       }
-    }
     if (odd) {
-      __syncwarp();   // every lane has waited for its copies: each may read the others'
+#pragma unroll
+      for (int h = 0; h < 2 * KT; ++h) {   // eight keys
 #pragma unroll 1
-      for (int k = 0; k < kSlice; ++k) {
-        const int tt = (k & 7) >> 1, kn = (k >> 3) * 2 + (k & 1);
+        for (int k = 0; k < 8; ++k) {
+          const uint32_t from = ring + use * SLOT + (8 * h + k) * PITCH + 2 * g;
 #pragma unroll
-        for (int n = 0; n < NR; ++n) {
-          const float* pr = s[n >> 1][0] + 2 * (n & 1);
-          const float* ps = s[n >> 1][1] + 2 * (n & 1);
-          const float p = k < 8 ? (k & 1 ? pr[1] : pr[0]) : (k & 1 ? ps[1] : ps[0]);
-          const float p0 = __shfl_sync(0xffffffffu, p, 8 * t + tt), p1 = __shfl_sync(0xffffffffu, p, 8 * t + 4 + tt);
+          for (int n = 0; n < NR; ++n) {
+            const float p = k & 1 ? s[n >> 1][h][2 * (n & 1) + 1] : s[n >> 1][h][2 * (n & 1)];
+            const float p0 = __shfl_sync(0xffffffffu, p, 8 * t + (k >> 1)), p1 = __shfl_sync(0xffffffffu, p, 8 * t + 4 + (k >> 1));
 #pragma unroll
-          for (int x = 0; x < D; ++x) {
-            const uint4 v = lds16(vs - lane * 16 + (g * 4 + tt) * 16 + (kn * D + x) * 512);
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+            for (int x = 0; x < STEPS; ++x)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const uint32_t bad = nonfinite2(w[j]);
-              const float v0 = __uint_as_float(w[j] << 16), v1 = __uint_as_float(w[j] & 0xffff0000u);
-              if (bad & 0xffffu) {
-                if (p0 != 0.f) o[4 * x + j][n][0] += p0 * v0;
-                if (p1 != 0.f) o[4 * x + j][n][1] += p1 * v0;
+              for (int y = 0; y < 2; ++y) {
+                const uint32_t w = lds2(from + x * 32 + y * 16);
+                if ((w & 0x7f80u) != 0x7f80u) continue;
+                const float val = __uint_as_float(w << 16);
+                if (p0 != 0.f) o[x][n][2 * y] += p0 * val;
+                if (p1 != 0.f) o[x][n][2 * y + 1] += p1 * val;
               }
-              if (bad >> 16) {
-                if (p0 != 0.f) o[4 * x + j][n][2] += p0 * v1;
-                if (p1 != 0.f) o[4 * x + j][n][3] += p1 * v1;
-              }
-            }
           }
         }
       }
-      __syncwarp();   // before anybody's slot is filled again
     }
     use = use + 1 == SLOTS ? 0 : use + 1;
-    if constexpr (SLOTS & 1) copy_k(i + AHEAD, AHEAD - 1);
+    __syncwarp();   // read by all: the slot may be filled again
+    if constexpr (SLOTS & 1) next_k(i + AHEAD);
     else copy_v(i + AHEAD);
   }
 
-  // the warps' sums, in the accumulators' order
   asm volatile("cp.async.wait_all;" ::: "memory");
-  __syncthreads();   // the ring becomes the sums' place, of any warp
-  float4* so = reinterpret_cast<float4*>(smem);
 #pragma unroll
   for (int j = 0; j < NR; ++j) {
     l[j] += __shfl_xor_sync(0xffffffffu, l[j], 1);
     l[j] += __shfl_xor_sync(0xffffffffu, l[j], 2);
-    if (t == 0) sm[warp * 8 * NR + 8 * j + g] = m[j], sl[warp * 8 * NR + 8 * j + g] = l[j];
   }
+  // the warps' sums, scaled to common maxima, to where the ring was
+  if (t == 0) {
 #pragma unroll
-  for (int x = 0; x < D; ++x)
-#pragma unroll
-    for (int n = 0; n < NR; ++n)
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        so[warp * (2 * NR * DH) + ((x * NR + n) * 4 + j) * 32 + lane] = make_float4(o[4 * x + j][n][0], o[4 * x + j][n][1], o[4 * x + j][n][2], o[4 * x + j][n][3]);
+    for (int j = 0; j < NR; ++j) end->m[warp][8 * j + g] = m[j], end->l[warp][8 * j + g] = l[j];
+  }
   __syncthreads();
-  finish<BF16, true, DH, 8 * NR>(a, c, so, sm, sl, ml);
+  if (a.clustered) cluster_arrive();   // the ring is free: others may send their shares
+  if (!a.warp_heads) common_rows(end);
+  float* so = reinterpret_cast<float*>(smem) + warp * (S::kBytes / 4);
+#pragma unroll
+  for (int n = 0; n < NR; ++n) {
+    const int r = 8 * n + 2 * t;
+    const float f0 = a.warp_heads ? 1.f : weight(end->m[warp][r], common_max(end, r));
+    const float f1 = a.warp_heads ? 1.f : weight(end->m[warp][r + 1], common_max(end, r + 1));
+    float* dst = so + r * S::kPitch + g;
+#pragma unroll
+    for (int x = 0; x < STEPS; ++x) {
+      dst[16 * x] = o[x][n][0] * f0;
+      dst[16 * x + S::kPitch] = o[x][n][1] * f1;
+      dst[16 * x + 8] = o[x][n][2] * f0;
+      dst[16 * x + 8 + S::kPitch] = o[x][n][3] * f1;
+    }
+  }
+  if (a.warp_heads) {   // the warp's rows are its own
+    __syncwarp();
+    for (int gr = 0; gr < S::kGroups; ++gr) {
+      const int r = S::row(gr, lane), d = S::dim(gr, lane);
+      if (r < c.rows) put_row<BF16>(a, c, r, d, *reinterpret_cast<const float4*>(so + r * S::kPitch + d), end->m[warp][r], end->l[warp][r], a.pieces == 1);
+    }
+    return;
+  }
+  __syncthreads();
+  finish<BF16, DH, 8 * NR>(a, c, reinterpret_cast<const float*>(smem), end, reinterpret_cast<float4*>(smem + (EXTRA ? RING : kWarps * S::kBytes)));
 }
 
 // ---- fp32 ---------------------------------------------------------------------------------------------------------
@@ -616,7 +614,9 @@ constexpr int f32_slice() { return DH == 256 ? 8 : 16; }
 template <int DH>
 constexpr int f32_slots() { return DH == 64 ? 4 : 3; }
 template <int DH>
-constexpr size_t f32_smem() { return (size_t)kWarps * f32_slots<DH>() * f32_slice<DH>() * DH * 4 + 8 * DH * 4 + kWarps * f32_slice<DH>() * 8 * 4 + 8 * (2 * kWarps * 4 + 8); }
+constexpr int f32_ring() { return kWarps * f32_slots<DH>() * f32_slice<DH>() * DH * 4; }
+template <int DH>
+constexpr size_t f32_smem() { return (size_t)f32_ring<DH>() + receive_extra<DH, 8>(f32_ring<DH>()) + sizeof(EndShared<8>) + 8 * DH * 4 + kWarps * f32_slice<DH>() * 8 * 4; }
 
 __device__ __forceinline__ void fma2(float2& d, float2 x, float2 y) {
   asm("{\n .reg .b64 a, b, c;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n mov.b64 c, {%0, %1};\n fma.rn.f32x2 c, a, b, c;\n mov.b64 {%0, %1}, c;\n}\n"
@@ -630,19 +630,17 @@ __device__ __forceinline__ float4 lds_f4(uint32_t s) {
 template <int DH>
 __global__ void __launch_bounds__(kThreads, 2) paged_attn_f32_kernel(const PagedAttnArgs a) {
   constexpr int KEYS = f32_slice<DH>(), SLOTS = f32_slots<DH>(), AHEAD = (SLOTS + 1) / 2, SLOT = KEYS * DH * 4, KJ = KEYS / 4, E = DH / 32;
-  static_assert(SLOTS * KEYS >= 8, "the warps' sums fit the ring");
   extern __shared__ __align__(16) unsigned char smem[];
-  const uint32_t base = su32(smem), sq = base + kWarps * SLOTS * SLOT;
+  constexpr int RING = f32_ring<DH>(), EXTRA = receive_extra<DH, 8>(RING), END = RING + EXTRA + (int)sizeof(EndShared<8>);
+  const uint32_t base = su32(smem), sq = base + END;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, kq = lane >> 3, dq = lane & 7;
-  float* sp = reinterpret_cast<float*>(smem + kWarps * SLOTS * SLOT + 8 * DH * 4) + warp * KEYS * 8;   // weights [key][row]
-  float* sm = reinterpret_cast<float*>(smem + kWarps * SLOTS * SLOT + 8 * DH * 4 + kWarps * KEYS * 8 * 4);
-  float* sl = sm + kWarps * 8;
-  float2* ml = reinterpret_cast<float2*>(sl + kWarps * 8);
+  float* sp = reinterpret_cast<float*>(smem + END + 8 * DH * 4) + warp * KEYS * 8;   // weights [key][row]
+  EndShared<8>* end = reinterpret_cast<EndShared<8>*>(smem + RING + EXTRA);
   pdl_wait();
   pdl_trigger();
   Piece c;
-  Found found;
-  if (!find_piece(a, 8, KEYS, &c, &found) || no_keys(a, c)) return;
+  Found first[AHEAD + 1], found;
+  if (!find_piece<AHEAD + 1>(a, 8, KEYS, &c, first) || no_keys(a, c)) return;
   for (int i = threadIdx.x; i < 8 * DH / 4; i += kThreads) {   // [row][dim]
     const int r = i / (DH / 4);
     const bool ok = r < c.rows;
@@ -666,18 +664,22 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attn_f32_kernel(const Paged
     cp_commit();
     slot = slot + 1 == SLOTS ? 0 : slot + 1;
   };
-  const auto copy_k = [&](int i, int at) {
-    cur = i < mine ? key_at(a, c, found) : -1;
+  const auto copy_k = [&](int i, int at, const Found& fnd) {
+    cur = i < mine ? key_at(a, c, fnd) : -1;
     seen |= (uint64_t)(__ballot_sync(0xffffffffu, cur >= 0) & ((1u << KEYS) - 1)) << (16 * at);
     copy(i, a.p.k);
+  };
+  const auto next_k = [&](int i) {
+    copy_k(i, AHEAD - 1, found);
     if (i + 1 < mine) found = find_key(a, slice_key(i + 1) + lane % KEYS);
   };
   const auto copy_v = [&](int i) { copy(i, a.p.v); };
 #pragma unroll
   for (int i = 0; i < SLOTS; ++i) {
     if (i & 1) copy_v(i / 2);
-    else copy_k(i / 2, i / 2);
+    else copy_k(i / 2, i / 2, first[i / 2]);
   }
+  found = first[AHEAD];
   float2 o[8][E / 2];
 #pragma unroll
   for (int r = 0; r < 8; ++r)
@@ -716,7 +718,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attn_f32_kernel(const Paged
     seen >>= 16;
     __syncwarp();   // read by all: the slot may be filled again
     if constexpr (SLOTS & 1) copy_v(i + AHEAD - 1);
-    else copy_k(i + AHEAD, AHEAD - 1);
+    else next_k(i + AHEAD);
 
     // the butterfly: of 8, 4, 2 rows a lane keeps half and gives the others to its partner
     float s[KJ];
@@ -795,28 +797,34 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attn_f32_kernel(const Paged
     }
     use = use + 1 == SLOTS ? 0 : use + 1;
     __syncwarp();   // read by all: the slot and the weights may be written again
-    if constexpr (SLOTS & 1) copy_k(i + AHEAD, AHEAD - 1);
+    if constexpr (SLOTS & 1) next_k(i + AHEAD);
     else copy_v(i + AHEAD);
   }
   asm volatile("cp.async.wait_all;" ::: "memory");
-  __syncthreads();
-  float4* so = reinterpret_cast<float4*>(smem);   // [warp][row][dim]
   l += __shfl_xor_sync(0xffffffffu, l, 8);
   l += __shfl_xor_sync(0xffffffffu, l, 16);
-  if (kq == 0) sm[warp * 8 + dq] = m, sl[warp * 8 + dq] = l;
+  if (kq == 0) end->m[warp][dq] = m, end->l[warp][dq] = l;
+  __syncthreads();
+  if (a.clustered) cluster_arrive();   // the ring is free: others may send their shares
+  common_rows(end);
+  const float scale = weight(m, common_max(end, dq));
+  using S = Sums<DH, 8>;
+  static_assert(kWarps * S::kBytes <= RING, "the warps' sums fit the ring");
+  float* so = reinterpret_cast<float*>(smem) + warp * (S::kBytes / 4);
 #pragma unroll
   for (int r = 0; r < 8; ++r) {
-    float* row = reinterpret_cast<float*>(so) + (size_t)(warp * 8 + r) * DH;
+    const float f = __shfl_sync(0xffffffffu, scale, r);
+    float* row = so + r * S::kPitch;
     if constexpr (E == 2) {
-      *reinterpret_cast<float2*>(row + 2 * lane) = o[r][0];
+      *reinterpret_cast<float2*>(row + 2 * lane) = make_float2(o[r][0].x * f, o[r][0].y * f);
     } else {
 #pragma unroll
       for (int x = 0; x < E / 4; ++x)
-        *reinterpret_cast<float4*>(row + 128 * x + 4 * lane) = make_float4(o[r][2 * x].x, o[r][2 * x].y, o[r][2 * x + 1].x, o[r][2 * x + 1].y);
+        *reinterpret_cast<float4*>(row + 128 * x + 4 * lane) = make_float4(o[r][2 * x].x * f, o[r][2 * x].y * f, o[r][2 * x + 1].x * f, o[r][2 * x + 1].y * f);
     }
   }
   __syncthreads();
-  finish<F32, false, DH, 8>(a, c, so, sm, sl, ml);
+  finish<F32, DH, 8>(a, c, reinterpret_cast<const float*>(smem), end, reinterpret_cast<float4*>(smem + (EXTRA ? RING : kWarps * S::kBytes)));
 }
 
 // ---- joining pieces ---------------------------------------------------------------------------------------------------
@@ -861,11 +869,12 @@ __global__ void __launch_bounds__(kThreads) paged_join_kernel(const PagedAttnArg
     x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
     sum += sl[i];
   }
-  x = make_float4(attn_value(x.x, top, sum), attn_value(x.y, top, sum), attn_value(x.z, top, sum), attn_value(x.w, top, sum));
+  const float f = row_factor(top, sum);
+  x = make_float4(x.x * f, x.y * f, x.z * f, x.w * f);
   const int64_t e = t * a.out_stride + (int64_t)h * DH + 4 * d;
   if constexpr (T == F32) *reinterpret_cast<float4*>(static_cast<float*>(a.out) + e) = x;
   else *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.out) + e) = make_uint2(pack_bf16(x.x, x.y), pack_bf16(x.z, x.w));
-  if (a.lse && d == 0) a.lse[t * a.n_heads + h] = attn_lse(top, sum);
+  if (a.lse && d == 0) a.lse[t * a.n_heads + h] = row_lse(top, sum);
 }
 
 // How many rows a CTA takes and how the keys are cut: into pieces of 64 keys (a slice a warp) and more, so many that the SMs
@@ -929,7 +938,10 @@ cudaError_t launch_attn(OncePerDevice& once, Kernel kernel, size_t smem, size_t 
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
-  e = (cudaError_t)once.run(dev, [&] { return (int)cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most); });
+  e = (cudaError_t)once.run(dev, [&] {
+    const cudaError_t f = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    return (int)(f != cudaSuccess ? f : cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most));
+  });
   if (e != cudaSuccess) return e;
   const dim3 grid((unsigned)a.row_blocks * a.pieces, a.warp_heads ? a.p.n_kv / kWarps : a.p.n_kv, a.p.n_seqs);
   return launch_cluster(kernel, grid, dim3(kThreads), smem, a.clustered ? a.pieces : 1, s, a);
