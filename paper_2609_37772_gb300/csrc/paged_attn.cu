@@ -877,32 +877,41 @@ __global__ void __launch_bounds__(kThreads) paged_join_kernel(const PagedAttnArg
   if (a.lse && d == 0) a.lse[t * a.n_heads + h] = row_lse(top, sum);
 }
 
-// How many rows a CTA takes and how the keys are cut: into pieces of 64 keys (a slice a warp) and more, so many that the SMs
-// are filled twice over and sequences of different lengths even out. From sizes alone: the workspace of a captured
-// call holds for what its graph replays.
-void attn_plan(const uad_kv_seqs* s, PagedAttnArgs* a) {
-  const int dh = a->p.dh, most = a->p.dtype == F32 ? 1 : dh == 256 ? 2 : 4;
-  const int64_t rows = (int64_t)a->p.max_new * a->group;
-  a->row_tiles = 1;
-  while (a->row_tiles < most && 8 * a->row_tiles < rows) a->row_tiles *= 2;
-  a->row_blocks = (int)((rows + 8 * a->row_tiles - 1) / (8 * a->row_tiles));
+// How many rows a CTA takes and how the keys are cut, from sizes alone (the workspace of a captured call holds for what its
+// graph replays). A CTA costs about 5 us before and after its keys, so there are no more of them than the SMs hold at once
+// (`slots`), and pieces are not shorter than 256 keys (fp32: 64) but where everything is one small wave. A cluster
+// joins its pieces in 1 us, the workspace and a second kernel take 3; but clusters are placed as a whole, which leaves
+// SMs idle once there are many of them or they are large. Long pieces are cut further, up to three waves, so that
+// sequences of different lengths even out. In us, pieces with / without a cluster:
+//   1 x 817 keys, 8 heads over 1 of 256:   13: 7.1 / 9.1,  7: 8.3 / 9.6
+//   64 x 282..1129, the same:               4: 16.3 / 18.4,  8: 23.3 / 17.1
+//   6 x 2001..8003, 5 new tokens:          12: 31.8 / 32.8,  16: 48.1 / 27.5
+//   2 x 32768, 131071, 32 over 8 of 128:   28: - / 130,  80: - / 117
+// With more heads than the SMs hold CTAs, a CTA's warps take a head each and need no joining (24 heads of 64: 51 x 5 keys 9.6 ->
+// 5.0, 64 x 60 keys 11.3 -> 7.6, 64 x 300 keys 26.5 -> 24.4; 2 x 6492 keys, fewer heads than that, 16.0 -> 27.9).
+void attn_plan(const uad_kv_seqs* s, int ctas_per_sm, PagedAttnArgs* a) {
   int64_t keys = s->max_len > 0 && s->max_len < a->p.capacity ? s->max_len : a->p.capacity;
   if (a->window > 0 && a->window + (int64_t)a->p.max_new - 1 < keys) keys = a->window + (int64_t)a->p.max_new - 1;
-  int64_t units = (int64_t)a->p.n_seqs * a->p.n_kv * a->row_blocks;
-  const int sms = 152;
-  a->warp_heads = a->p.dtype == BF16 && a->p.n_kv % kWarps == 0 && units >= 4 * sms;
-  if (a->warp_heads) units /= kWarps;
-  const int64_t target = sms * 6;
-  int64_t piece = (keys * units + target - 1) / target;
-  piece = (piece + 63) / 64 * 64;
-  if (piece < 64) piece = 64;
-  if ((keys + piece - 1) / piece > kMaxCluster && keys <= kMaxCluster * 512) piece = ((keys + kMaxCluster - 1) / kMaxCluster + 63) / 64 * 64;
+  if (keys < 1) keys = 1;
+  constexpr int sms = 152;
+  const int64_t units = (int64_t)a->p.n_seqs * a->p.n_kv * a->row_blocks, slots = sms * ctas_per_sm;
+  const int64_t least = a->p.dtype == F32 ? 64 : 256;
+  a->warp_heads = a->p.dtype == BF16 && a->p.n_kv % kWarps == 0 && units >= slots;
+  const auto most = [&](int64_t n) { return (keys + n - 1) / n; };   // pieces of at least n keys
+  int64_t n;
+  if (keys <= kMaxCluster * 256 && units * (most(64) < kMaxCluster ? most(64) : kMaxCluster) <= sms) {
+    n = most(64) < kMaxCluster ? most(64) : kMaxCluster;
+  } else {
+    n = units * 5 >= slots * 4 ? 1 : units * 2 > slots ? 2 : slots / units;
+    if (n > 1 && n <= 8 && units * n * 20 > slots * 17) n = slots * 17 / (units * 20) > 1 ? slots * 17 / (units * 20) : n;
+    if (n > most(least)) n = most(least);
+    if (keys / n >= 1024) n = 3 * n < most(1024) ? 3 * n : most(1024);
+  }
+  const int64_t piece = ((keys + n - 1) / n + 63) / 64 * 64;
   a->piece_keys = (int)(piece < (1ll << 30) ? piece : 1ll << 30);
   a->pieces = (int)((keys + a->piece_keys - 1) / a->piece_keys);
-  if (a->pieces < 1) a->pieces = 1;
-  a->clustered = a->pieces > 1 && a->pieces <= kMaxCluster && !a->warp_heads;
-  a->by_group = FastDiv((uint32_t)a->group);
-  a->by_x = FastDiv((uint32_t)(a->clustered ? a->pieces : a->row_blocks));
+  const int64_t ctas = units * a->pieces;
+  a->clustered = a->pieces > 1 && !a->warp_heads && ((a->pieces <= kMaxCluster && ctas <= sms) || (a->pieces <= 8 && ctas * 20 <= slots * 17));
 }
 // Bytes of the partial rows: maxima and sums, then values.
 int64_t attn_bytes(const PagedAttnArgs& a) {
@@ -927,7 +936,15 @@ int attn_args(const uad_kv_pages* pages, const uad_kv_seqs* seqs, const uad_attn
   a->scale = t->scale != 0.f ? t->scale : 1.f / sqrtf((float)a->p.dh);
   a->scale_log2 = a->scale * 1.4426950408889634f;
   a->n_heads = t->n_heads; a->group = t->n_heads / a->p.n_kv; a->causal = t->causal; a->window = t->window;
-  attn_plan(seqs, a);
+  // rows of a CTA: 8, 16 or 32, as many as there are, within what the registers hold
+  const int dh = a->p.dh, tiles = a->p.dtype == F32 ? 1 : dh == 256 ? 2 : 4;
+  const int64_t rows = (int64_t)a->p.max_new * a->group;
+  a->row_tiles = 1;
+  while (a->row_tiles < tiles && 8 * a->row_tiles < rows) a->row_tiles *= 2;
+  a->row_blocks = (int)((rows + 8 * a->row_tiles - 1) / (8 * a->row_tiles));
+  attn_plan(seqs, a->p.dtype == F32 || a->row_tiles == 4 || dh == 256 ? 2 : dh == 64 && a->row_tiles == 1 ? 4 : 3, a);
+  a->by_group = FastDiv((uint32_t)a->group);
+  a->by_x = FastDiv((uint32_t)(a->clustered ? a->pieces : a->row_blocks));
   return UAD_OK;
 }
 

@@ -249,6 +249,19 @@ def test_many_sequences():
     check_attention(c, q, out, lse)
 
 
+@pytest.mark.parametrize("heads,n,longest,new", [((24, 24, 64), 40, 90, 2), ((32, 8, 128), 60, 70, 1), ((16, 16, 256), 20, 80, 1),
+                                                 ((24, 24, 64), 26, 2300, 1), ((12, 4, 64), 152, 60, 17)],
+                         ids=lambda x: "x".join(map(str, x)) if isinstance(x, tuple) else str(x))
+def test_more_heads_than_ctas(heads, n, longest, new):
+    """Every warp of a CTA has a head of its own, with the pieces of long sequences too."""
+    lens = [max(new, 1 + (37 * i) % longest) for i in range(n)]
+    lens[1] = longest
+    c = Case(heads, 16, lens, [min(new, 1 + i % new) for i in range(n)], seed=n)
+    q, out, lse, status = run_attention(c)
+    assert status == 0
+    check_attention(c, q, out, lse)
+
+
 def test_offsets_past_32_bits():
     """Pages 2^30 elements apart: element offsets up to 3 * 2^30 + ..., bytes past 2^32."""
     buf = torch.zeros((3 << 30) + (1 << 21), dtype=torch.bfloat16, device="cuda")
