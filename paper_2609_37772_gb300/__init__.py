@@ -7,6 +7,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 import numpy as np
 
@@ -105,6 +106,15 @@ uad_paged_attention_workspace = _fn("uad_paged_attention_workspace", C.c_int64, 
 uad_paged_attention = _fn("uad_paged_attention", C.c_int, _PAGES, _SEQS, C.POINTER(uad_attn), _P, C.c_size_t, _P, _P)
 uad_linear_w4 = _fn("uad_linear_w4", C.c_int, _P, _P, _P, _P, _P, _P, _I32, _I32, _I32, _I32, _P)
 uad_quantize_w4 = _fn("uad_quantize_w4", C.c_int, _P, _I32, _I32, _I32, _P, _P, _P)
+# The same entries for the wrappers below, with structures as addresses or packed bytes: a decoding step makes several such
+# calls a layer, whose time on the host is longer than the kernels'.
+_append, _attention, _w4 = _lib["uad_kv_append"], _lib["uad_paged_attention"], _lib["uad_linear_w4"]
+_append.restype = _attention.restype = _w4.restype = C.c_int
+_append.argtypes = [_P] * 6
+_attention.argtypes = [_P] * 4 + [C.c_size_t, _P, _P]
+_w4.argtypes = uad_linear_w4.argtypes
+_pack_rows = struct.Struct("@3P3qPq4i").pack   # uad_kv_rows
+_pack_attn = struct.Struct("@4P3qf5i").pack    # uad_attn
 UAD_ETOOBIG = -7
 UAD_KV_BAD_PAGE, UAD_KV_BAD_SEQ = 1, 2
 UAD_W4_MAX_ROWS = 64
@@ -198,17 +208,23 @@ def plan_step(budgets, k, tr=True):
     return ns, f, tn, td
 
 
+_dtypes = {}   # torch's types by name, once a tensor has been seen: the binding itself does not import torch
+
+
 def _tensor(t, what, dtype, shape, device=None, rows=False):
-    """The address of a torch tensor that a kernel reads or writes: element type(s), shape (None: any size), contiguous
+    """The address of a torch tensor that a kernel reads or writes: element type, shape (None: any size), contiguous
     (rows: its rows alone, which may be apart) and on `device` (the GPU of the tensors beside it)."""
-    if str(t.dtype)[6:] not in dtype:
-        raise ValueError(f"{what}: expected {' or '.join(dtype)} elements, got {t.dtype}")
-    if t.dim() != len(shape) or any(a is not None and a != b for a, b in zip(shape, t.shape)):
+    if not _dtypes:
+        import torch
+        _dtypes.update({n: getattr(torch, n) for n in ("float32", "bfloat16", "int32", "uint8")})
+    if t.dtype is not _dtypes[dtype]:
+        raise ValueError(f"{what}: expected {dtype} elements, got {t.dtype}")
+    if t.shape != shape and (t.dim() != len(shape) or any(a is not None and a != b for a, b in zip(shape, t.shape))):
         raise ValueError(f"{what}: expected shape {list(shape)}, got {list(t.shape)}")
     if not t.is_contiguous() and not (rows and t.dim() == 2 and t.stride(1) == 1 and t.stride(0) >= t.shape[1]):
         raise ValueError(f"{what}: buffer must be contiguous" + (" along its rows" if rows else ""))
-    if t.device.type != "cuda" or (device is not None and t.device != device):
-        raise ValueError(f"{what}: must be on {'the GPU' if device is None else device}, is on {t.device}")
+    if t.get_device() < 0 or (device is not None and t.get_device() != device):
+        raise ValueError(f"{what}: must be on {'the GPU' if device is None else 'cuda:%d' % device}, is on {t.device}")
     return t.data_ptr()
 
 
@@ -232,14 +248,15 @@ class Sequences:
     def __init__(self, table, length, start=None, max_len=0, max_new=1):
         n = length.shape[0] if length.dim() else -1
         self.n = n
-        tp = _tensor(table, "table", ("int32",), (n, None), rows=True)
-        lp = _tensor(length, "length", ("int32",), (n,), table.device)
-        sp = None if start is None else _tensor(start, "start", ("int32",), (n + 1,), table.device)
+        tp = _tensor(table, "table", "int32", (n, None), rows=True)
+        self._gpu = table.get_device()
+        lp = _tensor(length, "length", "int32", (n,), self._gpu)
+        sp = None if start is None else _tensor(start, "start", "int32", (n + 1,), self._gpu)
         self.device = table.device
         self._keep = table, length, start
         self.seqs = uad_kv_seqs(table=tp, len=lp, start=sp, table_stride=table.stride(0) if n > 1 else max(1, table.shape[1]), n_seqs=n,
                                 table_width=table.shape[1], max_new=max_new, max_len=max_len)
-        self._ref = C.byref(self.seqs)
+        self._at = C.addressof(self.seqs)
 
 
 class PagedCache:
@@ -247,31 +264,47 @@ class PagedCache:
     bfloat16, the last dimension contiguous, the others in any order (a view of [pages][heads][slots][dim], or of keys and
     values in one tensor), both with the same strides. The tensors stay the caller's. Calls are asynchronous on `stream`
     (None: the legacy default stream); `status`: an int32 tensor of one element that device-side findings
-    (UAD_KV_BAD_PAGE, UAD_KV_BAD_SEQ) are added to."""
+    (UAD_KV_BAD_PAGE, UAD_KV_BAD_SEQ) are added to. On a stream of their own, the caller keeps the tensors until the work is done."""
 
     def __init__(self, k, v):
         if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.stride() != v.stride() or k.device != v.device:
             raise ValueError("pages: k and v must be [n_pages][page_size][n_kv_heads][head_dim] of one type, device and strides")
-        self.dtype = str(k.dtype)[6:]
-        if self.dtype not in ("float32", "bfloat16"):
+        name = str(k.dtype)[6:]
+        if name not in ("float32", "bfloat16"):
             raise ValueError(f"pages: expected float32 or bfloat16 elements, got {k.dtype}")
         if k.stride(3) != 1 or min(k.stride()) < 1:
             raise ValueError("pages: the last dimension must be contiguous")
         if k.device.type != "cuda":
             raise ValueError(f"pages: must be on the GPU, is on {k.device}")
-        self.k, self.v, self.device = k, v, k.device
-        self.n_kv_heads, self.head_dim = k.shape[2], k.shape[3]
+        self.k, self.v, self.device, self.dtype = k, v, k.device, k.dtype
+        self._gpu = k.get_device()
+        self.page_size, self.n_kv_heads, self.head_dim = k.shape[1], k.shape[2], k.shape[3]
         self.pages = uad_kv_pages(k=k.data_ptr(), v=v.data_ptr(), page_stride=k.stride(0), slot_stride=k.stride(1),
-                                  head_stride=k.stride(2), dtype=DTYPE["f32" if self.dtype == "float32" else "bf16"],
+                                  head_stride=k.stride(2), dtype=DTYPE["f32" if name == "float32" else "bf16"],
                                   n_pages=k.shape[0], page_size=k.shape[1], n_kv_heads=k.shape[2], head_dim=k.shape[3])
-        self._ref = C.byref(self.pages)
+        self._at = C.addressof(self.pages)
+
+    def _rows(self, t, what, dtype, n, width):
+        """Address and row stride of a [n][width] tensor of `dtype` whose rows may be apart."""
+        if t.dtype is dtype and t.get_device() == self._gpu and t.shape == (n, width):
+            ld, one = t.stride()
+            if one == 1 and ld >= width:
+                return t.data_ptr(), ld
+            if n == 1 and (one == 1 or width == 1):   # the stride of a single row says nothing
+                return t.data_ptr(), width
+        _tensor(t, what, str(dtype)[6:], (n, width), self._gpu, True)
+        return t.data_ptr(), width   # contiguous in spite of its strides: no rows
 
     def _status(self, status):
-        return None if status is None else _tensor(status, "status", ("int32",), (1,), self.device)
+        return None if status is None else _tensor(status, "status", "int32", (1,), self._gpu)
 
-    def _here(self, seqs):
-        if seqs.device != self.device:
-            raise ValueError(f"sequences: must be on {self.device}, are on {seqs.device}")
+    def _heads(self, t):
+        if t.dim() != 2:
+            raise ValueError(f"q: expected rows of heads, got shape {list(t.shape)}")
+        heads, rest = divmod(t.shape[1], self.head_dim)
+        if rest:
+            raise ValueError(f"q: expected a multiple of {self.head_dim} columns, got {t.shape[1]}")
+        return heads
 
     def _refused(self, rc, what):
         raise UADError(rc, f"{what}: the arguments break a rule of include/uad.h, or the pages are not on the current device"
@@ -281,37 +314,31 @@ class PagedCache:
         """Write the new tokens' keys and values [rows][n_kv_heads * head_dim] into their pages and their queries
         [rows][n_heads * head_dim] into q_out, keys and queries rotated by `rope` (None: not). float32 or bfloat16 rows,
         which may be parts of a fused projection; q_out in the cache's type."""
-        self._here(seqs)
         first = q if k is None else k
-        if first is None:
-            raise ValueError("append: neither keys nor queries")
-        kind, n = (str(first.dtype)[6:],), first.shape[0] if first.dim() else 0
-        if kind[0] not in ("float32", "bfloat16"):
-            raise ValueError(f"append: expected float32 or bfloat16 rows, got {first.dtype}")
-        r = uad_kv_rows(dtype=DTYPE["f32" if kind[0] == "float32" else "bf16"], n_rows=n)
-        width = self.n_kv_heads * self.head_dim
-        if (k is None) != (v is None) or (q is None) != (q_out is None):
-            raise ValueError("append: k goes with v, q with q_out")
+        if first is None or (k is None) != (v is None) or (q is None) != (q_out is None):
+            raise ValueError("append: k goes with v, q with q_out, and one of the two is needed")
+        if seqs._gpu != self._gpu:
+            raise ValueError(f"sequences: must be on {self.device}, are on {seqs.device}")
+        kind, n, width = first.dtype, first.shape[0] if first.dim() else 0, self.n_kv_heads * self.head_dim
+        code = 0 if (name := str(kind)) == "torch.float32" else 1
+        if code and name != "torch.bfloat16":
+            raise ValueError(f"append: expected float32 or bfloat16 rows, got {kind}")
+        kp = vp = qp = op = kl = vl = ql = ol = heads = 0
         if k is not None:
-            r.k, r.k_stride = _tensor(k, "k", kind, (n, width), self.device, True), k.stride(0)
-            r.v, r.v_stride = _tensor(v, "v", kind, (n, width), self.device, True), v.stride(0)
+            kp, kl = self._rows(k, "k", kind, n, width)
+            vp, vl = self._rows(v, "v", kind, n, width)
         if q is not None:
-            r.q, r.q_stride = _tensor(q, "q", kind, (n, None), self.device, True), q.stride(0)
-            r.q_out, r.q_out_stride = _tensor(q_out, "q_out", (self.dtype,), tuple(q.shape), self.device, True), q_out.stride(0)
-            r.n_heads, rest = divmod(q.shape[1], self.head_dim)
-            if rest:
-                raise ValueError(f"q: expected a multiple of {self.head_dim} columns, got {q.shape[1]}")
-        rc = uad_kv_append(self._ref, seqs._ref, C.byref(r), None if rope is None else C.byref(rope), self._status(status),
-                           _stream_handle(stream))
+            heads = self._heads(q)
+            qp, ql = self._rows(q, "q", kind, n, q.shape[1])
+            op, ol = self._rows(q_out, "q_out", self.dtype, n, q.shape[1])
+        rc = _append(self._at, seqs._at, _pack_rows(qp, kp, vp, ql, kl, vl, op, ol, code, heads, n, 0),
+                     None if rope is None else C.addressof(rope), self._status(status), _stream_handle(stream))
         if rc:
             self._refused(rc, "append")
 
-    def _attn(self, rows, n_heads, scale=None, causal=True, window=0):
-        return uad_attn(scale=scale or 0.0, n_heads=n_heads, n_rows=rows, causal=int(causal), window=window)
-
     def attention_workspace(self, seqs, rows, n_heads, window=0):
         """Bytes of the workspace that attention of these sizes needs (0 is possible)."""
-        n = uad_paged_attention_workspace(self._ref, seqs._ref, C.byref(self._attn(rows, n_heads, window=window)))
+        n = uad_paged_attention_workspace(self.pages, seqs.seqs, uad_attn(n_heads=n_heads, n_rows=rows, window=window))
         if n < 0:
             self._refused(n, "attention_workspace")
         return n
@@ -320,27 +347,26 @@ class PagedCache:
                   stream=None):
         """out = softmax(scale q k) v of the new tokens' queries [rows][n_heads * head_dim] over their sequences' pages
         (scale None: 1 / sqrt(head_dim)). causal: a token sees the keys up to its own; window > 0: no more than so many; key_mask
-        uint8 [sequences][>= longest length]: only where it is not 0. Where a token sees nothing, out is 0 and lse
+        uint8 [sequences][tokens that the table holds]: only where it is not 0. Where a token sees nothing, out is 0 and lse
         (float32 [rows][n_heads]) -inf. workspace: a uint8 tensor of attention_workspace bytes, not shared by calls that may
         run at the same time."""
-        self._here(seqs)
-        n = q.shape[0] if q.dim() else 0
-        qp = _tensor(q, "q", (self.dtype,), (n, None), self.device, True)
-        heads, rest = divmod(q.shape[1], self.head_dim)
-        if rest:
-            raise ValueError(f"q: expected a multiple of {self.head_dim} columns, got {q.shape[1]}")
-        a = self._attn(n, heads, scale, causal, window)
-        a.q, a.q_stride = qp, q.stride(0)
-        a.out, a.out_stride = _tensor(out, "out", (self.dtype,), tuple(q.shape), self.device, True), out.stride(0)
+        if seqs._gpu != self._gpu:
+            raise ValueError(f"sequences: must be on {self.device}, are on {seqs.device}")
+        heads, n = self._heads(q), q.shape[0]
+        qp, ql = self._rows(q, "q", self.dtype, n, q.shape[1])
+        op, ol = self._rows(out, "out", self.dtype, n, q.shape[1])
+        lp = mp = ml = wn = 0
+        wp = None
         if lse is not None:
-            a.lse = _tensor(lse, "lse", ("float32",), (n, heads), self.device)
+            lp = _tensor(lse, "lse", "float32", (n, heads), self._gpu)
         if key_mask is not None:
-            a.key_mask = _tensor(key_mask, "key_mask", ("uint8",), (seqs.n, None), self.device, True)
-            a.mask_stride = key_mask.stride(0)
-            if key_mask.shape[1] < seqs.seqs.table_width * self.pages.page_size:
-                raise ValueError(f"key_mask: expected {seqs.seqs.table_width * self.pages.page_size} columns, what the table holds")
-        wp, wn = (None, 0) if workspace is None else (_tensor(workspace, "workspace", ("uint8",), (None,), self.device), workspace.numel())
-        rc = uad_paged_attention(self._ref, seqs._ref, C.byref(a), wp, wn, self._status(status), _stream_handle(stream))
+            mp, ml = _tensor(key_mask, "key_mask", "uint8", (seqs.n, None), self._gpu, True), key_mask.stride(0)
+            if key_mask.shape[1] < seqs.seqs.table_width * self.page_size:
+                raise ValueError(f"key_mask: expected {seqs.seqs.table_width * self.page_size} columns, what the table holds")
+        if workspace is not None:
+            wp, wn = _tensor(workspace, "workspace", "uint8", (None,), self._gpu), workspace.numel()
+        rc = _attention(self._at, seqs._at, _pack_attn(qp, op, lp, mp, ql, ol, ml, scale or 0.0, heads, n, 1 if causal else 0, window, 0),
+                        wp, wn, self._status(status), _stream_handle(stream))
         if rc:
             self._refused(rc, "attention")
 
@@ -365,16 +391,16 @@ def linear_w4(x, q, scale, out, zero=None, bias=None, stream=None):
     128, M up to UAD_W4_MAX_ROWS. Asynchronous on `stream` (None: the legacy default stream)."""
     M, K = x.shape if x.dim() == 2 else (0, 0)
     N, groups = scale.shape if scale.dim() == 2 else (0, 0)
-    xp = _tensor(x, "x", ("bfloat16",), (M, K))
-    d = x.device
-    qp = _tensor(q, "q", ("uint8",), (N, K // 2), d)
-    sp = _tensor(scale, "scale", ("bfloat16",), (N, groups), d)
-    zp = None if zero is None else _tensor(zero, "zero", ("uint8",), (N, groups), d)
-    bp = None if bias is None else _tensor(bias, "bias", ("float32",), (N,), d)
-    op = _tensor(out, "out", ("float32",), (M, N), d)
+    xp = _tensor(x, "x", "bfloat16", (M, K))
+    d = x.get_device()
+    qp = _tensor(q, "q", "uint8", (N, K // 2), d)
+    sp = _tensor(scale, "scale", "bfloat16", (N, groups), d)
+    zp = None if zero is None else _tensor(zero, "zero", "uint8", (N, groups), d)
+    bp = None if bias is None else _tensor(bias, "bias", "float32", (N,), d)
+    op = _tensor(out, "out", "float32", (M, N), d)
     if groups < 1 or K % groups:
         raise ValueError(f"scale: {groups} groups do not divide {K} columns")
-    rc = uad_linear_w4(xp, qp, sp, zp, bp, op, M, N, K, K // groups, _stream_handle(stream))
+    rc = _w4(xp, qp, sp, zp, bp, op, M, N, K, K // groups, _stream_handle(stream))
     if rc:
         raise UADError(rc, "linear_w4: group must be 32, 64 or 128, x and q 16-byte aligned and on the current device, at most "
                        f"{UAD_W4_MAX_ROWS} rows")

@@ -881,7 +881,7 @@ __global__ void __launch_bounds__(kThreads) paged_join_kernel(const PagedAttnArg
 // graph replays). A CTA costs about 5 us before and after its keys, so there are no more of them than the SMs hold at once
 // (`slots`), and pieces are not shorter than 256 keys (fp32: 64) but where everything is one small wave. A cluster
 // joins its pieces in 1 us, the workspace and a second kernel take 3; but clusters are placed as a whole, which leaves
-// SMs idle once there are many of them or they are large. Long pieces are cut further, up to three waves, so that
+// SMs idle once there are many of them or they are large. Long pieces are cut further, up to four waves, so that
 // sequences of different lengths even out. In us, pieces with / without a cluster:
 //   1 x 817 keys, 8 heads over 1 of 256:   13: 7.1 / 9.1,  7: 8.3 / 9.6
 //   64 x 282..1129, the same:               4: 16.3 / 18.4,  8: 23.3 / 17.1
@@ -905,7 +905,8 @@ void attn_plan(const uad_kv_seqs* s, int ctas_per_sm, PagedAttnArgs* a) {
     n = units * 5 >= slots * 4 ? 1 : units * 2 > slots ? 2 : slots / units;
     if (n > 1 && n <= 8 && units * n * 20 > slots * 17) n = slots * 17 / (units * 20) > 1 ? slots * 17 / (units * 20) : n;
     if (n > most(least)) n = most(least);
-    if (keys / n >= 1024) n = 3 * n < most(1024) ? 3 * n : most(1024);
+    const int64_t waves = 4 * slots / units < most(1024) ? 4 * slots / units : most(1024);
+    if (waves > n) n = waves;
   }
   const int64_t piece = ((keys + n - 1) / n + 63) / 64 * 64;
   a->piece_keys = (int)(piece < (1ll << 30) ? piece : 1ll << 30);
