@@ -1,4 +1,6 @@
 // The projection of few tokens with 4-bit weights.
+#include <cuda_fp16.h>
+
 #include <cmath>
 #include <cstring>
 
@@ -44,6 +46,383 @@ __device__ __forceinline__ uint32_t lds4(uint32_t s) {
   asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(s) : "memory");
   return v;
 }
+
+// ---- up to 16 tokens: a stream of weights -------------------------------------------------------------------------------
+//
+// What bounds a few tokens, once the weights arrive at full bandwidth (14 cycles of an SM's quarter for 256 weights), is
+// taking the nibbles apart. As fp16 the bits of a nibble at the bottom of a half word are the subnormal q 2^-24, four bits
+// further up 16 q 2^-24, so four masks and a shift make operands of all eight of a word, with neither an exponent to set nor
+// an offset to subtract (bf16 takes 7 integer operations and 4 subtractions). The tokens are scaled to 2^14..2^15 by the power
+// of two of their group's largest value, which leaves a bf16's 8 bits whole down to 2^-30 of it in fp16, every second pair
+// divided by 16 as well. The products are exact and summed in fp32; a group's sum less zero times the tokens' own sum is then
+// scaled. That the zero is subtracted after the sum costs a bit: q is up to 15 where q - zero is up to 8.
+//
+// A tile of 16 rows is walked by wk of a CTA's warps, which take its chunks in turn and add up in shared memory: one, where
+// there are tiles enough for every warp, which saves the adding. A warp's copies run on from tile to tile. Where
+// there are fewer tiles than CTAs, or the tokens do not fit, a cluster shares K.
+//
+// In a chunk of 128 k, group j is words 4 GS j .. of a row's 16, of which lane t has GS neighbours, read at once (GS = G / 32 steps of an
+// MMA's 32 k): the order of k inside a group is free. Rows are so far apart in shared memory that this has no bank conflicts.
+constexpr int kFewSlots = 5;          // chunks of a warp in the ring, four of them on their way: 64 KB an SM
+constexpr int kFewX = 40 * 1024;      // bytes of tokens that a CTA should hold at most: two CTAs an SM
+constexpr int kSms = 152;
+template <int G>
+__host__ __device__ constexpr int few_pitch() { return G == 128 ? 64 : G == 64 ? 96 : 80; }
+struct FewArgs {
+  W4Args a;
+  int split;        // CTAs of a cluster that share K
+  int split_k;      // k of each, a multiple of kChunk
+  int vec;          // scales and zeros of a chunk are read as one word
+  int wk;           // warps of a tile: 1, 2, 4 or 8 (8 with a split)
+  int per_cta;      // tiles that a CTA takes at a time, at most kW4Warps / wk
+  FastDiv pieces;   // by the eights of k that a CTA holds
+};
+// A row's scales and zeros in a chunk, as the words they are loaded in.
+template <int N>
+struct Groups;
+template <>
+struct Groups<1> { uint16_t s; uint8_t z; };
+template <>
+struct Groups<2> { uint32_t s; uint16_t z; };
+template <>
+struct Groups<4> { uint64_t s; uint32_t z; };
+constexpr int kAhead = 3;             // chunks that scales and zeros are loaded ahead
+// Shared memory: 16 zeros; the warps' rings; their sums [2][warp][token][16]; the cluster's [2][rank][token][16]; the tokens'
+// factors and sums [group][token, an even number]; the tokens [step][token][t] of 16 bytes. k: a multiple of kChunk.
+template <int G>
+__host__ __device__ inline size_t few_smem(int rows, int k) {
+  return 16 + (size_t)kW4Warps * kFewSlots * 16 * few_pitch<G>() + (size_t)2 * kW4Warps * rows * 64 + (size_t)2 * 8 * rows * 64 +
+         (size_t)(k / G) * ((rows + 1) & ~1) * 8 + (size_t)rows * k * 2;
+}
+
+__device__ __forceinline__ void mma_f16(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_f16_first(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+}
+__device__ __forceinline__ uint32_t pack_f16(float x, float y) {
+  const __half2 h = __floats2half2_rn(x, y);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+template <int NT, int G>
+__global__ void __launch_bounds__(32 * kW4Warps, 2) w4_few_kernel(const FewArgs f) {
+  constexpr int PITCH = few_pitch<G>(), SLOT = 16 * PITCH, PG = kChunk / G, GS = G / 32;   // groups of a chunk, steps of a group
+  extern __shared__ __align__(16) unsigned char smem[];
+  pdl_wait();
+  pdl_trigger();
+  if (f.split > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");   // started: others may write here
+  const W4Args& a = f.a;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const int part = f.split > 1 ? blockIdx.x % f.split : 0, wk_bits = __ffs(f.wk) - 1, kw = warp & (f.wk - 1), of_cta = warp >> wk_bits;
+  const int cta = f.split > 1 ? blockIdx.x / f.split : blockIdx.x, ctas = f.split > 1 ? gridDim.x / f.split : gridDim.x;
+  const int tiles = (a.N + 15) / 16, groups = a.K / G, even = (a.M + 1) & ~1, stride = ctas * f.per_cta;
+  const int kb = part * f.split_k, ke = min(a.K, kb + f.split_k);
+  int tile = cta * f.per_cta + of_cta, rounds = (tiles - cta * f.per_cta + stride - 1) / stride;   // of the CTA
+  // this warp's chunks of a tile, and how many are left to copy and to find the scales of
+  const int chunks = (ke - kb + kChunk - 1) / kChunk, mine = chunks > kw ? (chunks - kw + f.wk - 1) >> wk_bits : 0;
+  const int own = of_cta < f.per_cta && tile < tiles && mine > 0 ? rounds - (tile + (rounds - 1) * stride >= tiles) : 0;   // rounds with work
+  const uint32_t ring = ptx::su32(smem) + 16 + warp * kFewSlots * SLOT;
+  float* red = reinterpret_cast<float*>(smem + 16 + kW4Warps * kFewSlots * SLOT);
+  float* recv = red + 2 * kW4Warps * a.M * 16;
+  float2* xg = reinterpret_cast<float2*>(recv + 2 * 8 * a.M * 16);             // x: 1 / scale, y: 2^-24 sum of the scaled values
+  unsigned char* xp = reinterpret_cast<unsigned char*>(xg + f.split_k / G * even);
+  const uint32_t xs = ptx::su32(xp);
+  if (threadIdx.x < 4) reinterpret_cast<uint32_t*>(smem)[threadIdx.x] = 0;
+
+  // Weights: 16 bytes a lane, 4 lanes a row's 64, rows g and g + 8 of the tile (past the last row: the last). What is past K is read
+  // from the row's start, and the tokens are 0 there.
+  int c_left = own * mine, c_tile = tile, c_i = 0, c_k = kb + kw * kChunk + 32 * t;
+  const uint8_t *r0 = nullptr, *r1 = nullptr;
+  const uint32_t to = ring + g * PITCH + 16 * t;
+  const auto copy = [&](int slot) {
+    if (c_left > 0) {
+      if (c_i == 0) {
+        r0 = a.q + ((int64_t)min(c_tile * 16 + g, a.N - 1) * a.K >> 1);
+        r1 = a.q + ((int64_t)min(c_tile * 16 + 8 + g, a.N - 1) * a.K >> 1);
+      }
+      const int at = (c_k < ke ? c_k : kb + 32 * t < ke ? kb + 32 * t : kb) >> 1;
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + slot * SLOT), "l"(r0 + at) : "memory");
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + slot * SLOT + 8 * PITCH), "l"(r1 + at) : "memory");
+      --c_left;
+      c_k += f.wk * kChunk;
+      if (++c_i == mine) c_i = 0, c_k = kb + kw * kChunk + 32 * t, c_tile += stride;
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+#pragma unroll
+  for (int i = 0; i < kFewSlots - 1; ++i) copy(i);
+  // scales and zeros
+  int g_left = own * mine, g_tile = tile, g_i = 0, g_at = (kb + kw * kChunk) / G;
+  const uint16_t *s0p = nullptr, *s1p = nullptr;
+  const uint8_t *z0p = nullptr, *z1p = nullptr;
+  Groups<PG> gs[kAhead + 1][2];
+  using ScaleWord = decltype(gs[0][0].s);
+  using ZeroWord = decltype(gs[0][0].z);
+  const auto load = [&](Groups<PG>* dst) {
+    if (g_left > 0) {
+      if (g_i == 0) {
+        const int64_t n0 = (int64_t)min(g_tile * 16 + g, a.N - 1) * groups, n1 = (int64_t)min(g_tile * 16 + 8 + g, a.N - 1) * groups;
+        s0p = reinterpret_cast<const uint16_t*>(a.scale) + n0; s1p = reinterpret_cast<const uint16_t*>(a.scale) + n1;
+        z0p = a.zero + n0; z1p = a.zero + n1;
+      }
+      dst[0].z = dst[1].z = (ZeroWord)0x08080808u;
+      if (f.vec) {
+        dst[0].s = *reinterpret_cast<const ScaleWord*>(s0p + g_at);
+        dst[1].s = *reinterpret_cast<const ScaleWord*>(s1p + g_at);
+        if (a.zero) {
+          dst[0].z = *reinterpret_cast<const ZeroWord*>(z0p + g_at);
+          dst[1].z = *reinterpret_cast<const ZeroWord*>(z1p + g_at);
+        }
+      } else {   // K % 128 != 0, or addresses that are no multiples of a chunk's groups
+        uint64_t sv[2] = {0, 0};
+        uint32_t zv[2] = {0, 0};
+#pragma unroll
+        for (int j = 0; j < PG; ++j)
+          if (g_at + j < groups) {
+            sv[0] |= (uint64_t)s0p[g_at + j] << (16 * j);
+            sv[1] |= (uint64_t)s1p[g_at + j] << (16 * j);
+            zv[0] |= (a.zero ? (uint32_t)z0p[g_at + j] : 8u) << (8 * j);
+            zv[1] |= (a.zero ? (uint32_t)z1p[g_at + j] : 8u) << (8 * j);
+          }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) dst[h].s = (ScaleWord)sv[h], dst[h].z = (ZeroWord)zv[h];
+      }
+      --g_left;
+      g_at += f.wk * PG;
+      if (++g_i == mine) g_i = 0, g_at = (kb + kw * kChunk) / G, g_tile += stride;
+    }
+  };
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i) load(gs[i]);
+  // Tokens: eight values a thread, a group's threads side by side; 0 past K.
+  const int work = a.M * (f.split_k / 8);
+  for (int i0 = 0; i0 < work; i0 += 4 * 32 * kW4Warps) {
+    uint4 vs[4];
+    int ms[4], ps[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int i = i0 + u * 32 * kW4Warps + threadIdx.x;
+      ms[u] = (int)f.pieces.div(i);
+      ps[u] = i - ms[u] * (int)f.pieces.d;
+      vs[u] = make_uint4(0, 0, 0, 0);
+      if (i < work && kb + 8 * ps[u] < ke) vs[u] = *reinterpret_cast<const uint4*>(a.x + (int64_t)ms[u] * a.K + kb + 8 * ps[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (i0 + u * 32 * kW4Warps >= work) break;
+      const int m = ms[u], p = ps[u];
+      const uint32_t w[4] = {vs[u].x, vs[u].y, vs[u].z, vs[u].w};
+      float x[8], top = 0.f, sum = 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        x[2 * j] = __uint_as_float(w[j] << 16);
+        x[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+        top = fmaxf(top, fmaxf(fabsf(x[2 * j]), fabsf(x[2 * j + 1])));
+      }
+#pragma unroll
+      for (int d = 1; d < G / 8; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+      const int e = min(max(__float_as_int(top) >> 23, 15), 254);
+      float scale = __int_as_float((268 - e) << 23), back = __int_as_float((e - 14) << 23);
+      if (top == INFINITY) {   // then only the infinite values count, as 1 and with an infinite factor
+        scale = 1.f;
+        back = INFINITY;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (x[j] == x[j]) x[j] = fabsf(x[j]) == INFINITY ? copysignf(1.f, x[j]) : 0.f;
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        x[j] *= scale;
+        sum += x[j];
+      }
+#pragma unroll
+      for (int d = 1; d < G / 8; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+      if (i0 + u * 32 * kW4Warps + (int)threadIdx.x < work) {
+        const int j = p / (4 * GS), tt = p / GS & 3, v = p & (GS - 1);   // group, lane and step of the group
+        if (p % (4 * GS) == 0) xg[j * even + m] = make_float2(back, sum * 5.9604644775390625e-08f);
+        *reinterpret_cast<uint4*>(xp + (((j * GS + v) * a.M + m) * 4 + tt) * 16) =
+            make_uint4(pack_f16(x[0], x[4]), pack_f16(x[1] * 0.0625f, x[5] * 0.0625f), pack_f16(x[2], x[6]), pack_f16(x[3] * 0.0625f, x[7] * 0.0625f));
+      }
+    }
+  }
+  __syncthreads();
+  if (f.split > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+
+  int slot = 0, buf = 0, i = 0;
+  float acc[NT][4] = {};
+  uint32_t x_at[NT], x_step[NT];   // a lane without a token reads zeros
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    const bool is = 8 * n + g < a.M;
+    x_step[n] = is ? a.M * 64 : 0;
+    x_at[n] = is ? xs + (32 * n + lane) * 16 + kw * 4 * x_step[n] : ptx::su32(smem);
+  }
+  // One chunk, with its scales, and those to be loaded. The loop below is unrolled over gs: moving a word that is on its way
+  // waits for it.
+  const auto chunk = [&](const Groups<PG>* now, Groups<PG>* later) {
+    load(later);
+    asm volatile("cp.async.wait_group %0;" ::"n"(kFewSlots - 2) : "memory");
+    __syncwarp();   // all lanes' copies are there, and what the next copy overwrites has been read
+    copy(slot == 0 ? kFewSlots - 1 : slot - 1);
+    const uint32_t ws = ring + slot * SLOT + g * PITCH + 4 * GS * t;
+    slot = slot + 1 == kFewSlots ? 0 : slot + 1;
+#pragma unroll
+    for (int j = 0; j < PG; ++j) {
+      uint32_t w[2][GS];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t at = ws + 8 * h * PITCH + 16 * GS * j;
+        if constexpr (GS == 4) asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[h][0]), "=r"(w[h][1]), "=r"(w[h][2]), "=r"(w[h][3]) : "r"(at) : "memory");
+        else if constexpr (GS == 2) asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(w[h][0]), "=r"(w[h][1]) : "r"(at) : "memory");
+        else w[h][0] = lds4(at);
+      }
+      float sum[NT][4];
+#pragma unroll
+      for (int v = 0; v < GS; ++v) {
+        const uint32_t w0 = w[0][v], w1 = w[1][v], v0 = w0 >> 8, v1 = w1 >> 8;
+        const uint32_t f0[4] = {w0 & 0x000f000fu, w1 & 0x000f000fu, w0 & 0x00f000f0u, w1 & 0x00f000f0u};
+        const uint32_t f1[4] = {v0 & 0x000f000fu, v1 & 0x000f000fu, v0 & 0x00f000f0u, v1 & 0x00f000f0u};
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          uint4 b;
+          asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(b.x), "=r"(b.y), "=r"(b.z), "=r"(b.w) : "r"(x_at[n] + (j * GS + v) * x_step[n]) : "memory");
+          if (v == 0) mma_f16_first(sum[n], f0, b.x, b.y);
+          else mma_f16(sum[n], f0, b.x, b.y);
+          mma_f16(sum[n], f1, b.z, b.w);
+        }
+      }
+      // (sum of q x - zero sum of x) 2^-24 of the scaled tokens, times 2^24 scale / their scale
+      const float z0 = (float)((uint32_t)now[0].z >> (8 * j) & 15u), z1 = (float)((uint32_t)now[1].z >> (8 * j) & 15u);
+      const float s0 = __uint_as_float((uint32_t)(now[0].s >> (16 * j)) << 16) * 16777216.f, s1 = __uint_as_float((uint32_t)(now[1].s >> (16 * j)) << 16) * 16777216.f;
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {   // tokens 2 t and 2 t + 1 (of those that are not there, anything)
+        const float4 x = *reinterpret_cast<const float4*>(xg + ((kw + i * f.wk) * PG + j) * even + min(8 * n + 2 * t, even - 2));
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          acc[n][c] = fmaf(fmaf(-(c < 2 ? z0 : z1), c & 1 ? x.w : x.y, sum[n][c]) * (c & 1 ? x.z : x.x), c < 2 ? s0 : s1, acc[n][c]);
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) x_at[n] += 4 * f.wk * x_step[n];
+  };
+  const auto end_tile = [&]() {
+    if (f.wk == 1) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int row = tile * 16 + 8 * h + g;
+        const float bias = a.bias && row < a.N ? a.bias[row] : 0.f;
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int m = 8 * n + 2 * t + e;
+            if (m < a.M && row < a.N) a.out[(int64_t)m * a.N + row] = acc[n][2 * h + e] + bias;
+          }
+      }
+    } else {
+      float* mine_red = red + (buf * kW4Warps + warp) * a.M * 16;
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int m = 8 * n + 2 * t + (e & 1);
+          if (m < a.M) mine_red[m * 16 + 8 * (e >> 1) + g] = acc[n][e];
+        }
+      __syncthreads();   // the buffer before this one is read by nobody any more
+      for (int j = threadIdx.x; j < a.M * 16 * f.per_cta; j += 32 * kW4Warps) {
+        const int c = f.per_cta > 1 ? j / (a.M * 16) : 0, r = j - c * (a.M * 16), n = (tile - of_cta + c) * 16 + (r & 15), m = r >> 4;
+        float v = 0.f;
+        for (int w = 0; w < f.wk; ++w) v += red[(buf * kW4Warps + c * f.wk + w) * a.M * 16 + r];
+        if (f.split > 1) {   // to the cluster's first CTA
+          uint32_t dst;
+          asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(dst) : "r"(ptx::su32(recv + (buf * 8 + part) * a.M * 16 + r)));
+          asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(dst), "f"(v) : "memory");
+        } else if (n < a.N) {
+          a.out[(int64_t)m * a.N + n] = v + (a.bias ? a.bias[n] : 0.f);
+        }
+      }
+      if (f.split > 1) {   // everybody's sums are there after the barrier; the next tile's go to the other buffer
+        asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
+        if (part == 0)
+          for (int j = threadIdx.x; j < a.M * 16; j += 32 * kW4Warps) {
+            const int n = tile * 16 + (j & 15), m = j >> 4;
+            float v = 0.f;
+            for (int c = 0; c < f.split; ++c) v += recv[(buf * 8 + c) * a.M * 16 + j];
+            if (n < a.N) a.out[(int64_t)m * a.N + n] = v + (a.bias ? a.bias[n] : 0.f);
+          }
+      }
+      buf ^= 1;
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[n][e] = 0.f;
+      x_at[n] -= 4 * f.wk * mine * x_step[n];
+    }
+    tile += stride;
+    i = 0;
+    --rounds;
+  };
+  int left = own * mine;
+  while (left > 0) {
+#pragma unroll
+    for (int u = 0; u <= kAhead; ++u)
+      if (left > 0) {
+        chunk(gs[u], gs[(u + kAhead) % (kAhead + 1)]);
+        --left;
+        if (++i == mine) end_tile();
+      }
+  }
+  if (f.wk > 1) {
+#pragma unroll
+    for (int n = 0; n < NT; ++n) x_step[n] = 0;
+    while (rounds > 0) end_tile();   // a warp without a tile in the last round, or without chunks, still meets the others
+  }
+}
+
+template <int NT, int RT, int G>
+cudaError_t launch_w4(const W4Args& a, int wn, cudaStream_t s);
+
+template <int NT, int G>
+cudaError_t launch_few(const W4Args& a, cudaStream_t s) {
+  static OncePerDevice once;
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  e = (cudaError_t)once.run(dev, [&] { return (int)cudaFuncSetAttribute(w4_few_kernel<NT, G>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024); });
+  if (e != cudaSuccess) return e;
+  FewArgs f{a, 1, 0, 0, 0, 0, FastDiv(1)};
+  const int tiles = (a.N + 15) / 16, chunks = (a.K + kChunk - 1) / kChunk;
+  while (f.split < 8 && (tiles * f.split * 2 <= 2 * kSms || (int64_t)a.M * 2 * ((chunks + f.split - 1) / f.split) * kChunk > kFewX) && chunks >= 2 * kW4Warps * f.split) f.split *= 2;
+  f.split_k = (chunks + f.split - 1) / f.split * kChunk;
+  f.pieces = FastDiv((uint32_t)(f.split_k / 8));
+  const size_t smem = few_smem<G>(a.M, f.split_k);
+  if (smem > 227 * 1024) return launch_w4<NT, 1, G>(a, 1, s);   // the tokens of a CTA do not fit: 16 of K past 30000
+  const int groups = a.K / G, pg = kChunk / G, ctas = (smem <= 113 * 1024 ? 2 : 1) * kSms;
+  f.vec = groups % pg == 0 && reinterpret_cast<uintptr_t>(a.scale) % (2 * pg) == 0 && reinterpret_cast<uintptr_t>(a.zero) % pg == 0;
+  // warps of a tile: the least of rounds times (chunks of a warp, and as much as a chunk for the adding)
+  f.wk = kW4Warps;
+  if (f.split == 1) {
+    int64_t best = INT64_MAX;
+    for (int wk = 1; wk <= kW4Warps; wk *= 2) {
+      const int64_t rounds = ((int64_t)tiles * wk + (int64_t)ctas * kW4Warps - 1) / ((int64_t)ctas * kW4Warps);
+      const int64_t cost = rounds * ((chunks + wk - 1) / wk + (wk > 1));
+      if (cost < best) best = cost, f.wk = wk;
+    }
+  }
+  const int64_t clusters = ctas / f.split, rounds = ((int64_t)tiles * f.wk + clusters * kW4Warps - 1) / (clusters * kW4Warps);
+  f.per_cta = (int)((tiles + clusters * rounds - 1) / (clusters * rounds));   // even rounds
+  const int64_t n = (tiles + f.per_cta - 1) / f.per_cta;
+  return launch_cluster(w4_few_kernel<NT, G>, dim3((unsigned)((n < clusters ? n : clusters) * f.split)), dim3(32 * kW4Warps), smem, f.split, s, f);
+}
+
+// ---- more tokens ------------------------------------------------------------------------------------------------------
 
 // Copies in flight a warp: about 10 KB.
 template <int RT>
@@ -215,8 +594,8 @@ template <int G>
 cudaError_t launch_group(const W4Args& a, cudaStream_t s) {
   const int tiles = (a.N + 15) / 16;   // of 16 rows
   const int tokens = (a.M + 7) / 8;
-  if (tokens == 1) return tiles >= 152 * 8 ? launch_w4<1, 2, G>(a, 2, s) : launch_w4<1, 1, G>(a, 1, s);
-  if (tokens == 2) return tiles >= 152 * 8 ? launch_w4<2, 2, G>(a, 2, s) : launch_w4<2, 1, G>(a, 1, s);
+  if (tokens == 1) return launch_few<1, G>(a, s);
+  if (tokens == 2) return launch_few<2, G>(a, s);
   if (tokens <= 4) return tiles >= 152 * 4 ? launch_w4<4, 2, G>(a, 2, s) : launch_w4<4, 1, G>(a, 1, s);
   if (tokens <= 6) return tiles >= 152 * 4 ? launch_w4<6, 2, G>(a, 2, s) : launch_w4<6, 1, G>(a, 1, s);
   return tiles >= 152 * 4 ? launch_w4<8, 2, G>(a, 2, s) : launch_w4<8, 1, G>(a, 1, s);
@@ -242,7 +621,7 @@ extern "C" {
 int uad_linear_w4(const void* x, const uint8_t* q, const uint16_t* scale, const uint8_t* zero, const float* bias, float* out,
                   int32_t M, int32_t N, int32_t K, int32_t group, void* stream) {
   if (!x || !q || !scale || !out || M < 1 || N < 1 || K < 1) return UAD_EINVAL;
-  if ((group != 32 && group != 64 && group != 128) || K % group || (int64_t)N * K >= (1ll << 40)) return UAD_EINVAL;
+  if ((group != 32 && group != 64 && group != 128) || K % group || (int64_t)N * K > (1ll << 35)) return UAD_EINVAL;
   if (reinterpret_cast<uintptr_t>(x) % 16 || reinterpret_cast<uintptr_t>(q) % 16 || reinterpret_cast<uintptr_t>(scale) % 2 ||
       reinterpret_cast<uintptr_t>(bias) % 4 || reinterpret_cast<uintptr_t>(out) % 4)
     return UAD_EINVAL;

@@ -39,7 +39,8 @@ def check(out, want, size, K, group, bias):
 
 SHAPES = [(1, 1, 32, 32), (1, 16, 64, 64), (1, 17, 128, 128), (1, 2560, 1024, 64), (1, 100, 4096, 128), (2, 33, 96, 32), (3, 1000, 256, 128),
           (5, 2048, 8192, 32), (7, 15, 384, 128), (8, 64, 2048, 64), (9, 640, 160, 32), (16, 129, 512, 64), (17, 77, 704, 64), (24, 4608, 1536, 128),
-          (31, 31, 992, 32), (32, 256, 1024, 128), (33, 513, 320, 64), (40, 1409, 4096, 64), (63, 48, 640, 128), (64, 1024, 2048, 32), (64, 7, 12288, 128)]
+          (31, 31, 992, 32), (32, 256, 1024, 128), (33, 513, 320, 64), (40, 1409, 4096, 64), (63, 48, 640, 128), (64, 1024, 2048, 32), (64, 7, 12288, 128),
+          (16, 40, 36864, 128), (9, 24, 8320, 64), (16, 300, 4224, 32), (4, 16, 16384, 128), (13, 5000, 2304, 64), (1, 9, 2176, 32), (2, 20000, 512, 64)]
 
 
 @pytest.mark.parametrize("M,N,K,group", SHAPES)
