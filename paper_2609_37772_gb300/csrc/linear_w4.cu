@@ -72,7 +72,6 @@ struct FewArgs {
   W4Args a;
   int split;        // CTAs of a cluster that share K
   int split_k;      // k of each, a multiple of kChunk
-  int vec;          // scales and zeros of a chunk are read as one word
   int wk;           // warps of a tile: 1, 2, 4 or 8 (8 with a split)
   int per_cta;      // tiles that a CTA takes at a time, at most kW4Warps / wk
   FastDiv pieces;   // by the eights of k that a CTA holds
@@ -110,7 +109,7 @@ __device__ __forceinline__ uint32_t pack_f16(float x, float y) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-template <int NT, int G>
+template <int NT, int G, bool VEC>   // VEC: a chunk's scales, and its zeros, are read as one word
 __global__ void __launch_bounds__(32 * kW4Warps, 2) w4_few_kernel(const FewArgs f) {
   constexpr int PITCH = few_pitch<G>(), SLOT = 16 * PITCH, PG = kChunk / G, GS = G / 32;   // groups of a chunk, steps of a group
   extern __shared__ __align__(16) unsigned char smem[];
@@ -164,6 +163,8 @@ __global__ void __launch_bounds__(32 * kW4Warps, 2) w4_few_kernel(const FewArgs 
   Groups<PG> gs[kAhead + 1][2];
   using ScaleWord = decltype(gs[0][0].s);
   using ZeroWord = decltype(gs[0][0].z);
+  uint16_t raw_s[2][PG];   // where they are not one word (K % 128 != 0, other addresses): as they come, put together a chunk later
+  uint8_t raw_z[2][PG];
   const auto load = [&](Groups<PG>* dst) {
     if (g_left > 0) {
       if (g_i == 0) {
@@ -171,35 +172,47 @@ __global__ void __launch_bounds__(32 * kW4Warps, 2) w4_few_kernel(const FewArgs 
         s0p = reinterpret_cast<const uint16_t*>(a.scale) + n0; s1p = reinterpret_cast<const uint16_t*>(a.scale) + n1;
         z0p = a.zero + n0; z1p = a.zero + n1;
       }
-      dst[0].z = dst[1].z = (ZeroWord)0x08080808u;
-      if (f.vec) {
+      if constexpr (VEC) {
+        dst[0].z = dst[1].z = (ZeroWord)0x08080808u;
         dst[0].s = *reinterpret_cast<const ScaleWord*>(s0p + g_at);
         dst[1].s = *reinterpret_cast<const ScaleWord*>(s1p + g_at);
         if (a.zero) {
           dst[0].z = *reinterpret_cast<const ZeroWord*>(z0p + g_at);
           dst[1].z = *reinterpret_cast<const ZeroWord*>(z1p + g_at);
         }
-      } else {   // K % 128 != 0, or addresses that are no multiples of a chunk's groups
-        uint64_t sv[2] = {0, 0};
-        uint32_t zv[2] = {0, 0};
+      } else {
 #pragma unroll
-        for (int j = 0; j < PG; ++j)
-          if (g_at + j < groups) {
-            sv[0] |= (uint64_t)s0p[g_at + j] << (16 * j);
-            sv[1] |= (uint64_t)s1p[g_at + j] << (16 * j);
-            zv[0] |= (a.zero ? (uint32_t)z0p[g_at + j] : 8u) << (8 * j);
-            zv[1] |= (a.zero ? (uint32_t)z1p[g_at + j] : 8u) << (8 * j);
-          }
-#pragma unroll
-        for (int h = 0; h < 2; ++h) dst[h].s = (ScaleWord)sv[h], dst[h].z = (ZeroWord)zv[h];
+        for (int j = 0; j < PG; ++j) {   // past K: any group of the row, the tokens are 0 there
+          const int at = min(g_at + j, groups - 1);
+          raw_s[0][j] = s0p[at];
+          raw_s[1][j] = s1p[at];
+          raw_z[0][j] = raw_z[1][j] = 8;
+          if (a.zero) raw_z[0][j] = z0p[at], raw_z[1][j] = z1p[at];
+        }
       }
       --g_left;
       g_at += f.wk * PG;
       if (++g_i == mine) g_i = 0, g_at = (kb + kw * kChunk) / G, g_tile += stride;
     }
   };
+  const auto put = [&](Groups<PG>* dst) {
+    if constexpr (!VEC) {
 #pragma unroll
-  for (int i = 0; i < kAhead; ++i) load(gs[i]);
+      for (int h = 0; h < 2; ++h) {
+        uint64_t sv = 0;
+        uint32_t zv = 0;
+#pragma unroll
+        for (int j = 0; j < PG; ++j) sv |= (uint64_t)raw_s[h][j] << (16 * j), zv |= (uint32_t)raw_z[h][j] << (8 * j);
+        dst[h].s = (ScaleWord)sv;
+        dst[h].z = (ZeroWord)zv;
+      }
+    }
+  };
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i) {
+    load(gs[i]);
+    if (i + 1 < kAhead) put(gs[i]);
+  }
   // Tokens: eight values a thread, a group's threads side by side; 0 past K.
   const int work = a.M * (f.split_k / 8);
   for (int i0 = 0; i0 < work; i0 += 4 * 32 * kW4Warps) {
@@ -265,7 +278,8 @@ __global__ void __launch_bounds__(32 * kW4Warps, 2) w4_few_kernel(const FewArgs 
   }
   // One chunk, with its scales, and those to be loaded. The loop below is unrolled over gs: moving a word that is on its way
   // waits for it.
-  const auto chunk = [&](const Groups<PG>* now, Groups<PG>* later) {
+  const auto chunk = [&](const Groups<PG>* now, Groups<PG>* before, Groups<PG>* later) {
+    put(before);
     load(later);
     asm volatile("cp.async.wait_group %0;" ::"n"(kFewSlots - 2) : "memory");
     __syncwarp();   // all lanes' copies are there, and what the next copy overwrites has been read
@@ -374,7 +388,7 @@ __global__ void __launch_bounds__(32 * kW4Warps, 2) w4_few_kernel(const FewArgs 
 #pragma unroll
     for (int u = 0; u <= kAhead; ++u)
       if (left > 0) {
-        chunk(gs[u], gs[(u + kAhead) % (kAhead + 1)]);
+        chunk(gs[u], gs[(u + kAhead - 1) % (kAhead + 1)], gs[(u + kAhead) % (kAhead + 1)]);
         --left;
         if (++i == mine) end_tile();
       }
@@ -389,23 +403,22 @@ __global__ void __launch_bounds__(32 * kW4Warps, 2) w4_few_kernel(const FewArgs 
 template <int NT, int RT, int G>
 cudaError_t launch_w4(const W4Args& a, int wn, cudaStream_t s);
 
-template <int NT, int G>
+template <int NT, int G, bool VEC>
 cudaError_t launch_few(const W4Args& a, cudaStream_t s) {
   static OncePerDevice once;
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
-  e = (cudaError_t)once.run(dev, [&] { return (int)cudaFuncSetAttribute(w4_few_kernel<NT, G>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024); });
+  e = (cudaError_t)once.run(dev, [&] { return (int)cudaFuncSetAttribute(w4_few_kernel<NT, G, VEC>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024); });
   if (e != cudaSuccess) return e;
-  FewArgs f{a, 1, 0, 0, 0, 0, FastDiv(1)};
+  FewArgs f{a, 1, 0, 0, 0, FastDiv(1)};
   const int tiles = (a.N + 15) / 16, chunks = (a.K + kChunk - 1) / kChunk;
   while (f.split < 8 && (tiles * f.split * 2 <= 2 * kSms || (int64_t)a.M * 2 * ((chunks + f.split - 1) / f.split) * kChunk > kFewX) && chunks >= 2 * kW4Warps * f.split) f.split *= 2;
   f.split_k = (chunks + f.split - 1) / f.split * kChunk;
   f.pieces = FastDiv((uint32_t)(f.split_k / 8));
   const size_t smem = few_smem<G>(a.M, f.split_k);
   if (smem > 227 * 1024) return launch_w4<NT, 1, G>(a, 1, s);   // the tokens of a CTA do not fit: 16 of K past 30000
-  const int groups = a.K / G, pg = kChunk / G, ctas = (smem <= 113 * 1024 ? 2 : 1) * kSms;
-  f.vec = groups % pg == 0 && reinterpret_cast<uintptr_t>(a.scale) % (2 * pg) == 0 && reinterpret_cast<uintptr_t>(a.zero) % pg == 0;
+  const int ctas = (smem <= 113 * 1024 ? 2 : 1) * kSms;
   // warps of a tile: the least of rounds times (chunks of a warp, and as much as a chunk for the adding)
   f.wk = kW4Warps;
   if (f.split == 1) {
@@ -419,7 +432,7 @@ cudaError_t launch_few(const W4Args& a, cudaStream_t s) {
   const int64_t clusters = ctas / f.split, rounds = ((int64_t)tiles * f.wk + clusters * kW4Warps - 1) / (clusters * kW4Warps);
   f.per_cta = (int)((tiles + clusters * rounds - 1) / (clusters * rounds));   // even rounds
   const int64_t n = (tiles + f.per_cta - 1) / f.per_cta;
-  return launch_cluster(w4_few_kernel<NT, G>, dim3((unsigned)((n < clusters ? n : clusters) * f.split)), dim3(32 * kW4Warps), smem, f.split, s, f);
+  return launch_cluster(w4_few_kernel<NT, G, VEC>, dim3((unsigned)((n < clusters ? n : clusters) * f.split)), dim3(32 * kW4Warps), smem, f.split, s, f);
 }
 
 // ---- more tokens ------------------------------------------------------------------------------------------------------
@@ -594,8 +607,12 @@ template <int G>
 cudaError_t launch_group(const W4Args& a, cudaStream_t s) {
   const int tiles = (a.N + 15) / 16;   // of 16 rows
   const int tokens = (a.M + 7) / 8;
-  if (tokens == 1) return launch_few<1, G>(a, s);
-  if (tokens == 2) return launch_few<2, G>(a, s);
+  if (tokens <= 2) {
+    constexpr int PG = kChunk / G;   // groups of a chunk
+    if (PG == 1 || (a.K % kChunk == 0 && reinterpret_cast<uintptr_t>(a.scale) % (2 * PG) == 0 && reinterpret_cast<uintptr_t>(a.zero) % PG == 0))
+      return tokens == 1 ? launch_few<1, G, true>(a, s) : launch_few<2, G, true>(a, s);
+    if constexpr (PG > 1) return tokens == 1 ? launch_few<1, G, false>(a, s) : launch_few<2, G, false>(a, s);
+  }
   if (tokens <= 4) return tiles >= 152 * 4 ? launch_w4<4, 2, G>(a, 2, s) : launch_w4<4, 1, G>(a, 1, s);
   if (tokens <= 6) return tiles >= 152 * 4 ? launch_w4<6, 2, G>(a, 2, s) : launch_w4<6, 1, G>(a, 1, s);
   return tiles >= 152 * 4 ? launch_w4<8, 2, G>(a, 2, s) : launch_w4<8, 1, G>(a, 1, s);
