@@ -24,23 +24,8 @@ struct W4Args {
   int M, N, K, group;
 };
 
-// mma.sync m16n8k16 with 16 weight rows as A and 8 tokens as B. A warp walks its rows in chunks of 128 k (64 bytes a row),
-// which it copies ahead into a ring of its own (cp.async; rows 80 bytes apart, so that eight rows' words lie in different
-// banks). Step i of a chunk is k = 32 i .. 32 i + 31, of which lane (g, t) has the word of k = 32 i + 8 t .. + 7 of rows g and g + 8:
-// the contraction's order is free, so a pair is (k, k + 4), whose bits one mask takes out of the word, and a step lies in
-// one group. 0x4300 | q is the bf16 128 + q; minus 128 + zero leaves q - zero, exactly. Tokens are read as they lie, 16 bytes
-// a lane, and put in the same order.
-constexpr int kChunk = 128, kRowPitch = 80, kW4Warps = 8;
+constexpr int kChunk = 128, kW4Warps = 8, kSms = 152;
 
-__device__ __forceinline__ void w4_mma(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ uint32_t sub2(uint32_t x, uint32_t y) {
-  const __nv_bfloat162 r = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&x), *reinterpret_cast<const __nv_bfloat162*>(&y));
-  return *reinterpret_cast<const uint32_t*>(&r);
-}
 __device__ __forceinline__ uint32_t lds4(uint32_t s) {
   uint32_t v;
   asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(s) : "memory");
@@ -65,7 +50,6 @@ __device__ __forceinline__ uint32_t lds4(uint32_t s) {
 // MMA's 32 k): the order of k inside a group is free. Rows are so far apart in shared memory that this has no bank conflicts.
 constexpr int kFewSlots = 5;          // chunks of a warp in the ring, four of them on their way: 64 KB an SM
 constexpr int kFewX = 40 * 1024;      // bytes of tokens that a CTA should hold at most: two CTAs an SM
-constexpr int kSms = 152;
 template <int G>
 __host__ __device__ constexpr int few_pitch() { return G == 128 ? 64 : G == 64 ? 96 : 80; }
 struct FewArgs {
@@ -400,8 +384,8 @@ __global__ void __launch_bounds__(32 * kW4Warps, 2) w4_few_kernel(const FewArgs 
   }
 }
 
-template <int NT, int RT, int G>
-cudaError_t launch_w4(const W4Args& a, int wn, cudaStream_t s);
+template <int NT, int G>
+cudaError_t launch_many(const W4Args& a, cudaStream_t s);
 
 template <int NT, int G, bool VEC>
 cudaError_t launch_few(const W4Args& a, cudaStream_t s) {
@@ -417,7 +401,7 @@ cudaError_t launch_few(const W4Args& a, cudaStream_t s) {
   f.split_k = (chunks + f.split - 1) / f.split * kChunk;
   f.pieces = FastDiv((uint32_t)(f.split_k / 8));
   const size_t smem = few_smem<G>(a.M, f.split_k);
-  if (smem > 227 * 1024) return launch_w4<NT, 1, G>(a, 1, s);   // the tokens of a CTA do not fit: 16 of K past 30000
+  if (smem > 227 * 1024) return launch_many<3, G>(a, s);   // the tokens of a CTA do not fit: 16 of K past 30000
   const int ctas = (smem <= 113 * 1024 ? 2 : 1) * kSms;
   // warps of a tile: the least of rounds times (chunks of a warp, and as much as a chunk for the adding)
   f.wk = kW4Warps;
@@ -435,177 +419,235 @@ cudaError_t launch_few(const W4Args& a, cudaStream_t s) {
   return launch_cluster(w4_few_kernel<NT, G, VEC>, dim3((unsigned)((n < clusters ? n : clusters) * f.split)), dim3(32 * kW4Warps), smem, f.split, s, f);
 }
 
-// ---- more tokens ------------------------------------------------------------------------------------------------------
+// ---- up to 64 tokens --------------------------------------------------------------------------------------------------
+//
+// Here mma.sync (8 cycles of an SM's quarter for 256 weights by 8 tokens) takes as long as the weights or longer, so the
+// weights become exact bf16 (0x4300 | q is 128 + q; less 128 + zero), which needs nothing of the tokens but their order. A warp
+// has 32 rows, whose tokens it reads once from shared memory; the four warps of a quarter of the CTA's rows share out K,
+// chunk by chunk, and those of the same chunks share the tokens' copies. k, k + 4 make a pair of each word and of the tokens.
+constexpr int kManyStages = 2, kManyPitch = 80;   // bytes between weight rows: no bank conflicts for words of eight rows
+template <int NT>
+constexpr int many_groups() { return NT <= 5 ? 3 : 2; }   // most 32-row groups of a CTA: registers
+template <int NT>
+__host__ __device__ constexpr size_t many_smem(int wn) {
+  // tokens [stage][quarter of K][token][256 bytes], weights [stage][warp][32 rows], scales and zeros [2][warp][4 groups][32 rows]
+  return kManyStages * ((size_t)4 * 8 * NT * 256 + (size_t)4 * wn * 32 * kManyPitch) + (size_t)2 * 4 * wn * 4 * 32 * 4;
+}
 
-// Copies in flight a warp: about 10 KB.
-template <int RT>
-constexpr int w4_slots() { return RT == 1 ? 8 : RT == 2 ? 4 : 3; }
-template <int RT>
-constexpr size_t w4_smem() { return (size_t)kW4Warps * w4_slots<RT>() * RT * 16 * kRowPitch; }
+__device__ __forceinline__ void mma_bf16_16816(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_bf16_first(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+}
+__device__ __forceinline__ uint32_t sub2(uint32_t x, uint32_t y) {
+  const __nv_bfloat162 r = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&x), *reinterpret_cast<const __nv_bfloat162*>(&y));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
 
-template <int NT, int RT, int G>   // 8 NT tokens, 16 RT rows a warp, group
-__global__ void __launch_bounds__(32 * kW4Warps, RT * NT > 3 ? 1 : 2) w4_kernel(const W4Args a, int wn) {
-  constexpr int SLOTS = w4_slots<RT>(), SLOT = RT * 16 * kRowPitch, PG = kChunk / G;
-  static_assert(RT * NT * 512 <= SLOTS * SLOT, "the warps' sums fit the ring");
+template <int NT, int G>   // 8 NT tokens, group
+__global__ void __launch_bounds__(128 * many_groups<NT>(), 1) w4_many_kernel(const W4Args a, int wn, int split) {
+  constexpr int PG = kChunk / G, GS = G / 32, XQ = 8 * NT * 256;
   extern __shared__ __align__(16) unsigned char smem[];
   pdl_wait();
   pdl_trigger();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int wk = kW4Warps / wn, kw = warp / wn;   // warps that share rows, and which of them this is
-  const int n0 = (blockIdx.x * wn + warp % wn) * RT * 16;
-  const int groups = a.K / G, chunks = (a.K + kChunk - 1) / kChunk, mine = n0 < a.N ? (chunks - kw + wk - 1) / wk : 0;
-  const uint32_t ring = ptx::su32(smem) + warp * SLOTS * SLOT;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, kq = warp & 3, rg = warp >> 2;
+  const int part = split > 1 ? blockIdx.x % split : 0, cta = split > 1 ? blockIdx.x / split : blockIdx.x;
+  const int n0 = (cta * wn + rg) * 32, groups = a.K / G, chunks = (a.K + kChunk - 1) / kChunk;
+  const int c0 = part * 4 + kq, next = 4 * split;   // this warp's first chunk, and how far it is to its next
+  const int iters = chunks > c0 ? (chunks - c0 + next - 1) / next : 0;   // the same for the warps that share tokens
+  const uint32_t base = ptx::su32(smem), wbase = base + kManyStages * 4 * XQ;
+  const int wstage = 4 * wn * 32 * kManyPitch;
+  uint32_t* sg = reinterpret_cast<uint32_t*>(smem + kManyStages * (4 * XQ + wstage)) + warp * 4 * 32;   // + buffer * 4 wn * 128
 
-  // 16 bytes a lane: 4 lanes a row's 64 bytes, 8 rows at a time
-  const uint8_t* src = a.q + (((int64_t)n0 + g) * a.K >> 1) + 16 * t;
-  const int64_t step8 = (int64_t)a.K * 4;   // 8 rows on
-  const auto copy = [&](int i, int slot) {
-    if (i < mine) {
-      const int k = (kw + i * wk) * kChunk;
+  // 16-byte pieces: tokens by the threads of this quarter of K, a token's pieces with bit 2 flipped for odd tokens (no bank
+  // conflicts for two tokens' 64 bytes); weights by the warp; 0 past the last token, row and k.
+  const int tid = rg * 32 + lane;
+  const uint8_t* wrow[4];
 #pragma unroll
-      for (int r = 0; r < 2 * RT; ++r) {
-        const bool ok = n0 + 8 * r + g < a.N && k + 32 * t < a.K;
-        const uint8_t* p = ok ? src + r * step8 + (k >> 1) : a.q;
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(ring + slot * SLOT + (8 * r + g) * kRowPitch + 16 * t), "l"(p), "r"(ok ? 16 : 0)
-                     : "memory");
+  for (int r = 0; r < 4; ++r) wrow[r] = a.q + ((int64_t)min(n0 + 8 * r + g, a.N - 1) * a.K >> 1);
+  const auto copy = [&](int i) {
+    if (i < iters) {
+      const int k0 = (c0 + next * i) * kChunk, st = i & 1, k = k0 + 8 * (tid & 15);
+      // 2 wn tokens at a time: an even number, so a thread's are all even or all odd
+      uint32_t xd = base + (st * 4 + kq) * XQ + (tid >> 4) * 256 + (((tid & 15) ^ (tid >> 4 & 1) * 4) << 4);
+      const __nv_bfloat16* src = a.x + (int64_t)(tid >> 4) * a.K + k;
+      const int last = k < a.K ? a.M : 0;
+      for (int m = tid >> 4; m < 8 * NT; m += 2 * wn) {
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(xd), "l"(m < last ? src : a.x), "r"(m < last ? 16 : 0) : "memory");
+        xd += 2 * wn * 256;
+        src += (int64_t)2 * wn * a.K;
       }
+      const int at = k0 + 32 * t < a.K ? (k0 + 32 * t) >> 1 : 0;   // past K anything: the tokens are 0
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(wbase + st * wstage + (warp * 32 + 8 * r + g) * kManyPitch + 16 * t), "l"(wrow[r] + at) : "memory");
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
+  // a lane's row's scales and zeros, held while a chunk is computed and then put to where all lanes find them
+  uint16_t raw_s[PG];
+  uint8_t raw_z[PG];
+  const int64_t row_at = (int64_t)min(n0 + lane, a.N - 1) * groups;
+  const auto load = [&](int i) {
+    if (i >= iters) return;
 #pragma unroll
-  for (int i = 0; i < SLOTS - 1; ++i) copy(i, i);
-
-  float acc[RT][NT][4] = {};
-  // scales and zero points of a chunk's groups, loaded a chunk ahead
-  uint16_t sc[RT][2][PG], sn[RT][2][PG];
-  uint8_t zc[RT][2][PG], zn[RT][2][PG];
-  const auto load_groups = [&](int i) {
-#pragma unroll
-    for (int r = 0; r < RT; ++r)
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int j = 0; j < PG; ++j) {
-          const int gr = (kw + i * wk) * PG + j, n = n0 + 16 * r + 8 * h + g;
-          const bool ok = i < mine && gr < groups && n < a.N;
-          const int64_t e = (int64_t)n * groups + gr;
-          sn[r][h][j] = ok ? reinterpret_cast<const uint16_t*>(a.scale)[e] : (uint16_t)0;
-          zn[r][h][j] = ok && a.zero ? a.zero[e] : (uint8_t)8;
-        }
+    for (int j = 0; j < PG; ++j) {
+      const int64_t e = row_at + min((c0 + next * i) * PG + j, groups - 1);
+      raw_s[j] = reinterpret_cast<const uint16_t*>(a.scale)[e];
+      raw_z[j] = a.zero ? a.zero[e] : (uint8_t)8;
+    }
   };
-  load_groups(0);
-  int slot = 0;
-  for (int i = 0; i < mine; ++i) {
+  const auto put = [&](int i) {
+    if (i >= iters) return;
 #pragma unroll
-    for (int r = 0; r < RT; ++r)
+    for (int j = 0; j < PG; ++j) sg[(i & 1) * 4 * wn * 128 + j * 32 + lane] = (uint32_t)raw_s[j] << 16 | (raw_z[j] & 15u);
+  };
+  copy(0);
+  copy(1);
+  load(0);
+  put(0);
+  load(1);
+  float acc[2][NT][4] = {};
+  for (int i = 0; i < iters; ++i) {
+    asm volatile("cp.async.wait_group 1;" ::: "memory");
+    ptx::named_sync(1 + kq, 32 * wn);   // the tokens that others copied
+    // token 8 n + g, piece 4 s + t, with bit 2 flipped for odd tokens
+    const uint32_t xg = base + ((i & 1) * 4 + kq) * XQ + g * 256 + t * 16, odd = g & 1, ws = wbase + (i & 1) * wstage + (warp * 32 + g) * kManyPitch + 4 * t;
+    const uint32_t* sgi = sg + (i & 1) * 4 * wn * 128;
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+    for (int j = 0; j < PG; ++j) {
+      float sum[2][NT][4];
+      uint32_t sz[2][2], z[2][2];
 #pragma unroll
-        for (int j = 0; j < PG; ++j) sc[r][h][j] = sn[r][h][j], zc[r][h][j] = zn[r][h][j];
-    load_groups(i + 1);
-    const int k0 = (kw + i * wk) * kChunk + 8 * t;
-    asm volatile("cp.async.wait_group %0;" ::"n"(SLOTS - 2) : "memory");
-    __syncwarp();   // all lanes' copies are there, and what the next copy overwrites has been read
-    copy(i + SLOTS - 1, slot == 0 ? SLOTS - 1 : slot - 1);
-    const uint32_t ws = ring + slot * SLOT + g * kRowPitch + 4 * t;
-    slot = slot + 1 == SLOTS ? 0 : slot + 1;
-    float part[RT][NT][4];
-    uint32_t z[RT][2];
+      for (int r = 0; r < 2; ++r)
 #pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      constexpr int kStepsOfGroup = G / 32;
-      if (s % kStepsOfGroup == 0) {
+        for (int h = 0; h < 2; ++h) {
+          sz[r][h] = sgi[j * 32 + 16 * r + 8 * h + g];
+          z[r][h] = 0x43004300u | (sz[r][h] & 15u) * 0x10001u;
+        }
 #pragma unroll
-        for (int r = 0; r < RT; ++r) {
+      for (int v = 0; v < GS; ++v) {
+        const int s = j * GS + v;
+        uint32_t xb[NT][4];
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            z[r][h] = 0x43004300u | (zc[r][h][s / kStepsOfGroup] & 15u) * 0x10001u;
+        for (int n = 0; n < NT; ++n) {
+          uint32_t x[4];
+          asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3])
+                       : "r"(xg + n * 2048 + (s ^ odd) * 64) : "memory");
+          xb[n][0] = __byte_perm(x[0], x[2], 0x5410);
+          xb[n][1] = __byte_perm(x[0], x[2], 0x7632);
+          xb[n][2] = __byte_perm(x[1], x[3], 0x5410);
+          xb[n][3] = __byte_perm(x[1], x[3], 0x7632);
+        }
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const uint32_t w0 = lds4(ws + (16 * r) * kManyPitch + 16 * s), w1 = lds4(ws + (16 * r + 8) * kManyPitch + 16 * s);
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            uint32_t f[4];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+              f[2 * u] = sub2((w0 >> (4 * (2 * y + u)) & 0x000f000fu) | 0x43004300u, z[r][0]);
+              f[2 * u + 1] = sub2((w1 >> (4 * (2 * y + u)) & 0x000f000fu) | 0x43004300u, z[r][1]);
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+              if (v == 0 && y == 0) mma_bf16_first(sum[r][n], f, xb[n][0], xb[n][1]);
+              else mma_bf16_16816(sum[r][n], f, xb[n][2 * y], xb[n][2 * y + 1]);
+            }
           }
-#pragma unroll
-          for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) part[r][n][e] = 0.f;
         }
       }
-      uint32_t xb[NT][4];
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (8 * n + g < a.M && k0 + 32 * s < a.K) v = __ldg(reinterpret_cast<const uint4*>(a.x + (int64_t)(8 * n + g) * a.K + k0 + 32 * s));
-        xb[n][0] = __byte_perm(v.x, v.z, 0x5410);
-        xb[n][1] = __byte_perm(v.x, v.z, 0x7632);
-        xb[n][2] = __byte_perm(v.y, v.w, 0x5410);
-        xb[n][3] = __byte_perm(v.y, v.w, 0x7632);
-      }
+      for (int r = 0; r < 2; ++r) {
+        const float s0 = __uint_as_float(sz[r][0] & 0xffff0000u), s1 = __uint_as_float(sz[r][1] & 0xffff0000u);
 #pragma unroll
-      for (int r = 0; r < RT; ++r) {
-        const uint32_t w0 = lds4(ws + (16 * r) * kRowPitch + 16 * s), w1 = lds4(ws + (16 * r + 8) * kRowPitch + 16 * s);
-#pragma unroll
-        for (int y = 0; y < 2; ++y) {
-          uint32_t f[4];
-#pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            f[2 * u] = sub2((w0 >> (4 * (2 * y + u)) & 0x000f000fu) | 0x43004300u, z[r][0]);
-            f[2 * u + 1] = sub2((w1 >> (4 * (2 * y + u)) & 0x000f000fu) | 0x43004300u, z[r][1]);
-          }
-#pragma unroll
-          for (int n = 0; n < NT; ++n) w4_mma(part[r][n], f, xb[n][2 * y], xb[n][2 * y + 1]);
-        }
-      }
-      if ((s + 1) % kStepsOfGroup == 0) {
-#pragma unroll
-        for (int r = 0; r < RT; ++r) {
-          const float s0 = __uint_as_float((uint32_t)sc[r][0][s / kStepsOfGroup] << 16), s1 = __uint_as_float((uint32_t)sc[r][1][s / kStepsOfGroup] << 16);
-#pragma unroll
-          for (int n = 0; n < NT; ++n) {
-            acc[r][n][0] += part[r][n][0] * s0;
-            acc[r][n][1] += part[r][n][1] * s0;
-            acc[r][n][2] += part[r][n][2] * s1;
-            acc[r][n][3] += part[r][n][3] * s1;
-          }
+        for (int n = 0; n < NT; ++n) {
+          acc[r][n][0] += sum[r][n][0] * s0;
+          acc[r][n][1] += sum[r][n][1] * s0;
+          acc[r][n][2] += sum[r][n][2] * s1;
+          acc[r][n][3] += sum[r][n][3] * s1;
         }
       }
     }
+    put(i + 1);
+    load(i + 2);
+    ptx::named_sync(1 + kq, 32 * wn);   // this stage has been read by all
+    copy(i + 2);
   }
-
-  // the sums of the warps that share rows: [warp][token][row]
   asm volatile("cp.async.wait_all;" ::: "memory");
   __syncthreads();
+  // the sums of the quarters of K: [quarter][row of the CTA][token], rows 8 NT + 2 floats apart
   float* sums = reinterpret_cast<float*>(smem);
-  constexpr int ROWS = 16 * RT, TOK = 8 * NT;
+  constexpr int SP = 8 * NT + 2;
 #pragma unroll
-  for (int r = 0; r < RT; ++r)
+  for (int r = 0; r < 2; ++r)
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        sums[(warp * TOK + 8 * n + 2 * t + (e & 1)) * ROWS + 16 * r + 8 * (e >> 1) + g] = acc[r][n][e];
+      for (int h = 0; h < 2; ++h)
+        *reinterpret_cast<float2*>(sums + (size_t)(kq * wn * 32 + rg * 32 + 16 * r + 8 * h + g) * SP + 8 * n + 2 * t) = make_float2(acc[r][n][2 * h], acc[r][n][2 * h + 1]);
   __syncthreads();
-  for (int i = threadIdx.x; i < a.M * wn * ROWS; i += 32 * kW4Warps) {
-    const int m = i / (wn * ROWS), r = i % (wn * ROWS), n = blockIdx.x * wn * ROWS + r;
-    if (n >= a.N) continue;
-    float v = 0.f;
-    for (int w = 0; w < wk; ++w) v += sums[((w * wn + r / ROWS) * TOK + m) * ROWS + r % ROWS];
-    a.out[(int64_t)m * a.N + n] = v + (a.bias ? a.bias[n] : 0.f);
+  const int rows = wn * 32;
+  if (split > 1) {   // each CTA's sums go to the cluster's first: [part][token][row], behind its own
+    asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");   // its copies are done
+    float* recv = sums + (size_t)4 * rows * SP;
+    for (int m = warp; m < a.M; m += 4 * wn)
+      for (int r = lane; r < rows; r += 32) {
+        float v = 0.f;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v += sums[(size_t)(q * rows + r) * SP + m];
+        uint32_t dst;
+        asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(dst) : "r"(ptx::su32(recv + (part * a.M + m) * rows + r)));
+        asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(dst), "f"(v) : "memory");
+      }
+    asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if (part) return;
+    for (int m = warp; m < a.M; m += 4 * wn)
+      for (int r = lane; r < rows; r += 32) {
+        const int n = cta * rows + r;
+        if (n >= a.N) continue;
+        float v = 0.f;
+        for (int c = 0; c < split; ++c) v += recv[(c * a.M + m) * rows + r];
+        a.out[(int64_t)m * a.N + n] = v + (a.bias ? a.bias[n] : 0.f);
+      }
+    return;
   }
+  for (int m = warp; m < a.M; m += 4 * wn)
+    for (int r = lane; r < rows; r += 32) {
+      const int n = cta * rows + r;
+      if (n >= a.N) continue;
+      float v = 0.f;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) v += sums[(size_t)(q * rows + r) * SP + m];
+      a.out[(int64_t)m * a.N + n] = v + (a.bias ? a.bias[n] : 0.f);
+    }
 }
 
-template <int NT, int RT, int G>
-cudaError_t launch_w4(const W4Args& a, int wn, cudaStream_t s) {
+template <int NT, int G>
+cudaError_t launch_many(const W4Args& a, cudaStream_t s) {
   static OncePerDevice once;
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
-  constexpr int smem = (int)w4_smem<RT>();
-  e = (cudaError_t)once.run(dev, [&] { return (int)cudaFuncSetAttribute(w4_kernel<NT, RT, G>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem); });
+  e = (cudaError_t)once.run(dev, [&] { return (int)cudaFuncSetAttribute(w4_many_kernel<NT, G>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)many_smem<NT>(many_groups<NT>())); });
   if (e != cudaSuccess) return e;
-  const int rows = 16 * RT * wn;
-  return launch_k(w4_kernel<NT, RT, G>, dim3((unsigned)(((int64_t)a.N + rows - 1) / rows)), 32 * kW4Warps, smem, s, a, wn);
+  // As few rows a CTA as fill the SMs once; with SMs left over, a cluster shares K as far as every warp keeps a chunk.
+  int wn = 1, split = 1;
+  while (wn < many_groups<NT>() && ((int64_t)a.N + 32 * wn - 1) / (32 * wn) > kSms) ++wn;
+  const int64_t ctas = ((int64_t)a.N + 32 * wn - 1) / (32 * wn);
+  const int chunks = (a.K + kChunk - 1) / kChunk;
+  while (wn == 1 && split < 8 && ctas * split * 2 <= kSms && chunks > 4 * split) split *= 2;
+  return launch_cluster(w4_many_kernel<NT, G>, dim3((unsigned)(ctas * split)), dim3(128 * wn), many_smem<NT>(wn), split, s, a, wn, split);
 }
 
 template <int G>
 cudaError_t launch_group(const W4Args& a, cudaStream_t s) {
-  const int tiles = (a.N + 15) / 16;   // of 16 rows
   const int tokens = (a.M + 7) / 8;
   if (tokens <= 2) {
     constexpr int PG = kChunk / G;   // groups of a chunk
@@ -613,9 +655,13 @@ cudaError_t launch_group(const W4Args& a, cudaStream_t s) {
       return tokens == 1 ? launch_few<1, G, true>(a, s) : launch_few<2, G, true>(a, s);
     if constexpr (PG > 1) return tokens == 1 ? launch_few<1, G, false>(a, s) : launch_few<2, G, false>(a, s);
   }
-  if (tokens <= 4) return tiles >= 152 * 4 ? launch_w4<4, 2, G>(a, 2, s) : launch_w4<4, 1, G>(a, 1, s);
-  if (tokens <= 6) return tiles >= 152 * 4 ? launch_w4<6, 2, G>(a, 2, s) : launch_w4<6, 1, G>(a, 1, s);
-  return tiles >= 152 * 4 ? launch_w4<8, 2, G>(a, 2, s) : launch_w4<8, 1, G>(a, 1, s);
+  switch (tokens) {
+    case 3: return launch_many<3, G>(a, s);
+    case 4: return launch_many<4, G>(a, s);
+    case 5: return launch_many<5, G>(a, s);
+    case 6: return launch_many<6, G>(a, s);
+    default: return launch_many<8, G>(a, s);
+  }
 }
 
 // fp32 -> bf16 bits, nearest, ties to even, for finite values.
