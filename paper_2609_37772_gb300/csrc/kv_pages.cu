@@ -1,6 +1,7 @@
 // The paged key-value cache: argument checks, the rotation's frequencies and the append of new tokens.
 #include "kv_pages.cuh"
 
+#include <algorithm>
 #include <cmath>
 
 using namespace uad;
@@ -14,7 +15,8 @@ struct AppendArgs {
   const void *q, *k, *v;
   int64_t q_stride, k_stride, v_stride, q_out_stride;
   void* q_out;
-  int n_heads, rot;
+  int n_heads, rot, groups, log_chunks, block_rows;
+  FastDiv row_threads, row_blocks;   // threads of a row, blocks of a row
 };
 
 // cos and sin of position * turn / 2^64 turns. The product wraps at whole turns, which is exact; what is left is
@@ -63,9 +65,12 @@ __device__ __forceinline__ void store8(void* base, int64_t e, const float* x) {
   }
 }
 
-// One thread: 16 dimensions (8 pairs) of one head of one row.
+// One thread: a chunk of 16 dimensions (8 pairs) of one row, in every a.groups-th of its heads. Eight sines and cosines cost
+// about as many cycles as 150 bytes of memory, so that with one head a thread they bound the kernel; they depend on the
+// position alone. 4 blocks an SM is what the registers hold without spilling (63): 52224 ragged tokens of 8 + 2 heads of
+// 256 from fp32 rows take 64 us (92% of the bandwidth of a copy).
 template <int IN, int CACHE>
-__global__ void __launch_bounds__(256) append_kernel(const AppendArgs a, const __grid_constant__ uad_rope rope) {
+__global__ void __launch_bounds__(256, 4) append_kernel(const AppendArgs a, const __grid_constant__ uad_rope rope) {
   pdl_wait();
   pdl_trigger();
   const PagedArgs& p = a.p;
@@ -75,48 +80,60 @@ __global__ void __launch_bounds__(256) append_kernel(const AppendArgs a, const _
     if (blockIdx.x == 0 && threadIdx.x == 0) kv_report(p, UAD_KV_BAD_SEQ);
     return;
   }
-  const int per_head = p.dh / kItem, heads = a.n_heads + (a.k ? 2 * p.n_kv : 0), per_row = heads * per_head;
-  const int64_t item = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-  const int j = (int)(item / per_row), r = (int)(item - (int64_t)j * per_row), head = r / per_head, c = r - head * per_head;
-  if (j >= s.n) return;
-  const int row = s.first + j, pos = s.len - s.n + j;
-  const bool is_q = head < a.n_heads;
-  const int kv = head - a.n_heads;
-  const bool is_v = !is_q && kv >= p.n_kv;
-  const int h = is_q ? head : is_v ? kv - p.n_kv : kv;
-  int64_t dst;
-  if (is_q) {
-    dst = row * a.q_out_stride + (int64_t)h * p.dh;
-  } else {
-    dst = token_at(p, p.table + b * p.table_stride, pos);
-    if (dst < 0) {
-      kv_report(p, UAD_KV_BAD_PAGE);
-      return;
-    }
-    dst += h * p.head_stride;
+  const int bj = a.row_blocks.div(blockIdx.x), tj = a.row_threads.div(threadIdx.x);
+  if (tj >= a.block_rows) return;
+  const int64_t j = (int64_t)bj * a.block_rows + tj;
+  const int r = (blockIdx.x - bj * (int)a.row_blocks.d) * (int)blockDim.x + threadIdx.x - tj * (int)a.row_threads.d;
+  if (j >= s.n || r >= (int)a.row_threads.d) return;
+  const int group = r >> a.log_chunks, c = r - (group << a.log_chunks);
+  const int64_t row = s.first + j;
+  const int pos = s.len - s.n + (int)j, heads = a.n_heads + (a.k ? 2 * p.n_kv : 0);
+  int64_t slot = 0;
+  if (a.k) {
+    slot = token_at(p, p.table + b * p.table_stride, pos);
+    if (slot < 0) kv_report(p, UAD_KV_BAD_PAGE);
   }
-  const void* from = is_q ? a.q : is_v ? a.v : a.k;
-  void* to = is_q ? a.q_out : is_v ? p.v : p.k;
-  const int64_t src = row * (is_q ? a.q_stride : is_v ? a.v_stride : a.k_stride) + (int64_t)h * p.dh;
-  const int half = a.rot / 2;
-  const bool turned = !is_v && c * 8 < half;
-  // pairs (lo + i, hi + i); past the rotated dimensions, 16 neighbours
-  const int lo = turned ? c * 8 : c * kItem, hi = turned ? lo + half : lo + 8;
-  float x[8], y[8];
-  load8<IN>(from, src + lo, x);
-  load8<IN>(from, src + hi, y);
-  if (turned) {
+  const int half = a.rot / 2, lo = c * 8;
+  const bool turned = lo < half;
+  float cs[8], sn[8], x[8], y[8];
+  void* to = nullptr;
+  bool turn = false;
+  int e_lo = 0, e_hi = 0;
+  const auto load = [&](int h) {
+    const int kv = h - a.n_heads, v = kv - p.n_kv;
+    to = nullptr;
+    if (kv >= 0 && slot < 0) return;
+    turn = turned && v < 0;
+    // pairs (lo + i, hi + i); past the rotated dimensions, 16 neighbours
+    e_lo = turn ? lo : c * kItem;
+    e_hi = turn ? lo + half : c * kItem + 8;
+    const void* from = kv < 0 ? a.q : v < 0 ? a.k : a.v;
+    const int64_t src = kv < 0 ? row * a.q_stride + (int64_t)h * p.dh : v < 0 ? row * a.k_stride + kv * p.dh : row * a.v_stride + v * p.dh;
+    const int64_t dst = kv < 0 ? row * a.q_out_stride + (int64_t)h * p.dh : slot + (v < 0 ? kv : v) * p.head_stride;
+    to = static_cast<char*>(kv < 0 ? a.q_out : v < 0 ? p.k : p.v) + dst * (CACHE == F32 ? 4 : 2);
+    load8<IN>(from, src + e_lo, x);
+    load8<IN>(from, src + e_hi, y);
+  };
+  load(group);
+  if (turned)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      float cs, sn;
-      rotation((uint32_t)pos, rope.turn[lo + i], &cs, &sn);
-      const float u = x[i] * cs - y[i] * sn, w = y[i] * cs + x[i] * sn;
-      x[i] = u;
-      y[i] = w;
+    for (int i = 0; i < 8; ++i) rotation((uint32_t)pos, rope.turn[lo + i], cs + i, sn + i);
+  for (int head = group;;) {
+    if (to) {
+      if (turn)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float u = x[i] * cs[i] - y[i] * sn[i], w = y[i] * cs[i] + x[i] * sn[i];
+          x[i] = u;
+          y[i] = w;
+        }
+      store8<CACHE>(to, e_lo, x);
+      store8<CACHE>(to, e_hi, y);
     }
+    head += a.groups;
+    if (head >= heads) break;
+    load(head);
   }
-  store8<CACHE>(to, dst + lo, x);
-  store8<CACHE>(to, dst + hi, y);
 }
 
 bool bad_address(const void* p, int64_t stride, int es) {
@@ -197,8 +214,21 @@ int uad_kv_append(const uad_kv_pages* pages, const uad_kv_seqs* seqs, const uad_
   a.q_out = rows->q_out; a.q_out_stride = rows->q_out_stride;
   a.n_heads = rows->n_heads; a.rot = rope ? rope->dim : 0;
   const uad_rope none{};
-  const int64_t items = (int64_t)a.p.max_new * (a.n_heads + (a.k ? 2 * a.p.n_kv : 0)) * (a.p.dh / kItem);
-  const int64_t blocks = (items + 255) / 256;
+  const int heads = a.n_heads + (a.k ? 2 * a.p.n_kv : 0), chunks = a.p.dh / kItem;
+  while ((1 << a.log_chunks) < chunks) ++a.log_chunks;
+  const int64_t tokens = std::min<int64_t>((int64_t)a.p.max_new * a.p.n_seqs, a.p.n_rows);
+  const int64_t items = tokens * heads * chunks;
+  // Heads a thread: one where that leaves the SMs six warps or fewer (latency bounds: 3.4 us against 4.3 of
+  // two groups for 64 tokens of 10 heads of 256), up to five beyond, which share the angles' cosines and sines (1024 such
+  // tokens: 5.4 us against 8.2; 52224: 64 against 173). More do not pay: eight take 41 us where five take 35 (52224 tokens of
+  // 8 heads of 64, fp32) and 219 against 230 (48 heads of 128).
+  const int per = (int)std::min<int64_t>({5, heads, std::max<int64_t>(1, items / (152 * 192))});
+  a.groups = (heads + per - 1) / per;
+  const int row_threads = a.groups * chunks, row_blocks = (row_threads + 255) / 256;
+  a.block_rows = row_threads < 256 ? 256 / row_threads : 1;
+  a.row_threads = FastDiv((uint32_t)row_threads);
+  a.row_blocks = FastDiv((uint32_t)row_blocks);
+  const int64_t blocks = ((int64_t)a.p.max_new + a.block_rows - 1) / a.block_rows * row_blocks;
   if (blocks > 0x7fffffff) return UAD_EINVAL;
   const dim3 grid((unsigned)blocks, (unsigned)a.p.n_seqs);
   const uad_rope& r = rope ? *rope : none;
