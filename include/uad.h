@@ -401,9 +401,9 @@ int uad_paged_attention(const uad_kv_pages* pages, const uad_kv_seqs* seqs, cons
  * decoding step, whose time is that of reading the weights. x: device bf16; q: device [N][K / 2], k even in the low
  * four bits of byte k / 2; scale: device bf16 [N][K / group]; |scale| < 2^100; zero: device uint8 [N][K / group], 0..15 (only the low
  * four bits are read), or NULL: 8; bias: device fp32 [N] or NULL; out: device fp32 [M][N]. Sums are in fp32, over a group
- * first and then scaled; up to 16 tokens, the sum of q x less zero times the sum of x (x to 30 bits below its group's largest
- * value), above, of the exact x (q - zero). x and q 16-byte aligned. 1 <= M <= UAD_W4_MAX_ROWS, N >= 1, K % group == 0,
- * group 32, 64 or 128, N * K <= 2^35. Asynchronous on `stream` and in its order; allocates nothing; may be captured.
+ * first and then scaled; up to 8 tokens with groups of 64 and 128, the sum of q x less zero times the sum of x (x to 30 bits below its group's largest
+ * value), else of the exact x (q - zero). x and q 16-byte aligned. 1 <= M <= UAD_W4_MAX_ROWS, N >= 1, K % group == 0,
+ * group 32, 64 or 128, K <= 2^30, N * K <= 2^35. Asynchronous on `stream` and in its order; allocates nothing; may be captured.
  * Errors: UAD_EINVAL, UAD_ETOOBIG (M: dequantise and use uad_linear), UAD_ECUDA. */
 #define UAD_W4_MAX_ROWS 64
 int uad_linear_w4(const void* x, const uint8_t* q, const uint16_t* scale, const uint8_t* zero, const float* bias,

@@ -32,7 +32,14 @@ __device__ __forceinline__ uint32_t lds4(uint32_t s) {
   return v;
 }
 
-// ---- up to 16 tokens: a stream of weights -------------------------------------------------------------------------------
+// Nibbles 0 and 4 of w as bf16: 128 + q. (x & mask) | constant in one instruction, which the compiler makes two of.
+__device__ __forceinline__ uint32_t nibbles(uint32_t w) {
+  uint32_t r;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(w), "r"(0x000f000fu), "r"(0x43004300u));
+  return r;
+}
+
+// ---- up to 8 tokens: a stream of weights --------------------------------------------------------------------------------
 //
 // What bounds a few tokens, once the weights arrive at full bandwidth (14 cycles of an SM's quarter for 256 weights), is
 // taking the nibbles apart. As fp16 the bits of a nibble at the bottom of a half word are the subnormal q 2^-24, four bits
@@ -93,8 +100,9 @@ __device__ __forceinline__ uint32_t pack_f16(float x, float y) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-template <int NT, int G, bool VEC>   // VEC: a chunk's scales, and its zeros, are read as one word
+template <int G, bool VEC>   // VEC: a chunk's scales, and its zeros, are read as one word
 __global__ void __launch_bounds__(32 * kW4Warps, 2) w4_few_kernel(const FewArgs f) {
+  constexpr int NT = 1;   // eights of tokens
   constexpr int PITCH = few_pitch<G>(), SLOT = 16 * PITCH, PG = kChunk / G, GS = G / 32;   // groups of a chunk, steps of a group
   extern __shared__ __align__(16) unsigned char smem[];
   pdl_wait();
@@ -387,13 +395,13 @@ __global__ void __launch_bounds__(32 * kW4Warps, 2) w4_few_kernel(const FewArgs 
 template <int NT, int G>
 cudaError_t launch_many(const W4Args& a, cudaStream_t s);
 
-template <int NT, int G, bool VEC>
+template <int G, bool VEC>
 cudaError_t launch_few(const W4Args& a, cudaStream_t s) {
   static OncePerDevice once;
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
-  e = (cudaError_t)once.run(dev, [&] { return (int)cudaFuncSetAttribute(w4_few_kernel<NT, G, VEC>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024); });
+  e = (cudaError_t)once.run(dev, [&] { return (int)cudaFuncSetAttribute(w4_few_kernel<G, VEC>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024); });
   if (e != cudaSuccess) return e;
   FewArgs f{a, 1, 0, 0, 0, FastDiv(1)};
   const int tiles = (a.N + 15) / 16, chunks = (a.K + kChunk - 1) / kChunk;
@@ -401,7 +409,6 @@ cudaError_t launch_few(const W4Args& a, cudaStream_t s) {
   f.split_k = (chunks + f.split - 1) / f.split * kChunk;
   f.pieces = FastDiv((uint32_t)(f.split_k / 8));
   const size_t smem = few_smem<G>(a.M, f.split_k);
-  if (smem > 227 * 1024) return launch_many<3, G>(a, s);   // the tokens of a CTA do not fit: 16 of K past 30000
   const int ctas = (smem <= 113 * 1024 ? 2 : 1) * kSms;
   // warps of a tile: the least of rounds times (chunks of a warp, and as much as a chunk for the adding)
   f.wk = kW4Warps;
@@ -413,25 +420,31 @@ cudaError_t launch_few(const W4Args& a, cudaStream_t s) {
       if (cost < best) best = cost, f.wk = wk;
     }
   }
+  // Three tokens and more go faster by tiles of 32 rows where a tile's chunks are shared out, unless they are few (4 tokens of
+  // 4096 x 4096 8.4 us against 7.4, 8 of 8192 x 2048 14.1 against 7.9; but 2.9 against 3.5 for 768 x 2304, and 13 against 18 for
+  // 2048 x 32768, where every warp has tiles of its own). Where the tokens of a CTA do not fit, all do.
+  if ((a.M > 2 && f.wk > 1 && chunks > 8) || smem > 227 * 1024) return launch_many<1, G>(a, s);
   const int64_t clusters = ctas / f.split, rounds = ((int64_t)tiles * f.wk + clusters * kW4Warps - 1) / (clusters * kW4Warps);
   f.per_cta = (int)((tiles + clusters * rounds - 1) / (clusters * rounds));   // even rounds
   const int64_t n = (tiles + f.per_cta - 1) / f.per_cta;
-  return launch_cluster(w4_few_kernel<NT, G, VEC>, dim3((unsigned)((n < clusters ? n : clusters) * f.split)), dim3(32 * kW4Warps), smem, f.split, s, f);
+  return launch_cluster(w4_few_kernel<G, VEC>, dim3((unsigned)((n < clusters ? n : clusters) * f.split)), dim3(32 * kW4Warps), smem, f.split, s, f);
 }
 
-// ---- up to 64 tokens --------------------------------------------------------------------------------------------------
+// ---- up to 64 tokens: mma.sync ------------------------------------------------------------------------------------------
 //
 // Here mma.sync (8 cycles of an SM's quarter for 256 weights by 8 tokens) takes as long as the weights or longer, so the
 // weights become exact bf16 (0x4300 | q is 128 + q; less 128 + zero), which needs nothing of the tokens but their order. A warp
 // has 32 rows, whose tokens it reads once from shared memory; the four warps of a quarter of the CTA's rows share out K,
 // chunk by chunk, and those of the same chunks share the tokens' copies. k, k + 4 make a pair of each word and of the tokens.
-constexpr int kManyStages = 2, kManyPitch = 80;   // bytes between weight rows: no bank conflicts for words of eight rows
+// What bounds it is issuing: with 40 tokens some 830 instructions a warp and chunk, 80 of them MMAs, at 0.45 a cycle. 16, 24 and 32
+// tokens: 4096 x 14337 in groups of 64 16.6, 18.5 and 21.9 us (30 MB: 1.8, 1.6 and 1.4 TB/s), 2048 x 32768 17, 23 and 32 us.
+constexpr int kManyPitch = 80;   // bytes between weight rows: no bank conflicts for words of eight rows
 template <int NT>
-constexpr int many_groups() { return NT <= 5 ? 3 : 2; }   // most 32-row groups of a CTA: registers
+constexpr int many_groups() { return NT <= 2 ? 4 : NT <= 5 ? 3 : 2; }   // most 32-row groups of a CTA: registers
 template <int NT>
-__host__ __device__ constexpr size_t many_smem(int wn) {
+__host__ __device__ constexpr size_t many_smem(int wn, int stages) {
   // tokens [stage][quarter of K][token][256 bytes], weights [stage][warp][32 rows], scales and zeros [2][warp][4 groups][32 rows]
-  return kManyStages * ((size_t)4 * 8 * NT * 256 + (size_t)4 * wn * 32 * kManyPitch) + (size_t)2 * 4 * wn * 4 * 32 * 4;
+  return stages * ((size_t)4 * 8 * NT * 256 + (size_t)4 * wn * 32 * kManyPitch) + (size_t)2 * 4 * wn * 4 * 32 * 4;
 }
 
 __device__ __forceinline__ void mma_bf16_16816(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
@@ -450,19 +463,19 @@ __device__ __forceinline__ uint32_t sub2(uint32_t x, uint32_t y) {
 }
 
 template <int NT, int G>   // 8 NT tokens, group
-__global__ void __launch_bounds__(128 * many_groups<NT>(), 1) w4_many_kernel(const W4Args a, int wn, int split) {
+__global__ void __launch_bounds__(128 * many_groups<NT>(), 1) w4_many_kernel(const W4Args a, int wn, int split, int stages) {
   constexpr int PG = kChunk / G, GS = G / 32, XQ = 8 * NT * 256;
   extern __shared__ __align__(16) unsigned char smem[];
   pdl_wait();
   pdl_trigger();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, kq = warp & 3, rg = warp >> 2;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, rg = warp >> 2, kq = (warp + rg) & 3;
   const int part = split > 1 ? blockIdx.x % split : 0, cta = split > 1 ? blockIdx.x / split : blockIdx.x;
   const int n0 = (cta * wn + rg) * 32, groups = a.K / G, chunks = (a.K + kChunk - 1) / kChunk;
   const int c0 = part * 4 + kq, next = 4 * split;   // this warp's first chunk, and how far it is to its next
   const int iters = chunks > c0 ? (chunks - c0 + next - 1) / next : 0;   // the same for the warps that share tokens
-  const uint32_t base = ptx::su32(smem), wbase = base + kManyStages * 4 * XQ;
+  const uint32_t base = ptx::su32(smem), wbase = base + stages * 4 * XQ;
   const int wstage = 4 * wn * 32 * kManyPitch;
-  uint32_t* sg = reinterpret_cast<uint32_t*>(smem + kManyStages * (4 * XQ + wstage)) + warp * 4 * 32;   // + buffer * 4 wn * 128
+  uint32_t* sg = reinterpret_cast<uint32_t*>(smem + stages * (4 * XQ + wstage)) + warp * 4 * 32;   // + buffer * 4 wn * 128
 
   // 16-byte pieces: tokens by the threads of this quarter of K, a token's pieces with bit 2 flipped for odd tokens (no bank
   // conflicts for two tokens' 64 bytes); weights by the warp; 0 past the last token, row and k.
@@ -470,9 +483,9 @@ __global__ void __launch_bounds__(128 * many_groups<NT>(), 1) w4_many_kernel(con
   const uint8_t* wrow[4];
 #pragma unroll
   for (int r = 0; r < 4; ++r) wrow[r] = a.q + ((int64_t)min(n0 + 8 * r + g, a.N - 1) * a.K >> 1);
-  const auto copy = [&](int i) {
+  const auto copy = [&](int i, int st) {
     if (i < iters) {
-      const int k0 = (c0 + next * i) * kChunk, st = i & 1, k = k0 + 8 * (tid & 15);
+      const int k0 = (c0 + next * i) * kChunk, k = k0 + 8 * (tid & 15);
       // 2 wn tokens at a time: an even number, so a thread's are all even or all odd
       uint32_t xd = base + (st * 4 + kq) * XQ + (tid >> 4) * 256 + (((tid & 15) ^ (tid >> 4 & 1) * 4) << 4);
       const __nv_bfloat16* src = a.x + (int64_t)(tid >> 4) * a.K + k;
@@ -489,15 +502,16 @@ __global__ void __launch_bounds__(128 * many_groups<NT>(), 1) w4_many_kernel(con
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  // a lane's row's scales and zeros, held while a chunk is computed and then put to where all lanes find them
+  // Scales and zeros of the warp's rows, PG neighbours of a row by as many lanes, held while a chunk is computed and then put to
+  // where all lanes find them
   uint16_t raw_s[PG];
   uint8_t raw_z[PG];
-  const int64_t row_at = (int64_t)min(n0 + lane, a.N - 1) * groups;
-  const auto load = [&](int i) {
+  const auto load = [&](int i) {   // N K / G < 2^31
     if (i >= iters) return;
+    const int gr = min((c0 + next * i) * PG + lane % PG, groups - 1);
 #pragma unroll
     for (int j = 0; j < PG; ++j) {
-      const int64_t e = row_at + min((c0 + next * i) * PG + j, groups - 1);
+      const int e = min(n0 + j * (32 / PG) + lane / PG, a.N - 1) * groups + gr;
       raw_s[j] = reinterpret_cast<const uint16_t*>(a.scale)[e];
       raw_z[j] = a.zero ? a.zero[e] : (uint8_t)8;
     }
@@ -505,19 +519,21 @@ __global__ void __launch_bounds__(128 * many_groups<NT>(), 1) w4_many_kernel(con
   const auto put = [&](int i) {
     if (i >= iters) return;
 #pragma unroll
-    for (int j = 0; j < PG; ++j) sg[(i & 1) * 4 * wn * 128 + j * 32 + lane] = (uint32_t)raw_s[j] << 16 | (raw_z[j] & 15u);
+    for (int j = 0; j < PG; ++j) sg[(i & 1) * 4 * wn * 128 + (lane % PG) * 32 + j * (32 / PG) + lane / PG] = (uint32_t)raw_s[j] << 16 | (raw_z[j] & 15u);
   };
-  copy(0);
-  copy(1);
+  for (int i = 0; i < stages - 1; ++i) copy(i, i);
   load(0);
   put(0);
   load(1);
   float acc[2][NT][4] = {};
-  for (int i = 0; i < iters; ++i) {
-    asm volatile("cp.async.wait_group 1;" ::: "memory");
-    ptx::named_sync(1 + kq, 32 * wn);   // the tokens that others copied
+  for (int i = 0, st = 0; i < iters; ++i) {
+    if (stages == 4) asm volatile("cp.async.wait_group 2;" ::: "memory");
+    else if (stages == 3) asm volatile("cp.async.wait_group 1;" ::: "memory");
+    else asm volatile("cp.async.wait_group 0;" ::: "memory");
+    ptx::named_sync(1 + kq, 32 * wn);   // the tokens that others copied are there, and the chunk before has been read by all
+    copy(i + stages - 1, st ? st - 1 : stages - 1);
     // token 8 n + g, piece 4 s + t, with bit 2 flipped for odd tokens
-    const uint32_t xg = base + ((i & 1) * 4 + kq) * XQ + g * 256 + t * 16, odd = g & 1, ws = wbase + (i & 1) * wstage + (warp * 32 + g) * kManyPitch + 4 * t;
+    const uint32_t xg = base + (st * 4 + kq) * XQ + g * 256 + t * 16, odd = g & 1, ws = wbase + st * wstage + (warp * 32 + g) * kManyPitch + 4 * t;
     const uint32_t* sgi = sg + (i & 1) * 4 * wn * 128;
 #pragma unroll
     for (int j = 0; j < PG; ++j) {
@@ -552,8 +568,8 @@ __global__ void __launch_bounds__(128 * many_groups<NT>(), 1) w4_many_kernel(con
             uint32_t f[4];
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-              f[2 * u] = sub2((w0 >> (4 * (2 * y + u)) & 0x000f000fu) | 0x43004300u, z[r][0]);
-              f[2 * u + 1] = sub2((w1 >> (4 * (2 * y + u)) & 0x000f000fu) | 0x43004300u, z[r][1]);
+              f[2 * u] = sub2(nibbles(w0 >> (4 * (2 * y + u))), z[r][0]);
+              f[2 * u + 1] = sub2(nibbles(w1 >> (4 * (2 * y + u))), z[r][1]);
             }
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
@@ -577,8 +593,7 @@ __global__ void __launch_bounds__(128 * many_groups<NT>(), 1) w4_many_kernel(con
     }
     put(i + 1);
     load(i + 2);
-    ptx::named_sync(1 + kq, 32 * wn);   // this stage has been read by all
-    copy(i + 2);
+    if (++st == stages) st = 0;
   }
   asm volatile("cp.async.wait_all;" ::: "memory");
   __syncthreads();
@@ -635,27 +650,322 @@ cudaError_t launch_many(const W4Args& a, cudaStream_t s) {
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
-  e = (cudaError_t)once.run(dev, [&] { return (int)cudaFuncSetAttribute(w4_many_kernel<NT, G>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)many_smem<NT>(many_groups<NT>())); });
+  e = (cudaError_t)once.run(dev, [&] { return (int)cudaFuncSetAttribute(w4_many_kernel<NT, G>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024); });
   if (e != cudaSuccess) return e;
-  // As few rows a CTA as fill the SMs once; with SMs left over, a cluster shares K as far as every warp keeps a chunk.
+  // The rows a CTA that leave the fullest SM the fewest, the more the better; with SMs left over, a cluster shares K as far as
+  // every warp keeps a chunk.
   int wn = 1, split = 1;
-  while (wn < many_groups<NT>() && ((int64_t)a.N + 32 * wn - 1) / (32 * wn) > kSms) ++wn;
+  const int64_t sets = ((int64_t)a.N + 31) / 32;
+  int64_t best = INT64_MAX;
+  for (int w = many_groups<NT>(); w >= 1; --w) {
+    const int64_t rows = ((sets + w - 1) / w + kSms - 1) / kSms * w;   // of the fullest SM
+    if (rows < best) best = rows, wn = w;
+  }
   const int64_t ctas = ((int64_t)a.N + 32 * wn - 1) / (32 * wn);
   const int chunks = (a.K + kChunk - 1) / kChunk;
   while (wn == 1 && split < 8 && ctas * split * 2 <= kSms && chunks > 4 * split) split *= 2;
-  return launch_cluster(w4_many_kernel<NT, G>, dim3((unsigned)(ctas * split)), dim3(128 * wn), many_smem<NT>(wn), split, s, a, wn, split);
+  // A CTA that is alone on its SM copies up to three chunks ahead; else the next CTA's work hides the copies, and smaller ones let
+  // more of them in (24 tokens: 14336 x 4096 21 us against 28, but 2048 x 32768 40 against 22).
+  int stages = ctas * split <= kSms ? 4 : 2;
+  while (stages > 2 && many_smem<NT>(wn, stages) > 227 * 1024) --stages;
+  return launch_cluster(w4_many_kernel<NT, G>, dim3((unsigned)(ctas * split)), dim3(128 * wn), many_smem<NT>(wn, stages), split, s, a, wn, split, stages);
+}
+
+// ---- up to 64 tokens: tcgen05 ------------------------------------------------------------------------------------------
+//
+// A CTA of four warps has 128 rows and a share of K. A thread takes a row's nibbles apart, 128 k (64) at a time, as exact bf16
+// (0x4300 | q is 128 + q; less 128 + zero) and puts them into tensor memory as the MMA's first operand; the tokens, in the
+// nibbles' order (k, k + 4 are neighbours), are the second, in shared memory. A group's products are summed by themselves
+// and read back: a thread has a row of them, and multiplies them by the group's scale. While the MMAs of one step run, the
+// nibbles of the next are taken apart.
+//
+// A step is a chain (weights, nibbles, tensor memory, the sums before, a barrier, MMAs) of a microsecond, in which a CTA's four
+// warps issue about 450 instructions each; what hides it is three CTAs an SM. MMAs are a fifth of it. With 40 and 64 tokens,
+// 2048 x 32768 takes 25 and 27 us (the kernel above: 38 and 52), 14336 x 4096 25 and 31 (33 and 42), in groups of 32 4096 x 32768
+// 55 and 58 (78 and 97); 4096 x 14336, which is an even share for the kernel above, 25 and 31 (22 and 44).
+constexpr int kTcPitch = 80, kTcW = 3;   // bytes between weight rows: no bank conflicts for eight rows' 16 bytes; chunks in the ring
+constexpr int kTcBlock = 8, kTcSg = 9;   // groups whose scales are loaded together; words between rows of them
+template <int NB, int G>
+struct TcShape {
+  static constexpr int KS = G == 128 ? 128 : 64;                // k of a step
+  static constexpr int GS = KS > G ? KS / G : 1;                // groups that end with a step
+  static constexpr int COLS = KS / 2 + GS * NB <= 128 ? 128 : 256;   // tensor memory: a step's weights, the sums
+  static constexpr int CTAS = COLS > 128 ? 2 : 3;                // of an SM
+  static constexpr int R = NB >= 48 && KS == 128 ? 2 : 3;                    // steps of tokens in the ring
+  static constexpr int XB = NB * 128, X = KS / 64 * XB;         // bytes of 64 k of the tokens, of a step's
+  static constexpr int W0 = R * X, SG0 = W0 + kTcW * 128 * kTcPitch, BAR0 = SG0 + 2 * 128 * kTcSg * 4;
+  static constexpr int SMEM = BAR0 + 16 + 1024;                 // and the alignment of the tokens
+};
+
+// MMAs that have been issued: a microsecond; false after a quarter of a second or so.
+__device__ __forceinline__ bool wait_mma(uint64_t* bar, uint32_t parity) {
+  for (uint32_t i = 0; i < (1u << 20); ++i)
+    if (ptx::mbar_test(bar, parity)) return true;
+  return false;
+}
+
+template <int NB, int G>   // tokens that the MMA has, group
+__global__ void __launch_bounds__(128, TcShape<NB, G>::CTAS) w4_tc_kernel(const W4Args a, int split) {
+  using S = TcShape<NB, G>;
+  constexpr int KS = S::KS, GS = S::GS, R = S::R, NX = NB / 16, HB = KS / 64;   // 16-byte pieces of a thread of 64 k of the tokens
+  constexpr int SB = kTcBlock * G / KS;                                       // steps of a block of scales
+  extern __shared__ __align__(16) unsigned char smem_raw[];
+  const uint32_t base = (ptx::su32(smem_raw) + 1023u) & ~1023u;
+  unsigned char* smem = smem_raw + (base - ptx::su32(smem_raw));
+  uint64_t* bar = reinterpret_cast<uint64_t*>(smem + S::BAR0);
+  uint32_t* slot = reinterpret_cast<uint32_t*>(smem + S::BAR0 + 8);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  pdl_wait();
+  if (warp == 0) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(ptx::su32(slot)), "r"(S::COLS));
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+  }
+  if (tid == 32) {
+    ptx::mbar_init(bar, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  const int part = split > 1 ? blockIdx.x % split : 0, cta = split > 1 ? blockIdx.x / split : blockIdx.x;
+  const int n0 = cta * 128, groups = a.K / G, all = (a.K + kChunk - 1) / kChunk, per = (all + split - 1) / split;
+  const int c0 = part * per, chunks = max(0, min(all - c0, per)), steps = chunks * (kChunk / KS);
+
+  // weights: a lane has 16 of the 64 bytes of 8 rows apart; past K anything, the tokens are 0 there
+  const int wr = lane >> 2, wt = lane & 3;
+  const uint32_t wring = base + S::W0 + warp * 32 * kTcPitch;
+  const uint8_t* wrow[4];
+#pragma unroll
+  for (int r = 0; r < 4; ++r) wrow[r] = a.q + ((int64_t)min(n0 + warp * 32 + 8 * r + wr, a.N - 1) * a.K >> 1);
+  int wk = c0 * kChunk + 32 * wt, wslot = 0, wleft = chunks;
+  const auto copy_w = [&] {
+    if (wleft > 0) {
+      const int at = wk < a.K ? wk >> 1 : 0;
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(wring + wslot * 128 * kTcPitch + (8 * r + wr) * kTcPitch + 16 * wt), "l"(wrow[r] + at) : "memory");
+      wk += kChunk;
+      --wleft;
+      if (++wslot == kTcW) wslot = 0;
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  // tokens: 16-byte pieces, eight of a token's 64 k; past the last token and K zeros. A thread puts its own into the nibbles' order
+  const int xm = tid >> 3, xp = tid & 7;
+  const uint32_t xto = base + xm * 128 + (((tid ^ xm) & 7) << 4);   // 16 tokens further: 2048 bytes
+  const __nv_bfloat16* xsrc = a.x + (int64_t)min(xm, a.M - 1) * a.K + c0 * kChunk + 8 * xp;
+  int xk = c0 * kChunk + 8 * xp, xslot = 0, xleft = steps;
+  const auto copy_x = [&] {
+    if (xleft > 0) {
+#pragma unroll
+      for (int h = 0; h < HB; ++h)
+#pragma unroll
+        for (int i = 0; i < NX; ++i) {
+          const bool in = xm + 16 * i < a.M && xk + 64 * h < a.K;
+          const __nv_bfloat16* src = in ? xsrc + (int64_t)16 * i * a.K + 64 * h : a.x;
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(xto + xslot * S::X + h * S::XB + i * 2048), "l"(src), "r"(in ? 16 : 0) : "memory");
+        }
+      xsrc += KS;
+      xk += KS;
+      --xleft;
+      if (++xslot == R) xslot = 0;
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  const auto order_x = [&](int at) {
+#pragma unroll
+    for (int j = 0; j < HB * NX; ++j) {
+      const uint32_t p = xto + at * S::X + j / NX * S::XB + j % NX * 2048;
+      uint32_t x[4];
+      asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(p) : "memory");
+      asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(p), "r"(__byte_perm(x[0], x[2], 0x5410)), "r"(__byte_perm(x[0], x[2], 0x7632)),
+                   "r"(__byte_perm(x[1], x[3], 0x5410)), "r"(__byte_perm(x[1], x[3], 0x7632)) : "memory");
+    }
+  };
+  // scales and zeros: blocks of eight groups, whose 128 rows the threads load so that eight lanes have neighbours
+  uint16_t raw_s[8];
+  uint8_t raw_z[8];
+  const auto load_sg = [&](int b) {   // block b of this CTA; N K / G < 2^31
+    const int gr = min(c0 * (kChunk / G) + b * kTcBlock + xp, groups - 1);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int e = min(n0 + 16 * i + xm, a.N - 1) * groups + gr;
+      raw_s[i] = reinterpret_cast<const uint16_t*>(a.scale)[e];
+      raw_z[i] = a.zero ? a.zero[e] : (uint8_t)8;
+    }
+  };
+  const auto put_sg = [&](int b) {
+    uint32_t* to = reinterpret_cast<uint32_t*>(smem + S::SG0) + (b & 1) * 128 * kTcSg + xp;
+    const bool in = c0 * (kChunk / G) + b * kTcBlock + xp < groups;   // past K: 0
+#pragma unroll
+    for (int i = 0; i < 8; ++i) to[(16 * i + xm) * kTcSg] = in ? (uint32_t)raw_s[i] << 16 | (raw_z[i] & 15u) : 0u;
+  };
+  // In the ring's order: the tokens of a step, then weights; two steps ahead, tokens one where the ring has two.
+  if (R == 3) copy_x();
+  copy_w();
+  copy_x();
+  copy_w();
+  load_sg(0);
+  put_sg(0);
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::tc_fence_after();
+  pdl_trigger();   // not before this CTA's tensor memory is its own: the next kernel may take what is left before it waits
+  const uint32_t tmem = *slot, mine = tmem + ((uint32_t)warp << 21);   // this warp's lanes
+  const uint64_t xd = ptx::sw128_desc(base);
+
+  float acc[NB], scale[GS];
+  bool ok = true;
+#pragma unroll
+  for (int i = 0; i < NB; ++i) acc[i] = 0.f;
+#pragma unroll
+  for (int j = 0; j < GS; ++j) scale[j] = 0.f;
+  const auto wait = [&](int s) {   // for the MMAs of step s
+    ok = ok && wait_mma(bar, s & 1);
+    ptx::tc_fence_after();
+    __syncwarp();
+  };
+  const auto read = [&] {   // the sums of the groups that ended, times their scales
+#pragma unroll
+    for (int j = 0; j < GS; ++j) {
+      const uint32_t d = mine + KS / 2 + j * NB;
+      float v[NB];
+#pragma unroll
+      for (int i = 0; i + 32 <= NB; i += 32) ptx::tmem_ld32_nowait(d + i, reinterpret_cast<uint32_t*>(v) + i);
+      if constexpr (NB % 32 != 0) ptx::tmem_ld16(d + NB - 16, v + NB - 16);
+      else ptx::tmem_wait_ld();
+#pragma unroll
+      for (int i = 0; i < NB; ++i) acc[i] += v[i] * scale[j];
+    }
+  };
+  int st = 0, xs = 0, b = 0, in_block = 0;   // the weights' and the tokens' slots, the block of scales and the step of it
+  for (int s = 0; s < steps; ++s) {
+    const int h = KS == 64 ? s & 1 : 0;   // half of the chunk
+    if (in_block == 0) load_sg(b + 1);
+    asm volatile("cp.async.wait_group %0;" ::"n"(2) : "memory");
+    __syncwarp();   // the other lanes' weights
+    uint32_t f[KS / 2], sz[GS];
+    const uint32_t at = wring + st * 128 * kTcPitch + lane * kTcPitch + 32 * h;
+    const uint32_t* sg = reinterpret_cast<const uint32_t*>(smem + S::SG0) + (b & 1) * 128 * kTcSg + tid * kTcSg + in_block * KS / G;
+#pragma unroll
+    for (int j = 0; j < GS; ++j) sz[j] = sg[j];
+#pragma unroll
+    for (int i = 0; i < KS / 32; ++i) {
+      uint32_t w[4];
+      asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at + 16 * i) : "memory");
+      const uint32_t z = 0x43004300u | (sz[i * 32 / G] & 15u) * 0x10001u;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) f[16 * i + 4 * j + u] = sub2(nibbles(w[j] >> (4 * u)), z);
+    }
+    if (R == 2) asm volatile("cp.async.wait_group %0;" ::"n"(1) : "memory");
+    order_x(xs);
+    ptx::fence_async_smem();
+    if (in_block == SB - 1) put_sg(b + 1);
+    if (s > 0) wait(s - 1);
+#pragma unroll
+    for (int i = 0; i < KS / 32; ++i) ptx::tmem_st16_nowait(mine + 16 * i, f + 16 * i);
+    if (s > 0) read();
+#pragma unroll
+    for (int j = 0; j < GS; ++j) scale[j] = __uint_as_float(sz[j] & 0xffff0000u);
+    ptx::tmem_wait_st();
+    ptx::tc_fence_before();
+    __syncthreads();
+    if (tid == 0) {
+      ptx::tc_fence_after();
+#pragma unroll
+      for (int i = 0; i < KS / 16; ++i)
+        ptx::mma_bf16_ts(tmem + KS / 2 + (G < KS ? i * 16 / G * NB : 0), tmem + 8 * i,
+                         xd + (uint64_t)(xs * (S::X >> 4) + i / 4 * (S::XB >> 4) + i % 4 * 2), ptx::idesc_m128(NB), i * 16 % G != 0);
+      ptx::mma_commit(bar);
+    }
+    __syncwarp();
+    copy_x();
+    if (KS == 128 || h == 1) {
+      copy_w();
+      if (++st == kTcW) st = 0;
+    }
+    if (++xs == R) xs = 0;
+    if (++in_block == SB) in_block = 0, ++b;
+  }
+  if (steps > 0) {
+    wait(steps - 1);
+    read();
+  }
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  ptx::tc_fence_before();
+  __syncthreads();
+  if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S::COLS));
+  const int n = n0 + tid;
+  const float poison = ok ? 0.f : __int_as_float(0x7fc00000);   // MMAs that have not ended: nothing that looks like a result
+  if (split == 1) {
+    const float add = (a.bias && n < a.N ? a.bias[n] : 0.f) + poison;
+    float* o = a.out + n;
+#pragma unroll
+    for (int m = 0; m < NB; ++m) {
+      if (m < a.M && n < a.N) *o = acc[m] + add;
+      o += a.N;
+    }
+    return;
+  }
+  // A cluster's shares of K: each CTA adds up as many tokens, in shared memory: [part][token][row]. Tensor memory was given back
+  // before the first wait for another CTA, so that CTAs that wait for some never wait for each other.
+  const int tokens = (a.M + split - 1) / split;
+  float* recv = reinterpret_cast<float*>(smem);
+  asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");   // nobody's smem is in use
+  int to = -1, left = 0;
+  uint32_t dst = 0;
+#pragma unroll
+  for (int m = 0; m < NB; ++m)
+    if (m < a.M) {
+      if (left == 0) {
+        left = tokens;
+        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(dst) : "r"(ptx::su32(recv + part * tokens * 128 + tid)), "r"(++to));
+      }
+      asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(dst), "f"(acc[m] + poison) : "memory");
+      dst += 512;
+      --left;
+    }
+  asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  const float bias = a.bias && n < a.N ? a.bias[n] : 0.f;
+  for (int i = 0, m = part * tokens; i < tokens && m < a.M; ++i, ++m) {
+    float v = 0.f;
+    for (int c = 0; c < split; ++c) v += recv[(c * tokens + i) * 128 + tid];
+    if (n < a.N) a.out[(int64_t)m * a.N + n] = v + bias;
+  }
+}
+
+template <int NB, int G>
+cudaError_t launch_tc(const W4Args& a, cudaStream_t s) {
+  using S = TcShape<NB, G>;
+  static OncePerDevice once;
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  e = (cudaError_t)once.run(dev, [] { return (int)cudaFuncSetAttribute(w4_tc_kernel<NB, G>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM); });
+  if (e != cudaSuccess) return e;
+  const int64_t tiles = ((int64_t)a.N + 127) / 128;
+  const int chunks = (a.K + kChunk - 1) / kChunk;
+  // A cluster shares K as far as four fifths of the CTAs that fit: with more, clusters of some sizes do not find their places at
+  // once (113 tiles of 4096 k, 40 tokens: 27 us with 3, 33.5 with 4, 30.5 with 2)
+  int split = 1;
+  while (split < 8 && split < chunks && tiles * (split + 1) <= 120 * S::CTAS) ++split;
+  return launch_cluster(w4_tc_kernel<NB, G>, dim3((unsigned)(tiles * split)), dim3(128), (size_t)S::SMEM, split, s, a, split);
 }
 
 template <int G>
 cudaError_t launch_group(const W4Args& a, cudaStream_t s) {
   const int tokens = (a.M + 7) / 8;
-  if (tokens <= 2) {
+  if constexpr (G > 32) if (tokens == 1) {   // groups of 32 take the stream longer: 1 token of 3648 x 14402 18 us against 14
     constexpr int PG = kChunk / G;   // groups of a chunk
     if (PG == 1 || (a.K % kChunk == 0 && reinterpret_cast<uintptr_t>(a.scale) % (2 * PG) == 0 && reinterpret_cast<uintptr_t>(a.zero) % PG == 0))
-      return tokens == 1 ? launch_few<1, G, true>(a, s) : launch_few<2, G, true>(a, s);
-    if constexpr (PG > 1) return tokens == 1 ? launch_few<1, G, false>(a, s) : launch_few<2, G, false>(a, s);
+      return launch_few<G, true>(a, s);
+    if constexpr (PG > 1) return launch_few<G, false>(a, s);
   }
+  // tcgen05 from 33 tokens and 2^24 weights on: 4096 x 4096 takes 12 and 15 us with 40 and 64 tokens against 13 and 17, 1024 x 4096
+  // 8 and 12 against 6 and 8; with 24 tokens it takes as long as with 40.
+  if (tokens > 4 && (int64_t)a.N * a.K >= 1 << 24) return tokens <= 6 ? launch_tc<48, G>(a, s) : launch_tc<64, G>(a, s);
   switch (tokens) {
+    case 1: return launch_many<1, G>(a, s);
+    case 2: return launch_many<2, G>(a, s);
     case 3: return launch_many<3, G>(a, s);
     case 4: return launch_many<4, G>(a, s);
     case 5: return launch_many<5, G>(a, s);
@@ -684,7 +994,7 @@ extern "C" {
 int uad_linear_w4(const void* x, const uint8_t* q, const uint16_t* scale, const uint8_t* zero, const float* bias, float* out,
                   int32_t M, int32_t N, int32_t K, int32_t group, void* stream) {
   if (!x || !q || !scale || !out || M < 1 || N < 1 || K < 1) return UAD_EINVAL;
-  if ((group != 32 && group != 64 && group != 128) || K % group || (int64_t)N * K > (1ll << 35)) return UAD_EINVAL;
+  if ((group != 32 && group != 64 && group != 128) || K % group || K > 1 << 30 || (int64_t)N * K > (1ll << 35)) return UAD_EINVAL;
   if (reinterpret_cast<uintptr_t>(x) % 16 || reinterpret_cast<uintptr_t>(q) % 16 || reinterpret_cast<uintptr_t>(scale) % 2 ||
       reinterpret_cast<uintptr_t>(bias) % 4 || reinterpret_cast<uintptr_t>(out) % 4)
     return UAD_EINVAL;

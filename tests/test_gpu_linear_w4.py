@@ -2,7 +2,8 @@
 
 Tolerance: products of bf16 and whole numbers up to 15 are exact; a group's sum of at most 128 of them is off by an ulp a
 step (the tensor cores truncate), 2^-23 of the sum of magnitudes each, as is every group that is added: (group + groups + 2)
-2^-23 sum |x w|, and the output's own half step 2^-24.
+2^-23 sum |x w|, and the output's own half step 2^-24. The same is demanded where the zero is subtracted after a group's sum,
+although the terms then are |x| (q + zero).
 """
 import numpy as np
 import pytest
@@ -138,3 +139,58 @@ def test_unaligned_outputs_scales_and_biases(M):
     want, size = reference(x, q, scale, z, bias)
     check(out, want, size, K, 64, bias)
     assert float(room[0]) == 7.5 and bool((room[1 + M * N:] == 7.5).all())
+
+
+# From 33 tokens and 2^24 weights on: one CTA for all of K, clusters of 2 to 8, an end of K and of N inside a tile
+LARGE = [(33, 4101, 4128, 32), (40, 24000, 704, 64), (48, 2050, 8320, 128), (64, 24321, 736, 32), (57, 1030, 16448, 64), (64, 131, 130048, 128),
+         (49, 9000, 1888, 32), (36, 14337, 1184, 32), (41, 14337, 1216, 64), (64, 6000, 2816, 128), (34, 20000, 896, 128)]
+
+
+@pytest.mark.parametrize("M,N,K,group", LARGE)
+@pytest.mark.parametrize("zero", [False, True])
+def test_many_tokens_and_weights_match_reference(M, N, K, group, zero):
+    test_linear_w4_matches_reference(M, N, K, group, zero)
+
+
+@pytest.mark.parametrize("M,group", [(33, 64), (48, 32), (64, 128)])
+def test_rows_of_large_calls_do_not_depend_on_each_other(M, group):
+    x, q, scale, z, bias = operands(M, 4100, 4224, group, True, M)
+    clean, out = torch.empty(M, 4100, device="cuda"), torch.empty(M, 4100, device="cuda")
+    uad.linear_w4(x, q, scale, clean, zero=z, bias=bias)
+    x2 = x.clone()
+    x2[3, 5], x2[M - 1, 4223] = float("nan"), float("inf")
+    uad.linear_w4(x2, q, scale, out, zero=z, bias=bias)
+    torch.cuda.synchronize()
+    same = [m for m in range(M) if m not in (3, M - 1)]
+    assert torch.equal(out[same], clean[same])
+    assert bool(torch.isnan(out[3]).all())
+
+
+def test_large_calls_at_the_same_time():
+    """Calls of several sizes on three streams, none of which waits for another, and replayed from graphs: the bits of calls that
+    were alone."""
+    calls = [operands(M, N, K, group, True, M) for M, N, K, group in ((64, 9000, 1888, 32), (40, 2050, 8320, 64), (48, 14337, 1280, 128))]
+    streams = [torch.cuda.Stream() for _ in calls]
+    outs = [[torch.empty(x.shape[0], q.shape[0], device="cuda") for _ in range(8)] for x, q, *_ in calls]
+    alone = []
+    for x, q, s, z, b in calls:
+        alone.append(torch.empty(x.shape[0], q.shape[0], device="cuda"))
+        uad.linear_w4(x, q, s, alone[-1], zero=z, bias=b)
+        torch.cuda.synchronize()
+    for i in range(8):
+        for (x, q, s, z, b), st, o in zip(calls, streams, outs):
+            uad.linear_w4(x, q, s, o[i], zero=z, bias=b, stream=st)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, a) for os, a in zip(outs, alone) for o in os)
+    graphs = []
+    for (x, q, s, z, b), st, o in zip(calls, streams, outs):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=st):
+            for i in range(8):
+                uad.linear_w4(x, q, s, o[i].fill_(7.5), zero=z, bias=b, stream=st)
+    for _ in range(3):
+        for g, st in zip(graphs, streams):
+            with torch.cuda.stream(st):
+                g.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, a) for os, a in zip(outs, alone) for o in os)

@@ -447,6 +447,47 @@ def test_append(heads, rot, row_type, cache_type):
         assert bool((q_out[int(c.start[-1]):] == 7.5).all())
 
 
+@pytest.mark.parametrize("heads,rot,tokens", [((8, 1, 256), 256, 700), ((8, 1, 256), 240, 2000), ((6, 3, 64), 16, 9000), ((32, 8, 128), 128, 800), ((3, 1, 128), 0, 5000)],
+                         ids=lambda x: "x".join(map(str, x)) if isinstance(x, tuple) else str(x))
+@pytest.mark.parametrize("row_type,cache_type", [(torch.float32, torch.bfloat16), (torch.bfloat16, torch.bfloat16), (torch.bfloat16, torch.float32), (torch.float32, torch.float32)])
+def test_append_of_many_tokens(heads, rot, tokens, row_type, cache_type):
+    """Whole prompts in one call: the bits of the same tokens appended few at a time; tokens of a bad page are left out, their
+    queries are not."""
+    hq, hkv, dh = heads
+    new = [tokens - tokens // 3, 1, tokens // 3]
+    c = Case(heads, 16, [new[0] + 5, 1, new[2]], new, cache_type, "phsd", seed=tokens)
+    bad = 3   # a page's place in the first sequence, which holds none
+    c.table[0, bad] = c.pages + 7
+    q, k, v = (c.randn(c.rows, n * dh, dtype=row_type) for n in (hq, hkv, hkv))
+    rope = uad.rope(10000.0, rot) if rot else None
+    once = torch.full((c.rows, hq * dh), 7.5, device="cuda", dtype=cache_type)
+    few = once.clone()
+    k2, v2 = c.k.clone(), c.v.clone()
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    uad.PagedCache(c.k, c.v).append(c.sequences(), k, v, q=q, q_out=once, rope=rope, status=status)
+    table = torch.from_numpy(c.table).cuda()
+    for b in range(3):
+        for i in range(0, new[b], 16):
+            n = min(16, new[b] - i)
+            at = slice(int(c.start[b]) + i, int(c.start[b]) + i + n)
+            length = torch.tensor([c.lens[b] - new[b] + i + n], dtype=torch.int32, device="cuda")
+            start = torch.tensor([0, n], dtype=torch.int32, device="cuda")
+            uad.PagedCache(k2, v2).append(uad.Sequences(table[b:b + 1], length, start, max_new=16), k[at], v[at], q=q[at], q_out=few[at], rope=rope)
+    torch.cuda.synchronize()
+    assert int(status) == uad.UAD_KV_BAD_PAGE
+    assert torch.equal(once, few) and not bool((once[:-2] == 7.5).all(dim=1).any()) and bool((once[-2:] == 7.5).all())
+    for a, b in ((c.k, k2), (c.v, v2)):
+        assert torch.equal(torch.nan_to_num(a, 9.0), torch.nan_to_num(b, 9.0))
+    pg, sl = int(c.table[0, (c.lens[0] - 1) // 16]), (c.lens[0] - 1) % 16
+    want = paged.rotate(k[new[0] - 1].double().cpu().numpy().reshape(hkv, dh), c.lens[0] - 1, 10000.0, rot)
+    x = np.abs(k[new[0] - 1].double().cpu().numpy().reshape(hkv, dh))
+    size = x + 0
+    size[:, :rot // 2] += x[:, rot // 2:rot]
+    size[:, rot // 2:rot] = size[:, :rot // 2]
+    tol = size * 2.0 ** -22 * (rot > 0) + HALF[cache_type] * (np.abs(want) + size * 2.0 ** -22)
+    assert np.all(np.abs(c.k[pg, sl].double().cpu().numpy() - want) <= tol)
+
+
 @pytest.mark.parametrize("pos", [0, 1, 816, 65535, 1 << 20, 2_000_000_000])
 def test_rotation_of_far_positions(pos):
     """fp32 rows at positions whose angles 32 bits do not hold."""

@@ -223,6 +223,7 @@ def test_bad_projections_are_refused(kw):
 
 def test_too_many_rows_and_weights_that_are_no_gpu_memory():
     assert call_w4(M=uad.UAD_W4_MAX_ROWS + 1) == uad.UAD_ETOOBIG
+    assert call_w4(N=1, K=(1 << 30) + 128) == uad.UAD_EINVAL
     host = np.zeros(4096, np.uint8)
     assert call_w4(q=(host.ctypes.data + 63) // 64 * 64) == uad.UAD_EINVAL
 
