@@ -396,6 +396,16 @@ int64_t uad_paged_attention_workspace(const uad_kv_pages* pages, const uad_kv_se
 int uad_paged_attention(const uad_kv_pages* pages, const uad_kv_seqs* seqs, const uad_attn* attn, void* workspace,
                         size_t workspace_bytes, int32_t* status, void* stream);
 
+/* Bind robot `robot`'s prefix from pages: uad_set_prefix_kv of the first arch.prefix_len tokens of a sequence whose keys and
+ * values a vision-language model has appended layer by layer. layers: the caches of the arch's n_layers layers, of one type and
+ * page size, with the arch's n_kv_heads and head_dim (experts of kind DIT take tokens, not keys: UAD_EINVAL), on the context's
+ * device, which has to be the current one. table: host or device, the pages of those tokens (table_len entries, at least as
+ * many), one table for all layers. Synchronous, and behind the legacy default stream; pages or a device table that another stream
+ * writes have to be finished first.
+ * Errors: UAD_EINVAL (also a page outside 0..n_pages-1), UAD_ESTATE (a chunk is in flight), UAD_ENOMEM, UAD_ECUDA. */
+int uad_set_prefix_paged(uad_ctx* ctx, int32_t robot, const uad_kv_pages* layers, int32_t n_layers, const int32_t* table,
+                         int32_t table_len);
+
 /* ---- The projection of few tokens with 4-bit weights ------------------------------------------------------
  * out[M][N] = x[M][K] w^T + bias with w[n][k] = (q[n][k] - zero[n][k / group]) * scale[n][k / group]: for the tokens of a
  * decoding step, whose time is that of reading the weights. x: device bf16; q: device [N][K / 2], k even in the low

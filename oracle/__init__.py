@@ -18,4 +18,5 @@ Modules
   so3.py    rotation vectors and Ghost Action Correction by composition on SO(3) (App. C.1)
   clock.py  action availability latency under the control-time alignment clock
             (Sec. 5.1 Metrics, App. C.3) and the latency model (App. B, Eqs. 11-12)
+  paged.py  the paged key-value cache's rotation and attention and the 4-bit projection's weights, which the paper has not
 """

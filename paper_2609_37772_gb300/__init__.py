@@ -104,6 +104,7 @@ _PAGES, _SEQS = C.POINTER(uad_kv_pages), C.POINTER(uad_kv_seqs)
 uad_kv_append = _fn("uad_kv_append", C.c_int, _PAGES, _SEQS, C.POINTER(uad_kv_rows), C.POINTER(uad_rope), _P, _P)
 uad_paged_attention_workspace = _fn("uad_paged_attention_workspace", C.c_int64, _PAGES, _SEQS, C.POINTER(uad_attn))
 uad_paged_attention = _fn("uad_paged_attention", C.c_int, _PAGES, _SEQS, C.POINTER(uad_attn), _P, C.c_size_t, _P, _P)
+uad_set_prefix_paged = _fn("uad_set_prefix_paged", C.c_int, _P, _I32, _PAGES, _I32, _P, _I32)
 uad_linear_w4 = _fn("uad_linear_w4", C.c_int, _P, _P, _P, _P, _P, _P, _I32, _I32, _I32, _I32, _P)
 uad_quantize_w4 = _fn("uad_quantize_w4", C.c_int, _P, _I32, _I32, _I32, _P, _P, _P)
 # The same entries for the wrappers below, with structures as addresses or packed bytes: a decoding step makes several such
@@ -124,7 +125,7 @@ EXPORTS = ["uad_version", "uad_last_error", "uad_init", "uad_set_prefix_kv", "ua
            "uad_launches_per_chunk", "uad_destroy", "uad_plan_step", "uad_profile_chunk",
            "uad_tile_weight", "uad_linear", "uad_linear_static_scratch", "uad_set_wait_limit",
            "uad_linear_status", "uad_linear_check", "uad_so3_check", "uad_rope_init", "uad_kv_append",
-           "uad_paged_attention_workspace", "uad_paged_attention", "uad_linear_w4", "uad_quantize_w4"]
+           "uad_paged_attention_workspace", "uad_paged_attention", "uad_set_prefix_paged", "uad_linear_w4", "uad_quantize_w4"]
 
 
 def tile_weight(w):
@@ -445,6 +446,17 @@ class Expert:
         return self._check(uad_set_prefix_kv(self.h, robot, _buf(k, n, el, "prefix k"),
                                              _buf(v, n, el, "prefix v"), a.prefix_len, code),
                            "set_prefix")
+
+    def set_prefix_paged(self, robot, caches, table):
+        """set_prefix from pages: the first arch.prefix_len tokens of a sequence. caches: a PagedCache for each layer; table: int32
+        [pages], a tensor or array on the host or the GPU, one for all layers. Synchronous and behind the legacy default stream: what
+        other streams write has to be finished first."""
+        t = np.ascontiguousarray(table, np.int32) if isinstance(table, (list, tuple)) else table
+        if len(t.shape) != 1:
+            raise ValueError(f"table: expected the pages of one sequence, got shape {list(t.shape)}")
+        layers = (uad_kv_pages * len(caches))(*[c.pages for c in caches])
+        return self._check(uad_set_prefix_paged(self.h, robot, layers, len(caches), _buf(t, t.shape[0], "int32", "table"), t.shape[0]),
+                           "set_prefix_paged")
 
     def prepare_times(self, max_budget):
         return self._check(uad_prepare_times(self.h, max_budget), "prepare_times")

@@ -136,6 +136,21 @@ __global__ void __launch_bounds__(256, 4) append_kernel(const AppendArgs a, cons
   }
 }
 
+// One block a token: a copy in 16-byte pieces, keys and values in turn.
+__global__ void __launch_bounds__(256) gather_kernel(const PagedArgs p, const int* table, char* k, char* v) {
+  pdl_wait();
+  pdl_trigger();
+  const int es = p.dtype == F32 ? 4 : 2, per_head = p.dh * es / 16, all = p.n_kv * per_head;
+  const int64_t at = token_at(p, table, blockIdx.x);
+  if (at < 0) return;
+  for (int i = threadIdx.x; i < 2 * all; i += blockDim.x) {
+    const bool is_v = i >= all;
+    const int r = is_v ? i - all : i, h = r / per_head;
+    const char* from = static_cast<const char*>(is_v ? p.v : p.k) + (at + h * p.head_stride) * es + (r - h * per_head) * 16;
+    *reinterpret_cast<uint4*>((is_v ? v : k) + ((int64_t)blockIdx.x * all + r) * 16) = *reinterpret_cast<const uint4*>(from);
+  }
+}
+
 bool bad_address(const void* p, int64_t stride, int es) {
   return reinterpret_cast<uintptr_t>(p) % 16 != 0 || stride < 0 || (stride * es) % 16 != 0;
 }
@@ -150,6 +165,10 @@ bool uad::on_current_device(const void* p) {
     return false;
   }
   return (at.type == cudaMemoryTypeDevice && at.device == dev) || at.type == cudaMemoryTypeManaged;
+}
+
+cudaError_t uad::launch_kv_gather(const PagedArgs& p, const int* table, int n, void* k, void* v, cudaStream_t s) {
+  return launch_k(gather_kernel, dim3((unsigned)n), 256, 0, s, p, table, static_cast<char*>(k), static_cast<char*>(v));
 }
 
 int uad::paged_args(const uad_kv_pages* g, const uad_kv_seqs* s, int n_rows, bool device, PagedArgs* p) {

@@ -45,6 +45,9 @@ __device__ __forceinline__ int64_t token_at(const PagedArgs& p, const int* row, 
 // kv_pages.cu: the checks of the structures; UAD_OK with the kernels' arguments, or UAD_EINVAL. device: also that the
 // pages are memory of the current device (tables and lengths may be null otherwise).
 int paged_args(const uad_kv_pages* pages, const uad_kv_seqs* seqs, int n_rows, bool device, PagedArgs* out);
+// Tokens 0 .. n - 1 of a sequence, whose pages are table[0 ..] (device memory, checked), next to each other: k, v [n][n_kv][dh] of the
+// pages' type, 16-byte aligned.
+cudaError_t launch_kv_gather(const PagedArgs& p, const int* table, int n, void* k, void* v, cudaStream_t s);
 // Whether p is memory of the current device.
 bool on_current_device(const void* p);
 

@@ -228,6 +228,10 @@ def test_too_many_rows_and_weights_that_are_no_gpu_memory():
     assert call_w4(q=(host.ctypes.data + 63) // 64 * 64) == uad.UAD_EINVAL
 
 
+def test_prefix_from_pages_needs_a_context():
+    assert uad.uad_set_prefix_paged(None, 0, (uad.uad_kv_pages * 1)(), 1, None, 0) == uad.UAD_EINVAL
+
+
 # ---- the binding stops malformed tensors before the call ----------------------------------------------------------------------
 
 
