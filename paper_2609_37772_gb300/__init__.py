@@ -392,16 +392,20 @@ def linear_w4(x, q, scale, out, zero=None, bias=None, stream=None):
     128, M up to UAD_W4_MAX_ROWS. Asynchronous on `stream` (None: the legacy default stream)."""
     M, K = x.shape if x.dim() == 2 else (0, 0)
     N, groups = scale.shape if scale.dim() == 2 else (0, 0)
-    xp = _tensor(x, "x", "bfloat16", (M, K))
-    d = x.get_device()
-    qp = _tensor(q, "q", "uint8", (N, K // 2), d)
-    sp = _tensor(scale, "scale", "bfloat16", (N, groups), d)
+    d, half, byte, full = x.get_device(), _dtypes.get("bfloat16"), _dtypes.get("uint8"), _dtypes.get("float32")
+    # all checks at once, which takes half of what one by one does; where one fails, they say which
+    if not (x.dtype is half and scale.dtype is half and q.dtype is byte and out.dtype is full and q.shape == (N, K // 2) and out.shape == (M, N) and
+            x.is_contiguous() and scale.is_contiguous() and q.is_contiguous() and out.is_contiguous() and
+            d >= 0 and d == scale.get_device() == q.get_device() == out.get_device()):
+        _tensor(x, "x", "bfloat16", (M, K))
+        _tensor(q, "q", "uint8", (N, K // 2), d)
+        _tensor(scale, "scale", "bfloat16", (N, groups), d)
+        _tensor(out, "out", "float32", (M, N), d)
     zp = None if zero is None else _tensor(zero, "zero", "uint8", (N, groups), d)
     bp = None if bias is None else _tensor(bias, "bias", "float32", (N,), d)
-    op = _tensor(out, "out", "float32", (M, N), d)
     if groups < 1 or K % groups:
         raise ValueError(f"scale: {groups} groups do not divide {K} columns")
-    rc = _w4(xp, qp, sp, zp, bp, op, M, N, K, K // groups, _stream_handle(stream))
+    rc = _w4(x.data_ptr(), q.data_ptr(), scale.data_ptr(), zp, bp, out.data_ptr(), M, N, K, K // groups, _stream_handle(stream))
     if rc:
         raise UADError(rc, "linear_w4: group must be 32, 64 or 128, x and q 16-byte aligned and on the current device, at most "
                        f"{UAD_W4_MAX_ROWS} rows")
