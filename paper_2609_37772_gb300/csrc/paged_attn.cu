@@ -515,21 +515,29 @@ __global__ void __launch_bounds__(kThreads, tc_ctas<DH, NR>()) paged_attn_tc_ker
       }
       odd = __any_sync(0xffffffffu, !(__low2float(any) == 0.f && __high2float(any) == 0.f));
     }
+    // the products of several dims, then those of the rest: a product that adds to the one before waits for it
+    constexpr int XS = NR == 1 ? 4 : NR == 2 ? 2 : 1;
 #pragma unroll
-    for (int x = 0; x < STEPS; ++x)
+    for (int x = 0; x < STEPS; x += XS)
 #pragma unroll
       for (int u = 0; u < KT; ++u) {
-        uint32_t v[4];
-        ldm4t(v, vs + u * 16 * PITCH + x * 32);
-        if (odd) {
+        uint32_t v[XS][4];
 #pragma unroll
-          for (int j = 0; j < 4; ++j) v[j] &= ~nonfinite2(v[j]);
+        for (int y = 0; y < XS; ++y) {
+          ldm4t(v[y], vs + u * 16 * PITCH + (x + y) * 32);
+          if (odd) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[y][j] &= ~nonfinite2(v[y][j]);
+          }
         }
 #pragma unroll
-        for (int n = 0; n < NR; ++n) {
-          mma16816(o[x][n], v, hi[n][2 * u], hi[n][2 * u + 1]);
-          mma16816(o[x][n], v, lo[n][2 * u], lo[n][2 * u + 1]);
-        }
+        for (int y = 0; y < XS; ++y)
+#pragma unroll
+          for (int n = 0; n < NR; ++n) mma16816(o[x + y][n], v[y], hi[n][2 * u], hi[n][2 * u + 1]);
+#pragma unroll
+        for (int y = 0; y < XS; ++y)
+#pragma unroll
+          for (int n = 0; n < NR; ++n) mma16816(o[x + y][n], v[y], lo[n][2 * u], lo[n][2 * u + 1]);
       }
     if (odd) {
 #pragma unroll
