@@ -653,7 +653,8 @@ cudaError_t launch_many(const W4Args& a, cudaStream_t s) {
   e = (cudaError_t)once.run(dev, [&] { return (int)cudaFuncSetAttribute(w4_many_kernel<NT, G>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024); });
   if (e != cudaSuccess) return e;
   // The rows a CTA that leave the fullest SM the fewest, the more the better; with SMs left over, a cluster shares K as far as
-  // every warp keeps a chunk.
+  // every warp keeps a chunk, and up to 16 tokens, four chunks, two CTAs an SM (5 tokens of 8192 x 2048 in groups of 32 7.1 us
+  // against 8.7, of 2048 x 2560 4.7 against 4.1; 24 of 4096 x 4096 12.9 against 10.0).
   int wn = 1, split = 1;
   const int64_t sets = ((int64_t)a.N + 31) / 32;
   int64_t best = INT64_MAX;
@@ -663,11 +664,15 @@ cudaError_t launch_many(const W4Args& a, cudaStream_t s) {
   }
   const int64_t ctas = ((int64_t)a.N + 32 * wn - 1) / (32 * wn);
   const int chunks = (a.K + kChunk - 1) / kChunk;
-  while (wn == 1 && split < 8 && ctas * split * 2 <= kSms && chunks > 4 * split) split *= 2;
+  const auto more = [&] {
+    const int64_t n = ctas * split * 2;
+    return (n <= kSms && chunks > 4 * split) || (NT <= 2 && n <= 2 * kSms && chunks >= 32 * split);
+  };
+  while (wn == 1 && split < 8 && more()) split *= 2;
   // A CTA that is alone on its SM copies up to three chunks ahead; else the next CTA's work hides the copies, and smaller ones let
   // more of them in (24 tokens: 14336 x 4096 21 us against 28, but 2048 x 32768 40 against 22).
   int stages = ctas * split <= kSms ? 4 : 2;
-  while (stages > 2 && many_smem<NT>(wn, stages) > 227 * 1024) --stages;
+  while (stages > 2 && many_smem<NT>(wn, stages) > (split == 8 ? 112 : 227) * 1024) --stages;   // clusters of 8 need two CTAs an SM to find their places
   return launch_cluster(w4_many_kernel<NT, G>, dim3((unsigned)(ctas * split)), dim3(128 * wn), many_smem<NT>(wn, stages), split, s, a, wn, split, stages);
 }
 
