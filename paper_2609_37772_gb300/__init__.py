@@ -209,6 +209,7 @@ def plan_step(budgets, k, tr=True):
     return ns, f, tn, td
 
 
+_row_types = {}   # 0 or 1 by the type of a row tensor, once seen
 _dtypes = {}   # torch's types by name, once a tensor has been seen: the binding itself does not import torch
 
 
@@ -315,23 +316,45 @@ class PagedCache:
         """Write the new tokens' keys and values [rows][n_kv_heads * head_dim] into their pages and their queries
         [rows][n_heads * head_dim] into q_out, keys and queries rotated by `rope` (None: not). float32 or bfloat16 rows,
         which may be parts of a fused projection; q_out in the cache's type."""
-        first = q if k is None else k
-        if first is None or (k is None) != (v is None) or (q is None) != (q_out is None):
-            raise ValueError("append: k goes with v, q with q_out, and one of the two is needed")
-        if seqs._gpu != self._gpu:
+        g = self._gpu
+        if seqs._gpu != g:
             raise ValueError(f"sequences: must be on {self.device}, are on {seqs.device}")
-        kind, n, width = first.dtype, first.shape[0] if first.dim() else 0, self.n_kv_heads * self.head_dim
-        code = 0 if (name := str(kind)) == "torch.float32" else 1
-        if code and name != "torch.bfloat16":
-            raise ValueError(f"append: expected float32 or bfloat16 rows, got {kind}")
         kp = vp = qp = op = kl = vl = ql = ol = heads = 0
+        if k is not None and v is not None:
+            kind, shape = k.dtype, k.shape
+        elif q is not None and k is v:
+            kind, shape = q.dtype, q.shape
+        else:
+            raise ValueError("append: k goes with v, q with q_out, and one of the two is needed")
+        if (q is None) != (q_out is None):
+            raise ValueError("append: k goes with v, q with q_out, and one of the two is needed")
+        n = shape[0] if len(shape) else 0
+        code = _row_types.get(kind)
+        if code is None:
+            if str(kind) not in ("torch.float32", "torch.bfloat16"):
+                raise ValueError(f"append: expected float32 or bfloat16 rows, got {kind}")
+            code = _row_types[kind] = int(str(kind) == "torch.bfloat16")
+        # the usual rows checked at once; where a check fails, _rows says which or finds them sound
         if k is not None:
-            kp, kl = self._rows(k, "k", kind, n, width)
-            vp, vl = self._rows(v, "v", kind, n, width)
+            width = self.n_kv_heads * self.head_dim
+            (kl, one), (vl, uno) = (k.stride(), v.stride()) if len(shape) == 2 == v.dim() else ((0, 0), (0, 0))
+            if (v.dtype is kind and shape == (n, width) == v.shape and one == 1 == uno and kl >= width <= vl and
+                    k.get_device() == g == v.get_device()):
+                kp, vp = k.data_ptr(), v.data_ptr()
+            else:
+                kp, kl = self._rows(k, "k", kind, n, width)
+                vp, vl = self._rows(v, "v", kind, n, width)
         if q is not None:
-            heads = self._heads(q)
-            qp, ql = self._rows(q, "q", kind, n, q.shape[1])
-            op, ol = self._rows(q_out, "q_out", self.dtype, n, q.shape[1])
+            wide = q.shape
+            heads = wide[1] // self.head_dim if len(wide) == 2 else 0
+            (ql, one), (ol, uno) = (q.stride(), q_out.stride()) if len(wide) == 2 == q_out.dim() else ((0, 0), (0, 0))
+            if (q.dtype is kind and q_out.dtype is self.dtype and wide == (n, heads * self.head_dim) == q_out.shape and one == 1 == uno and
+                    ql >= wide[1] <= ol and q.get_device() == g == q_out.get_device()):
+                qp, op = q.data_ptr(), q_out.data_ptr()
+            else:
+                heads = self._heads(q)
+                qp, ql = self._rows(q, "q", kind, n, wide[1])
+                op, ol = self._rows(q_out, "q_out", self.dtype, n, wide[1])
         rc = _append(self._at, seqs._at, _pack_rows(qp, kp, vp, ql, kl, vl, op, ol, code, heads, n, 0),
                      None if rope is None else C.addressof(rope), self._status(status), _stream_handle(stream))
         if rc:
