@@ -374,21 +374,38 @@ class PagedCache:
         uint8 [sequences][tokens that the table holds]: only where it is not 0. Where a token sees nothing, out is 0 and lse
         (float32 [rows][n_heads]) -inf. workspace: a uint8 tensor of attention_workspace bytes, not shared by calls that may
         run at the same time."""
-        if seqs._gpu != self._gpu:
+        g = self._gpu
+        if seqs._gpu != g:
             raise ValueError(f"sequences: must be on {self.device}, are on {seqs.device}")
-        heads, n = self._heads(q), q.shape[0]
-        qp, ql = self._rows(q, "q", self.dtype, n, q.shape[1])
-        op, ol = self._rows(out, "out", self.dtype, n, q.shape[1])
         lp = mp = ml = wn = 0
         wp = None
+        # the usual rows checked at once; where a check fails, _rows says which or finds them sound
+        wide = q.shape
+        heads = wide[1] // self.head_dim if len(wide) == 2 else 0
+        n = wide[0] if len(wide) else 0
+        (ql, one), (ol, uno) = (q.stride(), out.stride()) if len(wide) == 2 == out.dim() else ((0, 0), (0, 0))
+        if (q.dtype is self.dtype is out.dtype and wide == (n, heads * self.head_dim) == out.shape and one == 1 == uno and ql >= wide[1] <= ol and
+                q.get_device() == g == out.get_device()):
+            qp, op = q.data_ptr(), out.data_ptr()
+        else:
+            heads = self._heads(q)
+            qp, ql = self._rows(q, "q", self.dtype, n, wide[1])
+            op, ol = self._rows(out, "out", self.dtype, n, wide[1])
         if lse is not None:
-            lp = _tensor(lse, "lse", "float32", (n, heads), self._gpu)
+            if lse.dtype is _dtypes.get("float32") and lse.shape == (n, heads) and lse.is_contiguous() and lse.get_device() == g:
+                lp = lse.data_ptr()
+            else:
+                lp = _tensor(lse, "lse", "float32", (n, heads), g)
         if key_mask is not None:
             mp, ml = _tensor(key_mask, "key_mask", "uint8", (seqs.n, None), self._gpu, True), key_mask.stride(0)
             if key_mask.shape[1] < seqs.seqs.table_width * self.page_size:
                 raise ValueError(f"key_mask: expected {seqs.seqs.table_width * self.page_size} columns, what the table holds")
         if workspace is not None:
-            wp, wn = _tensor(workspace, "workspace", "uint8", (None,), self._gpu), workspace.numel()
+            wn = workspace.numel()
+            if workspace.dtype is _dtypes.get("uint8") and workspace.dim() == 1 and workspace.is_contiguous() and workspace.get_device() == g:
+                wp = workspace.data_ptr()
+            else:
+                wp = _tensor(workspace, "workspace", "uint8", (None,), g)
         rc = _attention(self._at, seqs._at, _pack_attn(qp, op, lp, mp, ql, ol, ml, scale or 0.0, heads, n, 1 if causal else 0, window, 0),
                         wp, wn, self._status(status), _stream_handle(stream))
         if rc:
@@ -424,8 +441,15 @@ def linear_w4(x, q, scale, out, zero=None, bias=None, stream=None):
         _tensor(q, "q", "uint8", (N, K // 2), d)
         _tensor(scale, "scale", "bfloat16", (N, groups), d)
         _tensor(out, "out", "float32", (M, N), d)
-    zp = None if zero is None else _tensor(zero, "zero", "uint8", (N, groups), d)
-    bp = None if bias is None else _tensor(bias, "bias", "float32", (N,), d)
+    zp = bp = None
+    if zero is not None:
+        if not (zero.dtype is byte and zero.shape == scale.shape and zero.is_contiguous() and zero.get_device() == d):
+            _tensor(zero, "zero", "uint8", (N, groups), d)
+        zp = zero.data_ptr()
+    if bias is not None:
+        if not (bias.dtype is full and bias.shape == (N,) and bias.is_contiguous() and bias.get_device() == d):
+            _tensor(bias, "bias", "float32", (N,), d)
+        bp = bias.data_ptr()
     if groups < 1 or K % groups:
         raise ValueError(f"scale: {groups} groups do not divide {K} columns")
     rc = _w4(x.data_ptr(), q.data_ptr(), scale.data_ptr(), zp, bp, out.data_ptr(), M, N, K, K // groups, _stream_handle(stream))
