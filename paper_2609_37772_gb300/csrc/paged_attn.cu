@@ -837,20 +837,23 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attn_f32_kernel(const Paged
 
 // ---- joining pieces ---------------------------------------------------------------------------------------------------
 
-// One CTA a row and head: groups of DH / 4 threads take the pieces in turn.
+// One CTA a row and head: groups of DH / 4 threads take the pieces in turn, 128 pieces at a time, whose weights the threads have
+// worked out before, so that the values are requested together.
 template <int T, int DH>
 __global__ void __launch_bounds__(kThreads) paged_join_kernel(const PagedAttnArgs a) {
   constexpr int TH = DH / 4, GR = kThreads / TH;
   __shared__ float4 so[GR][TH];
-  __shared__ float sm[kWarps], sl[GR];
+  __shared__ float sm[kWarps], sl[kWarps], sw[kThreads];
   pdl_wait();
   pdl_trigger();
   const SeqRows s = seq_rows(a.p, blockIdx.z);
   const int j = blockIdx.x / a.n_heads, h = blockIdx.x % a.n_heads;
   if (j >= s.n) return;
   const int64_t t = s.first + j, at = (t * a.n_heads + h) * a.pieces;
-  float top = -INFINITY;
-  for (int i = threadIdx.x; i < a.pieces; i += kThreads) top = fmaxf(top, a.part_ml[at + i].x);
+  const float2 none = make_float2(-INFINITY, 0.f);
+  float2 ml = threadIdx.x < a.pieces ? a.part_ml[at + threadIdx.x] : none;
+  float top = ml.x;
+  for (int i = threadIdx.x + kThreads; i < a.pieces; i += kThreads) top = fmaxf(top, a.part_ml[at + i].x);
   top = warp_max(top);
   if ((threadIdx.x & 31) == 0) sm[threadIdx.x >> 5] = top;
   __syncthreads();
@@ -858,24 +861,33 @@ __global__ void __launch_bounds__(kThreads) paged_join_kernel(const PagedAttnArg
   const int gr = threadIdx.x / TH, d = threadIdx.x % TH;
   float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
   float sum = 0.f;
-#pragma unroll 4
-  for (int i = gr; i < a.pieces; i += GR) {
-    const float2 ml = a.part_ml[at + i];
-    if (ml.y == 0.f) continue;   // nothing was seen there, and no values written
-    const float4 y = *reinterpret_cast<const float4*>(a.part_o + (at + i) * DH + 4 * d);
-    const float f = weight(ml.x, top);
-    x.x += y.x * f; x.y += y.y * f; x.z += y.z * f; x.w += y.w * f;
-    sum += ml.y * f;
+  for (int base = 0; base < a.pieces; base += kThreads) {
+    if (base > 0) {
+      ml = base + (int)threadIdx.x < a.pieces ? a.part_ml[at + base + threadIdx.x] : none;
+      __syncthreads();   // the weights before these have been read
+    }
+    const float w = ml.y == 0.f ? -1.f : weight(ml.x, top);   // -1: nothing was seen there, and no values written
+    if (ml.y != 0.f) sum += ml.y * w;
+    sw[threadIdx.x] = w;
+    __syncthreads();
+    const int n = min(kThreads, a.pieces - base);
+#pragma unroll 8
+    for (int i = gr; i < n; i += GR) {
+      const float f = sw[i];
+      if (f == -1.f) continue;
+      const float4 y = *reinterpret_cast<const float4*>(a.part_o + (at + base + i) * DH + 4 * d);
+      x.x += y.x * f; x.y += y.y * f; x.z += y.z * f; x.w += y.w * f;
+    }
   }
   so[gr][d] = x;
-  if (d == 0) sl[gr] = sum;
+  sum = warp_sum(sum);
+  if ((threadIdx.x & 31) == 0) sl[threadIdx.x >> 5] = sum;
   __syncthreads();
   if (gr) return;
-  sum = sl[0];
+  sum = (sl[0] + sl[1]) + (sl[2] + sl[3]);
   for (int i = 1; i < GR; ++i) {
     const float4 y = so[i][d];
     x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
-    sum += sl[i];
   }
   const float f = row_factor(top, sum);
   x = make_float4(x.x * f, x.y * f, x.z * f, x.w * f);
