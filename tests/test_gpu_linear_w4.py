@@ -194,3 +194,55 @@ def test_large_calls_at_the_same_time():
                 g.replay()
     torch.cuda.synchronize()
     assert all(torch.equal(o, a) for os, a in zip(outs, alone) for o in os)
+
+
+def test_large_calls_among_the_other_projections():
+    """Alternating with uad_linear, which also takes tensor memory and may start before the call in front of it has ended: in one
+    stream's order, on two streams at once, and in graphs."""
+    M, N, K = 48, 6144, 4096
+    calls = [operands(M, N, K, 64, True, 11), operands(40, 14337, 2048, 128, True, 12)]
+    g = torch.Generator(device="cuda")
+    g.manual_seed(13)
+    lin = []
+    for m, n, k in ((637, 1024, 2048), (50, 1024, 4096), (16, 4608, 1536), (3000, 1024, 128)):
+        w = torch.randn((k, n), generator=g, device="cuda").mul_(0.02).cpu().numpy()
+        lin.append((torch.randn((m, k), generator=g, device="cuda").bfloat16(), torch.from_numpy(uad.tile_weight(w).view(np.int16)).cuda(), m, n, k))
+
+    def chain(stream):
+        outs = []
+        for i in range(8):
+            x, q, s, z, b = calls[i % 2]
+            outs.append(torch.empty(x.shape[0], q.shape[0], device="cuda"))
+            uad.linear_w4(x, q, s, outs[-1], zero=z, bias=b, stream=stream)
+            x, w, m, n, k = lin[i % 4]
+            outs.append(torch.empty(m, n, device="cuda"))
+            assert uad.uad_linear(x.data_ptr(), w.data_ptr(), None, outs[-1].data_ptr(), m, n, k, stream.cuda_stream) == 0
+        return outs
+
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    with torch.cuda.stream(streams[0]):
+        alone = chain(streams[0])
+    torch.cuda.synchronize()
+    for i in range(2):
+        want, size = reference(*calls[i])
+        check(alone[2 * i], want, size, calls[i][0].shape[1], (64, 128)[i], calls[i][4])
+    got = []
+    for st in streams:
+        with torch.cuda.stream(st):
+            got += [chain(st), chain(st)]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=streams[0]):
+        got.append(chain(streams[0]))
+    with torch.cuda.stream(streams[1]):
+        got.append(chain(streams[1]))
+    with torch.cuda.stream(streams[0]):
+        for _ in range(3):
+            graph.replay()
+    torch.cuda.synchronize()
+    for outs in got:
+        for i, (o, a) in enumerate(zip(outs, alone)):
+            if i % 2:   # uad_linear's own tolerance
+                assert float((o - a).abs().max()) <= 1e-5 * float(a.abs().max())
+            else:
+                assert torch.equal(o, a)
