@@ -837,11 +837,12 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attn_f32_kernel(const Paged
 
 // ---- joining pieces ---------------------------------------------------------------------------------------------------
 
-// One CTA a row and head: groups of DH / 4 threads take the pieces in turn, 128 pieces at a time, whose weights the threads have
-// worked out before, so that the values are requested together.
+// One CTA 64 dims of a row and head: groups of 16 threads take the pieces in turn, 128 pieces at a time, whose weights the threads
+// have worked out before, so that the values are requested together (a CTA a row: 60 us against 40 for 8 heads of 256 over
+// 131071 keys, whose 304 pieces eight CTAs read).
 template <int T, int DH>
 __global__ void __launch_bounds__(kThreads) paged_join_kernel(const PagedAttnArgs a) {
-  constexpr int TH = DH / 4, GR = kThreads / TH;
+  constexpr int TH = 16, GR = kThreads / TH;
   __shared__ float4 so[GR][TH];
   __shared__ float sm[kWarps], sl[kWarps], sw[kThreads];
   pdl_wait();
@@ -875,7 +876,7 @@ __global__ void __launch_bounds__(kThreads) paged_join_kernel(const PagedAttnArg
     for (int i = gr; i < n; i += GR) {
       const float f = sw[i];
       if (f == -1.f) continue;
-      const float4 y = *reinterpret_cast<const float4*>(a.part_o + (at + base + i) * DH + 4 * d);
+      const float4 y = *reinterpret_cast<const float4*>(a.part_o + (at + base + i) * DH + 64 * blockIdx.y + 4 * d);
       x.x += y.x * f; x.y += y.y * f; x.z += y.z * f; x.w += y.w * f;
     }
   }
@@ -891,10 +892,10 @@ __global__ void __launch_bounds__(kThreads) paged_join_kernel(const PagedAttnArg
   }
   const float f = row_factor(top, sum);
   x = make_float4(x.x * f, x.y * f, x.z * f, x.w * f);
-  const int64_t e = t * a.out_stride + (int64_t)h * DH + 4 * d;
+  const int64_t e = t * a.out_stride + (int64_t)h * DH + 64 * blockIdx.y + 4 * d;
   if constexpr (T == F32) *reinterpret_cast<float4*>(static_cast<float*>(a.out) + e) = x;
   else *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.out) + e) = make_uint2(pack_bf16(x.x, x.y), pack_bf16(x.z, x.w));
-  if (a.lse && d == 0) a.lse[t * a.n_heads + h] = row_lse(top, sum);
+  if (a.lse && d == 0 && blockIdx.y == 0) a.lse[t * a.n_heads + h] = row_lse(top, sum);
 }
 
 // How many rows a CTA takes and how the keys are cut, from sizes alone (the workspace of a captured call holds for what its
@@ -902,13 +903,16 @@ __global__ void __launch_bounds__(kThreads) paged_join_kernel(const PagedAttnArg
 // (`slots`), and pieces are not shorter than 256 keys (fp32: 64) but where everything is one small wave. A cluster
 // joins its pieces in 1 us, the workspace and a second kernel take 3; but clusters are placed as a whole, which leaves
 // SMs idle once there are many of them or they are large. Long pieces are cut further, up to four waves, so that
-// sequences of different lengths even out. In us, pieces with / without a cluster:
+// sequences of different lengths even out; but a wave that is barely more than one costs like two. In us, pieces with / without a
+// cluster:
 //   1 x 817 keys, 8 heads over 1 of 256:   13: 7.1 / 9.1,  7: 8.3 / 9.6
 //   64 x 282..1129, the same:               4: 16.3 / 18.4,  8: 23.3 / 17.1
 //   6 x 2001..8003, 5 new tokens:          12: 31.8 / 32.8,  16: 48.1 / 27.5
 //   2 x 32768, 131071, 32 over 8 of 128:   28: - / 130,  80: - / 117
-// With more heads than the SMs hold CTAs, a CTA's warps take a head each and need no joining (24 heads of 64: 51 x 5 keys 9.6 ->
-// 5.0, 64 x 60 keys 11.3 -> 7.6, 64 x 300 keys 26.5 -> 24.4; 2 x 6492 keys, fewer heads than that, 16.0 -> 27.9).
+//   16 x 4000, 32 over 8 of 128:            3: - / 50,  4: - / 57
+//   16 x 700, 8 new tokens, 24 of 64:       1: 16.5,  2: - / 22.6
+// With more heads than the SMs hold CTAs and few keys, a CTA's warps take a head each and need no joining (24 heads of 64: 51 x 5
+// keys 9.6 -> 5.0, 64 x 60 keys 13.2 -> 8.5, 64 x 300 keys 26.7 -> 25.4; but 64 x up to 2000 keys 86 -> 106).
 void attn_plan(const uad_kv_seqs* s, int ctas_per_sm, PagedAttnArgs* a) {
   int64_t keys = s->max_len > 0 && s->max_len < a->p.capacity ? s->max_len : a->p.capacity;
   if (a->window > 0 && a->window + (int64_t)a->p.max_new - 1 < keys) keys = a->window + (int64_t)a->p.max_new - 1;
@@ -916,17 +920,18 @@ void attn_plan(const uad_kv_seqs* s, int ctas_per_sm, PagedAttnArgs* a) {
   constexpr int sms = 152;
   const int64_t units = (int64_t)a->p.n_seqs * a->p.n_kv * a->row_blocks, slots = sms * ctas_per_sm;
   const int64_t least = a->p.dtype == F32 ? 64 : 256;
-  a->warp_heads = a->p.dtype == BF16 && a->p.n_kv % kWarps == 0 && units >= slots;
+  a->warp_heads = a->p.dtype == BF16 && a->p.n_kv % kWarps == 0 && units >= slots && keys <= 512;
   const auto most = [&](int64_t n) { return (keys + n - 1) / n; };   // pieces of at least n keys
   int64_t n;
   if (keys <= kMaxCluster * 256 && units * (most(64) < kMaxCluster ? most(64) : kMaxCluster) <= sms) {
     n = most(64) < kMaxCluster ? most(64) : kMaxCluster;
   } else {
-    n = units * 5 >= slots * 4 ? 1 : units * 2 > slots ? 2 : slots / units;
+    n = units * 5 >= slots * 3 ? 1 : units * 2 > slots ? 2 : slots / units;
     if (n > 1 && n <= 8 && units * n * 20 > slots * 17) n = slots * 17 / (units * 20) > 1 ? slots * 17 / (units * 20) : n;
     if (n > most(least)) n = most(least);
     const int64_t waves = 4 * slots / units < most(1024) ? 4 * slots / units : most(1024);
     if (waves > n) n = waves;
+    if (n > 2 && units * n > slots && units * n * 2 < slots * 3) n = slots / units > 1 ? slots / units : n;
   }
   const int64_t piece = ((keys + n - 1) / n + 63) / 64 * 64;
   a->piece_keys = (int)(piece < (1ll << 30) ? piece : 1ll << 30);
@@ -1009,7 +1014,7 @@ cudaError_t launch_dh(const PagedAttnArgs& a, cudaStream_t s) {
     else e = cudaErrorInvalidValue;
   }
   if (e != cudaSuccess || a.pieces == 1 || a.clustered) return e;
-  const dim3 grid((unsigned)a.n_heads * a.p.max_new, 1, a.p.n_seqs);
+  const dim3 grid((unsigned)a.n_heads * a.p.max_new, DH / 64, a.p.n_seqs);
   return a.p.dtype == F32 ? launch_k(paged_join_kernel<F32, DH>, grid, kThreads, 0, s, a) : launch_k(paged_join_kernel<BF16, DH>, grid, kThreads, 0, s, a);
 }
 
