@@ -25,7 +25,7 @@ struct PagedAttnArgs {
   // how the work is split (attn_plan)
   int row_tiles;    // query rows of a CTA, in eights
   int row_blocks, pieces, piece_keys;
-  int warp_heads;   // 1: a CTA's warps have a key/value head each; 0: they share one and take its keys in turn
+  int warp_heads;   // 1: a CTA's warps have a key/value head each, in one piece; 0: they share one and take its keys in turn
   int clustered;    // 1: the pieces of a row block are one cluster, which joins them; 0: they go through the workspace
   FastDiv by_group, by_x;   // by_x: of blockIdx.x into row block and piece
   float* part_o;    // [row][head][piece][dh], unnormalised
@@ -154,7 +154,7 @@ __device__ __forceinline__ void put_peer(uint32_t s, float2 v) {
 // A piece that has no keys says so and is done (in a cluster it takes part in the joining). True: it was one.
 __device__ __forceinline__ bool no_keys(const PagedAttnArgs& a, const Piece& c) {
   if (c.k0 < c.k1 || a.pieces == 1 || a.clustered) return false;
-  for (int r = a.warp_heads ? threadIdx.x & 31 : threadIdx.x; r < c.rows; r += a.warp_heads ? 32 : kThreads)
+  for (int r = threadIdx.x; r < c.rows; r += kThreads)
     a.part_ml[row_at(a, c, r, a.n_heads, 1) * a.pieces + c.piece] = make_float2(-INFINITY, 0.f);
   return true;
 }
@@ -602,7 +602,7 @@ __global__ void __launch_bounds__(kThreads, tc_ctas<DH, NR>()) paged_attn_tc_ker
     __syncwarp();
     for (int gr = 0; gr < S::kGroups; ++gr) {
       const int r = S::row(gr, lane), d = S::dim(gr, lane);
-      if (r < c.rows) put_row<BF16>(a, c, r, d, *reinterpret_cast<const float4*>(so + r * S::kPitch + d), end->m[warp][r], end->l[warp][r], a.pieces == 1);
+      if (r < c.rows) put_row<BF16>(a, c, r, d, *reinterpret_cast<const float4*>(so + r * S::kPitch + d), end->m[warp][r], end->l[warp][r], true);
     }
     return;
   }
@@ -937,7 +937,7 @@ void attn_plan(const uad_kv_seqs* s, int ctas_per_sm, PagedAttnArgs* a) {
   a->piece_keys = (int)(piece < (1ll << 30) ? piece : 1ll << 30);
   a->pieces = (int)((keys + a->piece_keys - 1) / a->piece_keys);
   const int64_t ctas = units * a->pieces;
-  a->clustered = a->pieces > 1 && !a->warp_heads && ((a->pieces <= kMaxCluster && ctas <= sms) || (a->pieces <= 8 && ctas * 20 <= slots * 17));
+  a->clustered = a->pieces > 1 && ((a->pieces <= kMaxCluster && ctas <= sms) || (a->pieces <= 8 && ctas * 20 <= slots * 17));
 }
 // Bytes of the partial rows: maxima and sums, then values.
 int64_t attn_bytes(const PagedAttnArgs& a) {

@@ -262,6 +262,17 @@ def test_more_heads_than_ctas(heads, n, longest, new):
     check_attention(c, q, out, lse)
 
 
+@pytest.mark.parametrize("heads,n,longest,new", [((24, 24, 64), 30, 700, 1), ((32, 8, 128), 58, 530, 1), ((8, 4, 64), 160, 600, 1), ((24, 24, 64), 17, 650, 8),
+                                                 ((32, 8, 128), 16, 4100, 1)])
+def test_many_heads_and_longer_caches(heads, n, longest, new):
+    """More heads than CTAs whose keys are many, a wave that is nearly full, one that would be barely more than one."""
+    lens = [longest if b < 2 else max(new, longest * (b % 7) // 7) for b in range(n)]
+    c = Case(heads, 16, lens, [new] * n, seed=n)
+    q, out, lse, status = run_attention(c, max_len=longest)
+    assert status == 0
+    check_attention(c, q, out, lse)
+
+
 def test_offsets_past_32_bits():
     """Pages 2^30 elements apart: element offsets up to 3 * 2^30 + ..., bytes past 2^32."""
     buf = torch.zeros((3 << 30) + (1 << 21), dtype=torch.bfloat16, device="cuda")
