@@ -26,6 +26,7 @@ struct PagedAttnArgs {
   int row_tiles;    // query rows of a CTA, in eights
   int row_blocks, pieces, piece_keys;
   int warp_heads;   // 1: a CTA's warps have a key/value head each, in one piece; 0: they share one and take its keys in turn
+  int f32_ctas;     // CTAs of an SM that the fp32 kernel is compiled for
   int clustered;    // 1: the pieces of a row block are one cluster, which joins them; 0: they go through the workspace
   FastDiv by_group, by_x;   // by_x: of blockIdx.x into row block and piece
   float* part_o;    // [row][head][piece][dh], unnormalised
@@ -635,8 +636,8 @@ __device__ __forceinline__ float4 lds_f4(uint32_t s) {
   return make_float4(__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w));
 }
 
-template <int DH>
-__global__ void __launch_bounds__(kThreads, 2) paged_attn_f32_kernel(const PagedAttnArgs a) {
+template <int DH, int CTAS>   // CTAs of an SM
+__global__ void __launch_bounds__(kThreads, CTAS) paged_attn_f32_kernel(const PagedAttnArgs a) {
   constexpr int KEYS = f32_slice<DH>(), SLOTS = f32_slots<DH>(), AHEAD = (SLOTS + 1) / 2, SLOT = KEYS * DH * 4, KJ = KEYS / 4, E = DH / 32;
   extern __shared__ __align__(16) unsigned char smem[];
   constexpr int RING = f32_ring<DH>(), EXTRA = receive_extra<DH, 8>(RING), END = RING + EXTRA + (int)sizeof(EndShared<8>);
@@ -968,7 +969,11 @@ int attn_args(const uad_kv_pages* pages, const uad_kv_seqs* seqs, const uad_attn
   a->row_tiles = 1;
   while (a->row_tiles < tiles && 8 * a->row_tiles < rows) a->row_tiles *= 2;
   a->row_blocks = (int)((rows + 8 * a->row_tiles - 1) / (8 * a->row_tiles));
-  attn_plan(seqs, a->p.dtype == F32 || a->row_tiles == 4 || dh == 256 ? 2 : dh == 64 && a->row_tiles == 1 ? 4 : 3, a);
+  // fp32, 64 dims: three CTAs an SM hide more, two have the registers that make a lone one faster (64 x 8000 keys of two heads 119 us
+  // against 132, 33 x 600 with 4 new tokens 10.7 against 12.7; but 28.7 against 22.8 with 16, where two an SM are one wave)
+  const int64_t units = (int64_t)a->p.n_seqs * a->p.n_kv * a->row_blocks;
+  a->f32_ctas = dh == 64 && (units > 304 || units * 5 < 304 * 3) ? 3 : 2;
+  attn_plan(seqs, a->p.dtype == F32 ? a->f32_ctas : a->row_tiles == 4 || dh == 256 ? 2 : dh == 64 && a->row_tiles == 1 ? 4 : 3, a);
   a->by_group = FastDiv((uint32_t)a->group);
   a->by_x = FastDiv((uint32_t)(a->clustered ? a->pieces : a->row_blocks));
   return UAD_OK;
@@ -994,17 +999,18 @@ cudaError_t launch_tc(const PagedAttnArgs& a, cudaStream_t s) {
   static OncePerDevice once;
   return launch_attn(once, paged_attn_tc_kernel<DH, NR>, tc_smem<DH, NR>(a.warp_heads ? kWarps : 1), tc_smem<DH, NR>(kWarps), a, s);
 }
-template <int DH>
+template <int DH, int CTAS>
 cudaError_t launch_f32(const PagedAttnArgs& a, cudaStream_t s) {
   static OncePerDevice once;
-  return launch_attn(once, paged_attn_f32_kernel<DH>, f32_smem<DH>(), f32_smem<DH>(), a, s);
+  return launch_attn(once, paged_attn_f32_kernel<DH, CTAS>, f32_smem<DH>(), f32_smem<DH>(), a, s);
 }
 
 template <int DH>
 cudaError_t launch_dh(const PagedAttnArgs& a, cudaStream_t s) {
   cudaError_t e;
   if (a.p.dtype == F32) {
-    e = launch_f32<DH>(a, s);
+    if constexpr (DH == 64) e = a.f32_ctas == 3 ? launch_f32<DH, 3>(a, s) : launch_f32<DH, 2>(a, s);
+    else e = launch_f32<DH, 2>(a, s);
   } else if (a.row_tiles == 1) {
     e = launch_tc<DH, 1>(a, s);
   } else if (a.row_tiles == 2) {
