@@ -669,10 +669,13 @@ cudaError_t launch_many(const W4Args& a, cudaStream_t s) {
     return (n <= kSms && chunks > 4 * split) || (NT <= 2 && n <= 2 * kSms && chunks >= 32 * split);
   };
   while (wn == 1 && split < 8 && more()) split *= 2;
-  // A CTA that is alone on its SM copies up to three chunks ahead; else the next CTA's work hides the copies, and smaller ones let
-  // more of them in (24 tokens: 14336 x 4096 21 us against 28, but 2048 x 32768 40 against 22).
-  int stages = ctas * split <= kSms ? 4 : 2;
-  while (stages > 2 && many_smem<NT>(wn, stages) > (split == 8 ? 112 : 227) * 1024) --stages;   // clusters of 8 need two CTAs an SM to find their places
+  // A CTA that is alone on its SM, or one of two in clusters, copies up to three chunks ahead; else the next CTA's work hides the
+  // copies, and smaller ones let more of them in (24 tokens: 14336 x 4096 24 us against 29, but 2048 x 32768 39 against 23; 5 tokens of
+  // 8192 x 2048 8.2 us both from a graph, and 8.8 against 10.2 without one, where the next call's CTAs would come in earlier).
+  // Clusters of 8 need two CTAs an SM, or four, to find their places.
+  const int64_t n = ctas * split;
+  int stages = n <= kSms || (split > 1 && split < 8 && n <= 2 * kSms) ? 4 : 2;
+  while (stages > 2 && many_smem<NT>(wn, stages) > (n <= kSms && split < 8 ? 227 : 112) * 1024) --stages;
   return launch_cluster(w4_many_kernel<NT, G>, dim3((unsigned)(ctas * split)), dim3(128 * wn), many_smem<NT>(wn, stages), split, s, a, wn, split, stages);
 }
 
