@@ -271,7 +271,7 @@ __device__ __forceinline__ void common_rows(EndShared<ROWS>* e) {
 // would need 128 rows where there are 8 to 32.
 // One new token: 64 x 4000 keys of 32 heads over 8 of 128 take 170 us (1050 MB, 6.2 TB/s, memory bound), of 8 over 1 of 256 48 us
 // (5.5 TB/s), 2 sequences of up to 131071 of the former 116 us (5.8 TB/s). With more rows the latency of a slice bounds: 64 x 4000
-// keys and four tokens of 8 over 1 of 256 86 us, where two blocks of 16 rows read them (96 MMAs a slice and block).
+// keys and four tokens of 8 over 1 of 256 75 us, where two blocks of 16 rows read them (96 MMAs a slice and block).
 
 __device__ __forceinline__ void mma16816(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -908,7 +908,7 @@ __global__ void __launch_bounds__(kThreads) paged_join_kernel(const PagedAttnArg
 // (`slots`), and pieces are not shorter than 256 keys (fp32: 64) but where everything is one small wave. A cluster
 // joins its pieces in 1 us, the workspace and a second kernel take 3; but clusters are placed as a whole, which leaves
 // SMs idle once there are many of them or they are large. Long pieces are cut further, up to four waves, so that
-// sequences of different lengths even out; but a wave that is barely more than one costs like two. In us, pieces with / without a
+// sequences of different lengths even out; but less than 1.75 waves cost more than one. In us, pieces with / without a
 // cluster:
 //   1 x 817 keys, 8 heads over 1 of 256:   13: 7.1 / 9.1,  7: 8.3 / 9.6
 //   64 x 282..1129, the same:               4: 16.3 / 18.4,  8: 23.3 / 17.1
@@ -916,6 +916,7 @@ __global__ void __launch_bounds__(kThreads) paged_join_kernel(const PagedAttnArg
 //   2 x 32768, 131071, 32 over 8 of 128:   28: - / 130,  80: - / 117
 //   16 x 4000, 32 over 8 of 128:            3: - / 50,  4: - / 57
 //   16 x 700, 8 new tokens, 24 of 64:       1: 16.5,  2: - / 22.6
+//   64 x 4000, 4 new tokens, 8 over 1 of 256: 2: - / 75,  4: - / 86
 // With more heads than the SMs hold CTAs and few keys, a CTA's warps take a head each and need no joining (24 heads of 64: 51 x 5
 // keys 9.6 -> 5.0, 64 x 60 keys 13.2 -> 8.5, 64 x 300 keys 26.7 -> 25.4; but 64 x up to 2000 keys 86 -> 106).
 void attn_plan(const uad_kv_seqs* s, int ctas_per_sm, PagedAttnArgs* a) {
@@ -936,7 +937,7 @@ void attn_plan(const uad_kv_seqs* s, int ctas_per_sm, PagedAttnArgs* a) {
     if (n > most(least)) n = most(least);
     const int64_t waves = 4 * slots / units < most(1024) ? 4 * slots / units : most(1024);
     if (waves > n) n = waves;
-    if (n > 2 && units * n > slots && units * n * 2 < slots * 3) n = slots / units > 1 ? slots / units : n;
+    if (n > 2 && units * n > slots && units * n * 4 < slots * 7) n = slots / units > 1 ? slots / units : n;
   }
   const int64_t piece = ((keys + n - 1) / n + 63) / 64 * 64;
   a->piece_keys = (int)(piece < (1ll << 30) ? piece : 1ll << 30);
