@@ -968,6 +968,7 @@ int attn_args(const uad_kv_pages* pages, const uad_kv_seqs* seqs, const uad_attn
   a->scale = t->scale != 0.f ? t->scale : 1.f / sqrtf((float)a->p.dh);
   a->scale_log2 = a->scale * 1.4426950408889634f;
   a->n_heads = t->n_heads; a->group = t->n_heads / a->p.n_kv; a->causal = t->causal; a->window = t->window;
+  if (a->p.n_seqs == 0 || a->p.n_rows == 0) return UAD_OK;   // nothing to split: no pieces, no workspace, no launch
   // rows of a CTA: 8, 16 or 32, as many as there are, within what the registers hold
   const int dh = a->p.dh, tiles = a->p.dtype == F32 ? 1 : dh == 256 ? 2 : 4;
   const int64_t rows = (int64_t)a->p.max_new * a->group;

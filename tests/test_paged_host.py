@@ -4,6 +4,7 @@ import ctypes as C
 import os
 import shutil
 import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -263,3 +264,28 @@ def test_binding_refuses_malformed_tensors():
                 dict(bias=torch.zeros(4)), dict()):
         with pytest.raises(ValueError):
             uad.linear_w4(**(dict(x=x, q=q, scale=s, out=out) | bad))
+
+
+# ---- empty batches of long caches ---------------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("max_len", [0, 5000])
+@pytest.mark.parametrize("width", [256, 257, 313, 1 << 20])
+def test_empty_batches_of_long_caches(width, max_len):
+    """No sequences or no rows, over tables of 4096 tokens and more: no work to split, so no workspace and no launch. In a process of
+    its own, which a division by zero would end."""
+    code = f"""
+import paper_2609_37772_gb300 as uad
+P = 1 << 20
+pages = uad.uad_kv_pages(k=P, v=P, page_stride=2048, slot_stride=128, head_stride=64, dtype=1, n_pages=4, page_size=16, n_kv_heads=2, head_dim=64)
+for dtype in (0, 1):
+    pages.dtype = dtype
+    for n_seqs, n_rows in ((0, 3), (0, 0), (3, 0)):
+        for window in (0, 9000):
+            seqs = uad.uad_kv_seqs(table=P, len=P, start=P, table_stride={width}, n_seqs=n_seqs, table_width={width}, max_new=2, max_len={max_len})
+            attn = uad.uad_attn(q=P, out=P, lse=P, q_stride=256, out_stride=256, n_heads=4, n_rows=n_rows, causal=1, window=window)
+            assert uad.uad_paged_attention_workspace(pages, seqs, attn) == 0
+            assert uad.uad_paged_attention(pages, seqs, attn, None, 0, None, None) == 0
+"""
+    r = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True)
+    assert r.returncode == 0, (r.returncode, r.stderr)
