@@ -387,7 +387,9 @@ typedef struct uad_attn {
 } uad_attn;
 
 /* Bytes of device memory that uad_paged_attention needs for these arguments (0 is possible): host only, the same for
- * the same sizes. table, len and start may be NULL here. Returns UAD_EINVAL (negative) for bad arguments. */
+ * the same sizes. What a call without a window needs is enough for every window; another number of sequences, rows or heads, another
+ * max_new, max_len or table_width may need more or less. table, len and start may be NULL here. Returns UAD_EINVAL (negative) for bad
+ * arguments. */
 int64_t uad_paged_attention_workspace(const uad_kv_pages* pages, const uad_kv_seqs* seqs, const uad_attn* attn);
 
 /* workspace: 16-byte aligned, in use until the call's work is done: calls that may run at the same time (other streams,

@@ -361,7 +361,7 @@ class PagedCache:
             self._refused(rc, "append")
 
     def attention_workspace(self, seqs, rows, n_heads, window=0):
-        """Bytes of the workspace that attention of these sizes needs (0 is possible)."""
+        """Bytes of the workspace that attention of these sizes needs (0 is possible). Without a window: enough for every window."""
         n = uad_paged_attention_workspace(self.pages, seqs.seqs, uad_attn(n_heads=n_heads, n_rows=rows, window=window))
         if n < 0:
             self._refused(n, "attention_workspace")

@@ -34,6 +34,7 @@ struct PagedAttnArgs {
 };
 
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
+constexpr int kSms = 152;
 constexpr int kMaxCluster = 16;   // more than 8 need the opt-in of non-portable sizes
 // A seen key's score is at least this, a hidden one's -infinity: a row that sees nothing (0) and one whose every score
 // is -infinity (undefined) stay apart.
@@ -919,17 +920,23 @@ __global__ void __launch_bounds__(kThreads) paged_join_kernel(const PagedAttnArg
 //   64 x 4000, 4 new tokens, 8 over 1 of 256: 2: - / 75,  4: - / 86
 // With more heads than the SMs hold CTAs and few keys, a CTA's warps take a head each and need no joining (24 heads of 64: 51 x 5
 // keys 9.6 -> 5.0, 64 x 60 keys 13.2 -> 8.5, 64 x 300 keys 26.7 -> 25.4; but 64 x up to 2000 keys 86 -> 106).
-void attn_plan(const uad_kv_seqs* s, int ctas_per_sm, PagedAttnArgs* a) {
-  int64_t keys = s->max_len > 0 && s->max_len < a->p.capacity ? s->max_len : a->p.capacity;
-  if (a->window > 0 && a->window + (int64_t)a->p.max_new - 1 < keys) keys = a->window + (int64_t)a->p.max_new - 1;
-  if (keys < 1) keys = 1;
-  constexpr int sms = 152;
-  const int64_t units = (int64_t)a->p.n_seqs * a->p.n_kv * a->row_blocks, slots = sms * ctas_per_sm;
-  const int64_t least = a->p.dtype == F32 ? 64 : 256;
-  a->warp_heads = a->p.dtype == BF16 && a->p.n_kv % kWarps == 0 && units >= slots && keys <= 512;
+struct Split {
+  int pieces, piece_keys, clustered;
+};
+// `keys` in at most n pieces.
+Split cut_keys(int64_t keys, int64_t n, int64_t units, int64_t slots) {
+  const int64_t piece = ((keys + n - 1) / n + 63) / 64 * 64;
+  Split c;
+  c.piece_keys = (int)(piece < (1ll << 30) ? piece : 1ll << 30);
+  c.pieces = (int)((keys + c.piece_keys - 1) / c.piece_keys);
+  const int64_t ctas = units * c.pieces;
+  c.clustered = c.pieces > 1 && ((c.pieces <= kMaxCluster && ctas <= kSms) || (c.pieces <= 8 && ctas * 20 <= slots * 17));
+  return c;
+}
+Split split_keys(int64_t keys, int64_t units, int64_t slots, int64_t least) {
   const auto most = [&](int64_t n) { return (keys + n - 1) / n; };   // pieces of at least n keys
   int64_t n;
-  if (keys <= kMaxCluster * 256 && units * (most(64) < kMaxCluster ? most(64) : kMaxCluster) <= sms) {
+  if (keys <= kMaxCluster * 256 && units * (most(64) < kMaxCluster ? most(64) : kMaxCluster) <= kSms) {
     n = most(64) < kMaxCluster ? most(64) : kMaxCluster;
   } else {
     n = units * 5 >= slots * 3 ? 1 : units * 2 > slots ? 2 : slots / units;
@@ -939,11 +946,24 @@ void attn_plan(const uad_kv_seqs* s, int ctas_per_sm, PagedAttnArgs* a) {
     if (waves > n) n = waves;
     if (n > 2 && units * n > slots && units * n * 4 < slots * 7) n = slots / units > 1 ? slots / units : n;
   }
-  const int64_t piece = ((keys + n - 1) / n + 63) / 64 * 64;
-  a->piece_keys = (int)(piece < (1ll << 30) ? piece : 1ll << 30);
-  a->pieces = (int)((keys + a->piece_keys - 1) / a->piece_keys);
-  const int64_t ctas = units * a->pieces;
-  a->clustered = a->pieces > 1 && ((a->pieces <= kMaxCluster && ctas <= sms) || (a->pieces <= 8 && ctas * 20 <= slots * 17));
+  return cut_keys(keys, n, units, slots);
+}
+void attn_plan(const uad_kv_seqs* s, int ctas_per_sm, PagedAttnArgs* a) {
+  const int64_t all = s->max_len > 0 && s->max_len < a->p.capacity ? s->max_len : a->p.capacity;
+  const int64_t keys = a->window > 0 && a->window + (int64_t)a->p.max_new - 1 < all ? a->window + (int64_t)a->p.max_new - 1 : all;
+  const int64_t units = (int64_t)a->p.n_seqs * a->p.n_kv * a->row_blocks, slots = kSms * ctas_per_sm;
+  const int64_t least = a->p.dtype == F32 ? 64 : 256;
+  a->warp_heads = a->p.dtype == BF16 && a->p.n_kv % kWarps == 0 && units >= slots && keys <= 512;
+  Split c = split_keys(keys, units, slots, least);
+  if (keys < all && c.pieces > 1 && !c.clustered) {
+    // Fewer keys can be more pieces, or as many that are no cluster: no more than there are without the window, so that what
+    // a call without one needs is enough for every window. (What makes a cluster of so many pieces makes one of fewer.)
+    const int most = split_keys(all, units, slots, least).pieces;
+    if (most < c.pieces) c = cut_keys(keys, most, units, slots);
+  }
+  a->pieces = c.pieces;
+  a->piece_keys = c.piece_keys;
+  a->clustered = c.clustered;
 }
 // Bytes of the partial rows: maxima and sums, then values.
 int64_t attn_bytes(const PagedAttnArgs& a) {

@@ -591,3 +591,19 @@ def test_calls_that_the_binding_refuses_on_the_gpu():
         bq = big.randn(big.rows, 2048)
         with pytest.raises(uad.UADError):
             bc.attention(bs, bq, torch.empty_like(bq), torch.empty(n - 1, dtype=torch.uint8, device="cuda"))
+
+
+@pytest.mark.parametrize("heads,dtype,lens,new,window", [((8, 2, 64), torch.bfloat16, [2400] * 32, 1, 2100), ((8, 1, 256), torch.float32, [2350] * 8, 4, 1714)],
+                         ids=["bf16", "f32"])
+def test_a_window_takes_the_workspace_of_the_call_without_one(heads, dtype, lens, new, window):
+    """One workspace for a model's layers with and without a window, where fewer keys would be cut into more pieces."""
+    c = Case(heads, 16, lens, [new] * len(lens), dtype, seed=17, rows_behind=0)
+    s, cache = c.sequences(max_len=max(lens)), uad.PagedCache(c.k, c.v)
+    q = c.randn(c.rows, c.hq * c.dh)
+    ws = torch.full((cache.attention_workspace(s, c.rows, c.hq) + 64,), 255, dtype=torch.uint8, device="cuda")
+    for w in (window, 0):
+        out, lse = torch.empty_like(q), torch.empty(c.rows, c.hq, device="cuda")
+        cache.attention(s, q, out, ws[:-64], window=w, lse=lse)
+        torch.cuda.synchronize()
+        assert bool((ws[-64:] == 255).all())
+        check_attention(c, q, out, lse, window=w)

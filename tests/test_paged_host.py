@@ -289,3 +289,28 @@ for dtype in (0, 1):
 """
     r = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True)
     assert r.returncode == 0, (r.returncode, r.stderr)
+
+
+# ---- one workspace for layers with and without a window ------------------------------------------------------------------------
+
+
+def workspace(heads, dtype, n_seqs, new, max_len, window, width=4096):
+    hq, hkv, dh = heads
+    p = pages(dtype=dtype, n_kv_heads=hkv, head_dim=dh, head_stride=dh, slot_stride=hkv * dh, page_stride=16 * hkv * dh)
+    s = seqs(table=None, len=None, start=None, table_width=width, table_stride=width, n_seqs=n_seqs, max_new=new, max_len=max_len)
+    return uad.uad_paged_attention_workspace(p, s, attn(n_heads=hq, n_rows=n_seqs * new, q_stride=hq * dh, out_stride=hq * dh, window=window))
+
+
+def test_a_workspace_without_a_window_holds_for_every_window():
+    """Fewer keys may be cut into more pieces: what they need stays within what all keys need."""
+    assert workspace((8, 2, 64), 1, 32, 1, 2400, 2100) <= workspace((8, 2, 64), 1, 32, 1, 2400, 0)
+    assert workspace((8, 1, 256), 0, 8, 4, 2350, 1714) <= workspace((8, 1, 256), 0, 8, 4, 2350, 0)
+    rng = np.random.default_rng(0)
+    heads = [(8, 1, 256), (4, 1, 128), (8, 2, 64), (24, 24, 64), (32, 8, 128), (4, 2, 64)]
+    for _ in range(4000):
+        h, dtype = heads[rng.integers(len(heads))], int(rng.integers(2))
+        n_seqs, new = int(np.exp(rng.uniform(0, 6))), int(np.exp(rng.uniform(0, 4)))
+        max_len = int(np.exp(rng.uniform(0, 11))) if rng.integers(4) else 0
+        most = workspace(h, dtype, n_seqs, new, max_len, 0)
+        for w in np.exp(rng.uniform(0, np.log(max_len or 65536), 6)).astype(int):
+            assert 0 <= workspace(h, dtype, n_seqs, new, max_len, int(w)) <= most, (h, dtype, n_seqs, new, max_len, w)
