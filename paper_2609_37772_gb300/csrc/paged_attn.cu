@@ -918,8 +918,22 @@ __global__ void __launch_bounds__(kThreads) paged_join_kernel(const PagedAttnArg
 //   16 x 4000, 32 over 8 of 128:            3: - / 50,  4: - / 57
 //   16 x 700, 8 new tokens, 24 of 64:       1: 16.5,  2: - / 22.6
 //   64 x 4000, 4 new tokens, 8 over 1 of 256: 2: - / 75,  4: - / 86
-// With more heads than the SMs hold CTAs and few keys, a CTA's warps take a head each and need no joining (24 heads of 64: 51 x 5
-// keys 9.6 -> 5.0, 64 x 60 keys 13.2 -> 8.5, 64 x 300 keys 26.7 -> 25.4; but 64 x up to 2000 keys 86 -> 106).
+// With more heads than the SMs hold CTAs and up to 512 keys, a CTA's warps may have a key/value head each, which needs no joining. Its
+// queries then take four times the shared memory, so that fewer CTAs fit an SM (heads of 256: one and not two), and their number is a
+// quarter. Both forms cost their rounds (about 4 us a round, 40000 / head_dim keys of a head, before and after the keys) and the keys
+// of the fullest SM, an eighth more where warps have heads, half more where they have 32 rows and are alone on their SM. In us, one
+// token, with / without, and what the costs choose:
+//   51 x 5 keys, 24 heads of 64:                4.7 / 9.0, with         256 x 60, the same:     21.7 / 40.2, with
+//   26 x 512, the same:                        22.7 / 18.9, without     64 x 300, the same:     23.8 / 25.5, with
+//   64 x 60, 32 over 8 of 128:                  8.1 / 9.8, with         102 x 512, the same:    40.3 / 37.0, without
+//   51 x 60, 8 of 256:                         10.5 / 11.4, with        38 x 300, the same:     28.9 / 19.1, without
+//   102 x 60, 128 over 4 of 128:               13.8 / 14.8, with        76 x 512, the same:     49.1 / 20.4, without
+// Keys past 512 gain nothing (64 x up to 2000 keys of 24 heads of 64: 106 / 86).
+size_t warp_heads_smem(int dh, int row_tiles) {
+  if (dh == 64) return row_tiles == 1 ? tc_smem<64, 1>(kWarps) : row_tiles == 2 ? tc_smem<64, 2>(kWarps) : tc_smem<64, 4>(kWarps);
+  if (dh == 128) return row_tiles == 1 ? tc_smem<128, 1>(kWarps) : row_tiles == 2 ? tc_smem<128, 2>(kWarps) : tc_smem<128, 4>(kWarps);
+  return row_tiles == 1 ? tc_smem<256, 1>(kWarps) : tc_smem<256, 2>(kWarps);
+}
 struct Split {
   int pieces, piece_keys, clustered;
 };
@@ -953,7 +967,14 @@ void attn_plan(const uad_kv_seqs* s, int ctas_per_sm, PagedAttnArgs* a) {
   const int64_t keys = a->window > 0 && a->window + (int64_t)a->p.max_new - 1 < all ? a->window + (int64_t)a->p.max_new - 1 : all;
   const int64_t units = (int64_t)a->p.n_seqs * a->p.n_kv * a->row_blocks, slots = kSms * ctas_per_sm;
   const int64_t least = a->p.dtype == F32 ? 64 : 256;
-  a->warp_heads = a->p.dtype == BF16 && a->p.n_kv % kWarps == 0 && units >= slots && keys <= 512;
+  a->warp_heads = 0;
+  if (a->p.dtype == BF16 && a->p.n_kv % kWarps == 0 && keys <= 512) {
+    const int64_t fit = 228 * 1024 / ((int64_t)warp_heads_smem(a->p.dh, a->row_tiles) + 1024);   // an SM's, and what it keeps of each CTA's
+    const int64_t ctas = units / kWarps, held = kSms * (fit < ctas_per_sm ? fit : ctas_per_sm), round = 8 * (40000 / a->p.dh);
+    const int64_t with = (ctas + held - 1) / held * round + (ctas + kSms - 1) / kSms * kWarps * keys * (a->row_tiles == 4 ? 12 : 9);
+    const int64_t without = (units + slots - 1) / slots * round + (units + kSms - 1) / kSms * keys * 8;
+    a->warp_heads = with < without;
+  }
   Split c = split_keys(keys, units, slots, least);
   if (keys < all && c.pieces > 1 && !c.clustered) {
     // Fewer keys can be more pieces, or as many that are no cluster: no more than there are without the window, so that what

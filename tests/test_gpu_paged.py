@@ -607,3 +607,16 @@ def test_a_window_takes_the_workspace_of_the_call_without_one(heads, dtype, lens
         torch.cuda.synchronize()
         assert bool((ws[-64:] == 255).all())
         check_attention(c, q, out, lse, window=w)
+
+
+@pytest.mark.parametrize("heads,n,longest,new", [((8, 8, 256), 38, 60, 1), ((8, 8, 256), 51, 60, 1), ((16, 16, 256), 51, 70, 1), ((16, 4, 256), 76, 50, 3), ((128, 4, 128), 76, 40, 1),
+                                                 ((128, 4, 128), 102, 40, 1), ((32, 8, 128), 102, 60, 1), ((64, 8, 128), 60, 50, 1), ((32, 8, 64), 76, 130, 1), ((64, 4, 64), 130, 40, 2)],
+                         ids=lambda x: "x".join(map(str, x)) if isinstance(x, tuple) else str(x))
+def test_heads_to_warps_or_to_ctas(heads, n, longest, new):
+    """Sizes on both sides of where a CTA's warps get heads of their own, every head size, 8 to 32 rows."""
+    lens = [max(new, 1 + (41 * i) % longest) for i in range(n)]
+    lens[-1] = longest
+    c = Case(heads, 16, lens, [new] * n, seed=n + heads[2])
+    q, out, lse, status = run_attention(c, max_len=longest)
+    assert status == 0
+    check_attention(c, q, out, lse)
