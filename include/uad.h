@@ -411,10 +411,9 @@ int uad_set_prefix_paged(uad_ctx* ctx, int32_t robot, const uad_kv_pages* layers
 /* ---- The projection of few tokens with 4-bit weights ------------------------------------------------------
  * out[M][N] = x[M][K] w^T + bias with w[n][k] = (q[n][k] - zero[n][k / group]) * scale[n][k / group]: for the tokens of a
  * decoding step, whose time is that of reading the weights. x: device bf16; q: device [N][K / 2], k even in the low
- * four bits of byte k / 2; scale: device bf16 [N][K / group]; |scale| < 2^100; zero: device uint8 [N][K / group], 0..15 (only the low
- * four bits are read), or NULL: 8; bias: device fp32 [N] or NULL; out: device fp32 [M][N]. Sums are in fp32, over a group
- * first and then scaled; up to 8 tokens with groups of 64 and 128, the sum of q x less zero times the sum of x (x to 30 bits
- * below its group's largest value), else of the exact x (q - zero). A row of x with infinities gives infinities or NaN. x and q
+ * four bits of byte k / 2; scale: device bf16 [N][K / group]; zero: device uint8 [N][K / group], 0..15 (only the low four bits are
+ * read), or NULL: 8; bias: device fp32 [N] or NULL; out: device fp32 [M][N]. Sums are in fp32: of the exact x (q - zero) over a group
+ * first, which has to stay within fp32 by itself, and then scaled. A row of x with infinities gives infinities or NaN. x and q
  * 16-byte aligned. 1 <= M <= UAD_W4_MAX_ROWS, N >= 1, K % group == 0,
  * group 32, 64 or 128, K <= 2^30, N * K <= 2^35. Asynchronous on `stream` and in its order; allocates nothing; may be captured.
  * Errors: UAD_EINVAL, UAD_ETOOBIG (M: dequantise and use uad_linear), UAD_ECUDA. */

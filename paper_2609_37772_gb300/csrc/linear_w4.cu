@@ -1,6 +1,4 @@
 // The projection of few tokens with 4-bit weights.
-#include <cuda_fp16.h>
-
 #include <cmath>
 #include <cstring>
 
@@ -38,16 +36,28 @@ __device__ __forceinline__ uint32_t nibbles(uint32_t w) {
   asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(w), "r"(0x000f000fu), "r"(0x43004300u));
   return r;
 }
+__device__ __forceinline__ void mma_bf16_16816(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_bf16_first(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+}
+__device__ __forceinline__ uint32_t sub2(uint32_t x, uint32_t y) {
+  const __nv_bfloat162 r = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&x), *reinterpret_cast<const __nv_bfloat162*>(&y));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
 
 // ---- up to 8 tokens: a stream of weights --------------------------------------------------------------------------------
 //
 // What bounds a few tokens, once the weights arrive at full bandwidth (14 cycles of an SM's quarter for 256 weights), is
-// taking the nibbles apart. As fp16 the bits of a nibble at the bottom of a half word are the subnormal q 2^-24, four bits
-// further up 16 q 2^-24, so four masks and a shift make operands of all eight of a word, with neither an exponent to set nor
-// an offset to subtract (bf16 takes 7 integer operations and 4 subtractions). The tokens are scaled to 2^14..2^15 by the power
-// of two of their group's largest value, which leaves a bf16's 8 bits whole down to 2^-30 of it in fp16, every second pair
-// divided by 16 as well. The products are exact and summed in fp32; a group's sum less zero times the tokens' own sum is then
-// scaled. That the zero is subtracted after the sum costs a bit: q is up to 15 where q - zero is up to 8.
+// taking the nibbles apart: three shifts, four masks and four subtractions for the eight of a word, which make exact bf16 of
+// q - zero (0x4300 | q is 128 + q; less 128 + zero). The tokens stay as they are, but for their order. A group's products are exact and
+// summed in fp32, and the sum is then scaled. Products of q itself would save the subtractions, but sums of q x cancel against zero
+// times the tokens' sum: a large token whose weights are all zero would take the small ones' bits.
 //
 // A tile of 16 rows is walked by wk of a CTA's warps, which take its chunks in turn and add up in shared memory: one, where
 // there are tiles enough for every warp, which saves the adding. A warp's copies run on from tile to tile. Where
@@ -77,27 +87,12 @@ struct Groups<2> { uint32_t s; uint16_t z; };
 template <>
 struct Groups<4> { uint64_t s; uint32_t z; };
 constexpr int kAhead = 3;             // chunks that scales and zeros are loaded ahead
-// Shared memory: 16 zeros; the warps' rings; their sums [2][warp][token][16]; the cluster's [2][rank][token][16]; the tokens'
-// factors and sums [group][token, an even number]; the tokens [step][token][t] of 16 bytes. k: a multiple of kChunk.
+// Shared memory: 16 zeros; the warps' rings; their sums [2][warp][token][16]; the cluster's [2][rank][token][16]; the
+// tokens [step][token][t] of 16 bytes. k: a multiple of kChunk.
 template <int G>
 __host__ __device__ inline size_t few_smem(int rows, int k) {
   return 16 + (size_t)kW4Warps * kFewSlots * 16 * few_pitch<G>() + (size_t)2 * kW4Warps * rows * 64 + (size_t)2 * 8 * rows * 64 +
-         (size_t)(k / G) * ((rows + 1) & ~1) * 8 + (size_t)rows * k * 2;
-}
-
-__device__ __forceinline__ void mma_f16(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
-  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ void mma_f16_first(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
-  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
-      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
-}
-__device__ __forceinline__ uint32_t pack_f16(float x, float y) {
-  const __half2 h = __floats2half2_rn(x, y);
-  return *reinterpret_cast<const uint32_t*>(&h);
+         (size_t)rows * k * 2;
 }
 
 template <int G, bool VEC>   // VEC: a chunk's scales, and its zeros, are read as one word
@@ -112,7 +107,7 @@ __global__ void __launch_bounds__(32 * kW4Warps, 2) w4_few_kernel(const FewArgs 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int part = f.split > 1 ? blockIdx.x % f.split : 0, wk_bits = __ffs(f.wk) - 1, kw = warp & (f.wk - 1), of_cta = warp >> wk_bits;
   const int cta = f.split > 1 ? blockIdx.x / f.split : blockIdx.x, ctas = f.split > 1 ? gridDim.x / f.split : gridDim.x;
-  const int tiles = (a.N + 15) / 16, groups = a.K / G, even = (a.M + 1) & ~1, stride = ctas * f.per_cta;
+  const int tiles = (a.N + 15) / 16, groups = a.K / G, stride = ctas * f.per_cta;
   const int kb = part * f.split_k, ke = min(a.K, kb + f.split_k);
   int tile = cta * f.per_cta + of_cta, rounds = (tiles - cta * f.per_cta + stride - 1) / stride;   // of the CTA
   // this warp's chunks of a tile, and how many are left to copy and to find the scales of
@@ -121,8 +116,7 @@ __global__ void __launch_bounds__(32 * kW4Warps, 2) w4_few_kernel(const FewArgs 
   const uint32_t ring = ptx::su32(smem) + 16 + warp * kFewSlots * SLOT;
   float* red = reinterpret_cast<float*>(smem + 16 + kW4Warps * kFewSlots * SLOT);
   float* recv = red + 2 * kW4Warps * a.M * 16;
-  float2* xg = reinterpret_cast<float2*>(recv + 2 * 8 * a.M * 16);             // x: 1 / scale, y: 2^-24 sum of the scaled values
-  unsigned char* xp = reinterpret_cast<unsigned char*>(xg + f.split_k / G * even);
+  unsigned char* xp = reinterpret_cast<unsigned char*>(recv + 2 * 8 * a.M * 16);
   const uint32_t xs = ptx::su32(xp);
   if (threadIdx.x < 4) reinterpret_cast<uint32_t*>(smem)[threadIdx.x] = 0;
 
@@ -205,7 +199,7 @@ __global__ void __launch_bounds__(32 * kW4Warps, 2) w4_few_kernel(const FewArgs 
     load(gs[i]);
     if (i + 1 < kAhead) put(gs[i]);
   }
-  // Tokens: eight values a thread, a group's threads side by side; 0 past K.
+  // Tokens: eight values a thread, put into the nibbles' order (k and k + 4 are a pair); 0 past K.
   const int work = a.M * (f.split_k / 8);
   for (int i0 = 0; i0 < work; i0 += 4 * 32 * kW4Warps) {
     uint4 vs[4];
@@ -220,40 +214,11 @@ __global__ void __launch_bounds__(32 * kW4Warps, 2) w4_few_kernel(const FewArgs 
     }
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      if (i0 + u * 32 * kW4Warps >= work) break;
-      const int m = ms[u], p = ps[u];
-      const uint32_t w[4] = {vs[u].x, vs[u].y, vs[u].z, vs[u].w};
-      float x[8], top = 0.f, sum = 0.f;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        x[2 * j] = __uint_as_float(w[j] << 16);
-        x[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
-        top = fmaxf(top, fmaxf(fabsf(x[2 * j]), fabsf(x[2 * j + 1])));
-      }
-#pragma unroll
-      for (int d = 1; d < G / 8; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-      const int e = min(max(__float_as_int(top) >> 23, 15), 254);
-      float scale = __int_as_float((268 - e) << 23), back = __int_as_float((e - 14) << 23);
-      if (top == INFINITY) {   // then only the infinite values count, as 1 and with an infinite factor
-        scale = 1.f;
-        back = INFINITY;
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (x[j] == x[j]) x[j] = fabsf(x[j]) == INFINITY ? copysignf(1.f, x[j]) : 0.f;
-      }
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        x[j] *= scale;
-        sum += x[j];
-      }
-#pragma unroll
-      for (int d = 1; d < G / 8; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-      if (i0 + u * 32 * kW4Warps + (int)threadIdx.x < work) {
-        const int j = p / (4 * GS), tt = p / GS & 3, v = p & (GS - 1);   // group, lane and step of the group
-        if (p % (4 * GS) == 0) xg[j * even + m] = make_float2(back, sum * 5.9604644775390625e-08f);
-        *reinterpret_cast<uint4*>(xp + (((j * GS + v) * a.M + m) * 4 + tt) * 16) =
-            make_uint4(pack_f16(x[0], x[4]), pack_f16(x[1] * 0.0625f, x[5] * 0.0625f), pack_f16(x[2], x[6]), pack_f16(x[3] * 0.0625f, x[7] * 0.0625f));
-      }
+      if (i0 + u * 32 * kW4Warps + (int)threadIdx.x >= work) break;
+      const int m = ms[u], p = ps[u], j = p / (4 * GS), tt = p / GS & 3, v = p & (GS - 1);   // group, lane and step of the group
+      *reinterpret_cast<uint4*>(xp + (((j * GS + v) * a.M + m) * 4 + tt) * 16) =
+          make_uint4(__byte_perm(vs[u].x, vs[u].z, 0x5410), __byte_perm(vs[u].x, vs[u].z, 0x7632), __byte_perm(vs[u].y, vs[u].w, 0x5410),
+                     __byte_perm(vs[u].y, vs[u].w, 0x7632));
     }
   }
   __syncthreads();
@@ -289,30 +254,29 @@ __global__ void __launch_bounds__(32 * kW4Warps, 2) w4_few_kernel(const FewArgs 
         else w[h][0] = lds4(at);
       }
       float sum[NT][4];
+      const uint32_t z0 = 0x43004300u | ((uint32_t)now[0].z >> (8 * j) & 15u) * 0x10001u, z1 = 0x43004300u | ((uint32_t)now[1].z >> (8 * j) & 15u) * 0x10001u;
 #pragma unroll
       for (int v = 0; v < GS; ++v) {
-        const uint32_t w0 = w[0][v], w1 = w[1][v], v0 = w0 >> 8, v1 = w1 >> 8;
-        const uint32_t f0[4] = {w0 & 0x000f000fu, w1 & 0x000f000fu, w0 & 0x00f000f0u, w1 & 0x00f000f0u};
-        const uint32_t f1[4] = {v0 & 0x000f000fu, v1 & 0x000f000fu, v0 & 0x00f000f0u, v1 & 0x00f000f0u};
+        uint32_t a0[2][4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          a0[u >> 1][2 * (u & 1)] = sub2(nibbles(w[0][v] >> (4 * u)), z0);
+          a0[u >> 1][2 * (u & 1) + 1] = sub2(nibbles(w[1][v] >> (4 * u)), z1);
+        }
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
           uint4 b;
           asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(b.x), "=r"(b.y), "=r"(b.z), "=r"(b.w) : "r"(x_at[n] + (j * GS + v) * x_step[n]) : "memory");
-          if (v == 0) mma_f16_first(sum[n], f0, b.x, b.y);
-          else mma_f16(sum[n], f0, b.x, b.y);
-          mma_f16(sum[n], f1, b.z, b.w);
+          if (v == 0) mma_bf16_first(sum[n], a0[0], b.x, b.y);
+          else mma_bf16_16816(sum[n], a0[0], b.x, b.y);
+          mma_bf16_16816(sum[n], a0[1], b.z, b.w);
         }
       }
-      // (sum of q x - zero sum of x) 2^-24 of the scaled tokens, times 2^24 scale / their scale
-      const float z0 = (float)((uint32_t)now[0].z >> (8 * j) & 15u), z1 = (float)((uint32_t)now[1].z >> (8 * j) & 15u);
-      const float s0 = __uint_as_float((uint32_t)(now[0].s >> (16 * j)) << 16) * 16777216.f, s1 = __uint_as_float((uint32_t)(now[1].s >> (16 * j)) << 16) * 16777216.f;
+      const float s0 = __uint_as_float((uint32_t)(now[0].s >> (16 * j)) << 16), s1 = __uint_as_float((uint32_t)(now[1].s >> (16 * j)) << 16);
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {   // tokens 2 t and 2 t + 1 (of those that are not there, anything)
-        const float4 x = *reinterpret_cast<const float4*>(xg + ((kw + i * f.wk) * PG + j) * even + min(8 * n + 2 * t, even - 2));
+      for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int c = 0; c < 4; ++c)
-          acc[n][c] = fmaf(fmaf(-(c < 2 ? z0 : z1), c & 1 ? x.w : x.y, sum[n][c]) * (c & 1 ? x.z : x.x), c < 2 ? s0 : s1, acc[n][c]);
-      }
+        for (int c = 0; c < 4; ++c) acc[n][c] = fmaf(sum[n][c], c < 2 ? s0 : s1, acc[n][c]);
     }
 #pragma unroll
     for (int n = 0; n < NT; ++n) x_at[n] += 4 * f.wk * x_step[n];
@@ -420,9 +384,10 @@ cudaError_t launch_few(const W4Args& a, cudaStream_t s) {
       if (cost < best) best = cost, f.wk = wk;
     }
   }
-  // Three tokens and more go faster by tiles of 32 rows where a tile's chunks are shared out, unless they are few (4 tokens of
-  // 4096 x 4096 8.4 us against 7.4, 8 of 8192 x 2048 14.1 against 7.9; but 2.9 against 3.5 for 768 x 2304, and 13 against 18 for
-  // 2048 x 32768, where every warp has tiles of its own). Where the tokens of a CTA do not fit, all do.
+  // Three tokens and more go faster by tiles of 32 rows where a tile's chunks are shared out, unless they are few (8 tokens of
+  // 4096 x 4096 in groups of 128 7.3 us against 8.9, 4 of 14336 x 4096 15.3 against 23.6; but 3.3 against 2.7 for 4 of 768 x 2304, and
+  // 15.0 against 14.4 for 2048 x 32768 in groups of 64, where every warp has tiles of its own). Where the tokens of a CTA do not fit,
+  // all do.
   if ((a.M > 2 && f.wk > 1 && chunks > 8) || smem > 227 * 1024) return launch_many<1, G>(a, s);
   const int64_t clusters = ctas / f.split, rounds = ((int64_t)tiles * f.wk + clusters * kW4Warps - 1) / (clusters * kW4Warps);
   f.per_cta = (int)((tiles + clusters * rounds - 1) / (clusters * rounds));   // even rounds
@@ -445,21 +410,6 @@ template <int NT>
 __host__ __device__ constexpr size_t many_smem(int wn, int stages) {
   // tokens [stage][quarter of K][token][256 bytes], weights [stage][warp][32 rows], scales and zeros [2][warp][4 groups][32 rows]
   return stages * ((size_t)4 * 8 * NT * 256 + (size_t)4 * wn * 32 * kManyPitch) + (size_t)2 * 4 * wn * 4 * 32 * 4;
-}
-
-__device__ __forceinline__ void mma_bf16_16816(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
-  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ void mma_bf16_first(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
-  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
-      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
-}
-__device__ __forceinline__ uint32_t sub2(uint32_t x, uint32_t y) {
-  const __nv_bfloat162 r = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&x), *reinterpret_cast<const __nv_bfloat162*>(&y));
-  return *reinterpret_cast<const uint32_t*>(&r);
 }
 
 template <int NT, int G>   // 8 NT tokens, group

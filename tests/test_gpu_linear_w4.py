@@ -246,3 +246,43 @@ def test_large_calls_among_the_other_projections():
                 assert float((o - a).abs().max()) <= 1e-5 * float(a.abs().max())
             else:
                 assert torch.equal(o, a)
+
+
+# From one token to 64: rows of 16 that a CTA's warps share or own, a K that a cluster shares, tiles of 32 rows, tcgen05
+NEAR_ZERO = [(M, N, K, group) for group in (32, 64, 128) for M, N, K in ((1, 75, 512), (1, 2560, 4096), (2, 300, 16384), (2, 20000, 512), (3, 2100, 2048),
+                                                                        (6, 20000, 512), (8, 640, 1024), (20, 333, 2048), (40, 4101, 4224))]
+
+
+@pytest.mark.parametrize("M,N,K,group", NEAR_ZERO)
+@pytest.mark.parametrize("zero", [False, True])
+def test_large_tokens_at_the_zero_point_have_no_influence(M, N, K, group, zero):
+    """Half of the tokens' values are thousands of times the others (a model's outlier channels), and all their weights the zero
+    point: the terms that are left are small, and so is the tolerance, which counts |x w| alone."""
+    x, q, scale, z, bias = operands(M, N, K, group, zero, M + N + K + 1)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(M + K)
+    out = torch.empty(M, N, device="cuda")
+    big = torch.rand(K, generator=g, device="cuda") < 0.5
+    x = torch.where(big, x.float() * 4096 + 2048, x.float()).bfloat16()
+    zp = torch.full((N, K // group), 8, device="cuda", dtype=torch.uint8) if z is None else z & 15
+    rep = zp.repeat_interleave(group, dim=1)
+    w = torch.where(big, rep, torch.stack([q & 15, q >> 4], dim=-1).reshape(N, K))
+    q = (w[:, 0::2] | w[:, 1::2] << 4).contiguous()
+    uad.linear_w4(x, q, scale, out, zero=z)
+    torch.cuda.synchronize()
+    want, size = reference(x, q, scale, z, None)
+    check(out, want, size, K, group, None)
+
+
+@pytest.mark.parametrize("M,N,K,group", NEAR_ZERO)
+@pytest.mark.parametrize("zero", [False, True])
+def test_rows_of_the_zero_point_alone_give_the_bias(M, N, K, group, zero):
+    x, q, scale, z, bias = operands(M, N, K, group, zero, M + N + K + 2)
+    x = (x.float() + 1).bfloat16()
+    zp = torch.full((N, K // group), 8, device="cuda", dtype=torch.uint8) if z is None else z & 15
+    rows = (zp | zp << 4).repeat_interleave(group // 2, dim=1)
+    q[::3] = rows[::3]
+    out = torch.empty(M, N, device="cuda")
+    uad.linear_w4(x, q, scale, out, zero=z, bias=bias)
+    torch.cuda.synchronize()
+    assert torch.equal(out[:, ::3], bias[::3].expand(M, -1))
