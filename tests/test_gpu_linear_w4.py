@@ -4,7 +4,10 @@ Tolerance: products of bf16 and whole numbers up to 15 are exact; a group's sum 
 step (the tensor cores truncate), 2^-23 of the sum of magnitudes each, as is every group that is added: (group + groups + 2)
 2^-23 sum |x w|, and the output's own half step 2^-24. The same is demanded where the zero is subtracted after a group's sum,
 although the terms then are |x| (q + zero).
+(Every kernel now subtracts the zero before the product.)
 """
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -286,3 +289,29 @@ def test_rows_of_the_zero_point_alone_give_the_bias(M, N, K, group, zero):
     uad.linear_w4(x, q, scale, out, zero=z, bias=bias)
     torch.cuda.synchronize()
     assert torch.equal(out[:, ::3], bias[::3].expand(M, -1))
+
+
+INFINITE = [(1, 96, 512), (2, 96, 512), (1, 20000, 512), (3, 20000, 512), (2, 300, 16384), (4, 2100, 2048), (12, 96, 512), (20, 333, 2048), (64, 96, 512), (33, 4100, 4224)]
+
+
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("M,N,K", INFINITE)
+def test_infinite_tokens_give_infinities_or_nan(M, N, K, group):
+    """Every value of a row with an infinity, by itself or beside others, is what the definition has: an infinity of the weight's
+    sign, NaN where the weight is 0 or infinities meet. The rows beside it keep their bits."""
+    x, q, scale, z, bias = operands(M, N, K, group, True, M + N)
+    clean, out = torch.empty(M, N, device="cuda"), torch.empty(M, N, device="cuda")
+    uad.linear_w4(x, q, scale, clean, zero=z, bias=bias)
+    for row, at in ((M - 1, {K - 12: math.inf}), (0, {5: -math.inf}), (M // 2, {7: math.inf, K - 3: -math.inf, K // 2: math.inf})):
+        x2 = x.clone()
+        for k, v in at.items():
+            x2[row, k] = v
+        uad.linear_w4(x2, q, scale, out, zero=z, bias=bias)
+        torch.cuda.synchronize()
+        w = paged.dequantize(q.cpu().numpy(), scale.float().cpu().numpy(), z.cpu().numpy())
+        with np.errstate(invalid="ignore"):
+            want = sum(v * w[:, k] for k, v in at.items())
+        got = out[row].double().cpu().numpy()
+        assert not np.isfinite(got).any() and np.array_equal(got, want, equal_nan=True)
+        same = [m for m in range(M) if m != row]
+        assert torch.equal(out[same], clean[same])
