@@ -351,7 +351,8 @@ int uad_rope_init(double theta, int32_t dim, uad_rope* out);
 typedef struct uad_kv_rows {
   const void *q, *k, *v; /* q: NULL = no queries; k, v: both or NULL = only queries are rotated */
   int64_t q_stride, k_stride, v_stride;
-  void* q_out;           /* rotated queries in the cache's type, head h of row t at t * q_out_stride + h * head_dim; may be q */
+  void* q_out;           /* rotated queries in the cache's type, head h of row t at t * q_out_stride + h * head_dim. May be q where rows
+                            and cache are of one type and the strides are the same; otherwise it must not overlap q, k or v */
   int64_t q_out_stride;
   int32_t dtype;         /* type of q, k and v: UAD_DTYPE_F32 (such as uad_linear's output) or UAD_DTYPE_BF16 */
   int32_t n_heads;       /* query heads; 0 without q */

@@ -315,7 +315,7 @@ class PagedCache:
     def append(self, seqs, k=None, v=None, q=None, q_out=None, rope=None, status=None, stream=None):
         """Write the new tokens' keys and values [rows][n_kv_heads * head_dim] into their pages and their queries
         [rows][n_heads * head_dim] into q_out, keys and queries rotated by `rope` (None: not). float32 or bfloat16 rows,
-        which may be parts of a fused projection; q_out in the cache's type."""
+        which may be parts of a fused projection; q_out in the cache's type (q itself only where that is the rows')."""
         g = self._gpu
         if seqs._gpu != g:
             raise ValueError(f"sequences: must be on {self.device}, are on {seqs.device}")

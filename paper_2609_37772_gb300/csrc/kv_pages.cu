@@ -225,6 +225,8 @@ int uad_kv_append(const uad_kv_pages* pages, const uad_kv_seqs* seqs, const uad_
   if (bad_address(rows->q, rows->q_stride, es) || bad_address(rows->k, rows->k_stride, es) || bad_address(rows->v, rows->v_stride, es) ||
       bad_address(rows->q_out, rows->q_out_stride, ces))
     return UAD_EINVAL;
+  // in place, a thread writes the bytes that it has read: not where an element of the output has another size or place
+  if (rows->q && rows->q == rows->q_out && (es != ces || (rows->q_stride != rows->q_out_stride && rows->n_rows > 1))) return UAD_EINVAL;
   if (rope && (rope->dim < 16 || rope->dim > a.p.dh || rope->dim % 16)) return UAD_EINVAL;
   if (a.p.n_seqs == 0 || a.p.n_rows == 0) return UAD_OK;
   a.p.status = status;

@@ -314,3 +314,16 @@ def test_a_workspace_without_a_window_holds_for_every_window():
         most = workspace(h, dtype, n_seqs, new, max_len, 0)
         for w in np.exp(rng.uniform(0, np.log(max_len or 65536), 6)).astype(int):
             assert 0 <= workspace(h, dtype, n_seqs, new, max_len, int(w)) <= most, (h, dtype, n_seqs, new, max_len, w)
+
+
+# ---- queries rotated in place -----------------------------------------------------------------------------------------------
+
+
+def test_queries_in_place_need_one_type_and_stride():
+    """With another element size or stride a thread's output lies on what another thread has yet to read. (Without
+    sequences a call whose arguments are sound is answered, and reaches no GPU.)"""
+    for cache, row, out_stride, sound in ((1, 1, 256, True), (0, 0, 256, True), (1, 0, 256, False), (0, 1, 256, False), (1, 1, 512, False), (0, 0, 264, False)):
+        r = rows(dtype=row, q=P, q_out=P, q_out_stride=out_stride)
+        assert call_append(pages(dtype=cache), seqs(n_seqs=0), r) == (uad.UAD_OK if sound else uad.UAD_EINVAL)
+        assert call_append(pages(dtype=cache), seqs(n_seqs=0), rows(dtype=row, q=P, q_out=P + (1 << 16), q_out_stride=out_stride)) == uad.UAD_OK
+    assert call_append(pages(), seqs(n_seqs=0), rows(dtype=1, n_rows=1, q_out_stride=512)) == uad.UAD_OK   # the stride of one row says nothing
