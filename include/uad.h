@@ -379,7 +379,7 @@ typedef struct uad_attn {
   float* lse;            /* [n_rows][n_heads] natural logarithm of the softmax's denominator; NULL: not wanted */
   const uint8_t* key_mask;   /* rows of table_width * page_size bytes, mask_stride apart */
   int64_t q_stride, out_stride, mask_stride;
-  float scale;           /* 0: 1 / sqrt(head_dim) */
+  float scale;           /* 0: 1 / sqrt(head_dim). For a softmax of zeros, fp32's least number above 0 */
   int32_t n_heads;       /* a multiple of n_kv_heads, at most 64 times it */
   int32_t n_rows;
   int32_t causal;        /* 0 or 1 */

@@ -116,6 +116,7 @@ _attention.argtypes = [_P] * 4 + [C.c_size_t, _P, _P]
 _w4.argtypes = uad_linear_w4.argtypes
 _pack_rows = struct.Struct("@3P3qPq4i").pack   # uad_kv_rows
 _pack_attn = struct.Struct("@4P3qf5i").pack    # uad_attn
+_LEAST = 2.0 ** -149   # fp32's least number above 0
 UAD_ETOOBIG = -7
 UAD_KV_BAD_PAGE, UAD_KV_BAD_SEQ = 1, 2
 UAD_W4_MAX_ROWS = 64
@@ -370,7 +371,7 @@ class PagedCache:
     def attention(self, seqs, q, out, workspace=None, scale=None, causal=True, window=0, key_mask=None, lse=None, status=None,
                   stream=None):
         """out = softmax(scale q k) v of the new tokens' queries [rows][n_heads * head_dim] over their sequences' pages
-        (scale None: 1 / sqrt(head_dim)). causal: a token sees the keys up to its own; window > 0: no more than so many; key_mask
+        (scale None: 1 / sqrt(head_dim); 0: all keys alike). causal: a token sees the keys up to its own; window > 0: no more than so many; key_mask
         uint8 [sequences][tokens that the table holds]: only where it is not 0. Where a token sees nothing, out is 0 and lse
         (float32 [rows][n_heads]) -inf. workspace: a uint8 tensor of attention_workspace bytes, not shared by calls that may
         run at the same time."""
@@ -406,7 +407,9 @@ class PagedCache:
                 wp = workspace.data_ptr()
             else:
                 wp = _tensor(workspace, "workspace", "uint8", (None,), g)
-        rc = _attention(self._at, seqs._at, _pack_attn(qp, op, lp, mp, ql, ol, ml, scale or 0.0, heads, n, 1 if causal else 0, window, 0),
+        # uad_attn takes 0 for the default: a scale of 0, or one that fp32 does not hold, is the least that it does
+        factor = 0.0 if scale is None else _LEAST if abs(scale) < _LEAST else scale
+        rc = _attention(self._at, seqs._at, _pack_attn(qp, op, lp, mp, ql, ol, ml, factor, heads, n, 1 if causal else 0, window, 0),
                         wp, wn, self._status(status), _stream_handle(stream))
         if rc:
             self._refused(rc, "attention")

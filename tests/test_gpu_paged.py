@@ -620,3 +620,24 @@ def test_heads_to_warps_or_to_ctas(heads, n, longest, new):
     q, out, lse, status = run_attention(c, max_len=longest)
     assert status == 0
     check_attention(c, q, out, lse)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("scale", [0.0, -0.0, 0, 1e-60])
+def test_a_scale_of_zero_is_not_the_default(scale, dtype):
+    """Every seen key has the same weight: the mean of the values, and the logarithm of their number. (The scores, below 2^10,
+    vanish beside 1 with fp32's least scale, so the errors are those of the sum, as for any scale.)"""
+    c = Case((8, 2, 64), 16, [40, 700, 1, 65], [3, 1, 1, 9], dtype, seed=18)
+    mask = torch.ones((c.n, c.width * c.page), dtype=torch.uint8, device="cuda")
+    mask[1, 100:650] = 0
+    q, out, lse, status = run_attention(c, mask=mask, scale=scale)
+    assert status == 0
+    mn = mask.cpu().numpy()
+    for t, (b, pos) in enumerate(paged.rows_of(c.lens, c.start)):
+        seen = np.flatnonzero(mn[b, :pos + 1])
+        for h in range(c.hq):
+            v = c.values[b][seen, h // 4]
+            want, size, n = v.mean(axis=0), np.abs(v).mean(axis=0), len(seen)
+            tol = 2 * (2.0 ** -20 + 2.0 ** -16 + n * 2.0 ** -23) * size + HALF[dtype] * np.abs(want) + TINY
+            assert np.all(np.abs(out[t, h * 64:(h + 1) * 64].double().cpu().numpy() - want) <= tol)
+            assert abs(float(lse[t, h]) - math.log(n)) <= 2.0 ** -20 + n * 2.0 ** -23 + 2.0 ** -22 * math.log(n)
