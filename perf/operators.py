@@ -199,7 +199,7 @@ def prepare(case, seed):
         if case["op"] == "append":
             s["rope"] = uad.rope(THETA, case["rot"])
         else:
-            s["ws"] = torch.empty(s["cache"].attention_workspace(s["seqs"], s["rows"], hq), dtype=torch.uint8, device="cuda")
+            s["ws"] = torch.empty(s["cache"].attention_workspace(s["seqs"], s["rows"], hq, case["window"]), dtype=torch.uint8, device="cuda")
     return s
 
 
