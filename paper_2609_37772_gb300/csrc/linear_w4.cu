@@ -97,7 +97,6 @@ __host__ __device__ inline size_t few_smem(int rows, int k) {
 
 template <int G, bool VEC>   // VEC: a chunk's scales, and its zeros, are read as one word
 __global__ void __launch_bounds__(32 * kW4Warps, 2) w4_few_kernel(const FewArgs f) {
-  constexpr int NT = 1;   // eights of tokens
   constexpr int PITCH = few_pitch<G>(), SLOT = 16 * PITCH, PG = kChunk / G, GS = G / 32;   // groups of a chunk, steps of a group
   extern __shared__ __align__(16) unsigned char smem[];
   pdl_wait();
@@ -225,14 +224,8 @@ __global__ void __launch_bounds__(32 * kW4Warps, 2) w4_few_kernel(const FewArgs 
   if (f.split > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 
   int slot = 0, buf = 0, i = 0;
-  float acc[NT][4] = {};
-  uint32_t x_at[NT], x_step[NT];   // a lane without a token reads zeros
-#pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    const bool is = 8 * n + g < a.M;
-    x_step[n] = is ? a.M * 64 : 0;
-    x_at[n] = is ? xs + (32 * n + lane) * 16 + kw * 4 * x_step[n] : ptx::su32(smem);
-  }
+  float acc[4] = {};
+  uint32_t x_step = g < a.M ? a.M * 64 : 0, x_at = g < a.M ? xs + lane * 16 + kw * 4 * x_step : ptx::su32(smem);   // a lane without a token reads zeros
   // One chunk, with its scales, and those to be loaded. The loop below is unrolled over gs: moving a word that is on its way
   // waits for it.
   const auto chunk = [&](const Groups<PG>* now, Groups<PG>* before, Groups<PG>* later) {
@@ -253,7 +246,7 @@ __global__ void __launch_bounds__(32 * kW4Warps, 2) w4_few_kernel(const FewArgs 
         else if constexpr (GS == 2) asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(w[h][0]), "=r"(w[h][1]) : "r"(at) : "memory");
         else w[h][0] = lds4(at);
       }
-      float sum[NT][4];
+      float sum[4];
       const uint32_t z0 = 0x43004300u | ((uint32_t)now[0].z >> (8 * j) & 15u) * 0x10001u, z1 = 0x43004300u | ((uint32_t)now[1].z >> (8 * j) & 15u) * 0x10001u;
 #pragma unroll
       for (int v = 0; v < GS; ++v) {
@@ -263,23 +256,17 @@ __global__ void __launch_bounds__(32 * kW4Warps, 2) w4_few_kernel(const FewArgs 
           a0[u >> 1][2 * (u & 1)] = sub2(nibbles(w[0][v] >> (4 * u)), z0);
           a0[u >> 1][2 * (u & 1) + 1] = sub2(nibbles(w[1][v] >> (4 * u)), z1);
         }
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          uint4 b;
-          asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(b.x), "=r"(b.y), "=r"(b.z), "=r"(b.w) : "r"(x_at[n] + (j * GS + v) * x_step[n]) : "memory");
-          if (v == 0) mma_bf16_first(sum[n], a0[0], b.x, b.y);
-          else mma_bf16_16816(sum[n], a0[0], b.x, b.y);
-          mma_bf16_16816(sum[n], a0[1], b.z, b.w);
-        }
+        uint4 b;
+        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(b.x), "=r"(b.y), "=r"(b.z), "=r"(b.w) : "r"(x_at + (j * GS + v) * x_step) : "memory");
+        if (v == 0) mma_bf16_first(sum, a0[0], b.x, b.y);
+        else mma_bf16_16816(sum, a0[0], b.x, b.y);
+        mma_bf16_16816(sum, a0[1], b.z, b.w);
       }
       const float s0 = __uint_as_float((uint32_t)(now[0].s >> (16 * j)) << 16), s1 = __uint_as_float((uint32_t)(now[1].s >> (16 * j)) << 16);
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int c = 0; c < 4; ++c) acc[n][c] = fmaf(sum[n][c], c < 2 ? s0 : s1, acc[n][c]);
+      for (int c = 0; c < 4; ++c) acc[c] = fmaf(sum[c], c < 2 ? s0 : s1, acc[c]);
     }
-#pragma unroll
-    for (int n = 0; n < NT; ++n) x_at[n] += 4 * f.wk * x_step[n];
+    x_at += 4 * f.wk * x_step;
   };
   const auto end_tile = [&]() {
     if (f.wk == 1) {
@@ -288,22 +275,18 @@ __global__ void __launch_bounds__(32 * kW4Warps, 2) w4_few_kernel(const FewArgs 
         const int row = tile * 16 + 8 * h + g;
         const float bias = a.bias && row < a.N ? a.bias[row] : 0.f;
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const int m = 8 * n + 2 * t + e;
-            if (m < a.M && row < a.N) a.out[(int64_t)m * a.N + row] = acc[n][2 * h + e] + bias;
-          }
+        for (int e = 0; e < 2; ++e) {
+          const int m = 2 * t + e;
+          if (m < a.M && row < a.N) a.out[(int64_t)m * a.N + row] = acc[2 * h + e] + bias;
+        }
       }
     } else {
       float* mine_red = red + (buf * kW4Warps + warp) * a.M * 16;
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int m = 8 * n + 2 * t + (e & 1);
-          if (m < a.M) mine_red[m * 16 + 8 * (e >> 1) + g] = acc[n][e];
-        }
+      for (int e = 0; e < 4; ++e) {
+        const int m = 2 * t + (e & 1);
+        if (m < a.M) mine_red[m * 16 + 8 * (e >> 1) + g] = acc[e];
+      }
       __syncthreads();   // the buffer before this one is read by nobody any more
       for (int j = threadIdx.x; j < a.M * 16 * f.per_cta; j += 32 * kW4Warps) {
         const int c = f.per_cta > 1 ? j / (a.M * 16) : 0, r = j - c * (a.M * 16), n = (tile - of_cta + c) * 16 + (r & 15), m = r >> 4;
@@ -330,11 +313,8 @@ __global__ void __launch_bounds__(32 * kW4Warps, 2) w4_few_kernel(const FewArgs 
       buf ^= 1;
     }
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) acc[n][e] = 0.f;
-      x_at[n] -= 4 * f.wk * mine * x_step[n];
-    }
+    for (int e = 0; e < 4; ++e) acc[e] = 0.f;
+    x_at -= 4 * f.wk * mine * x_step;
     tile += stride;
     i = 0;
     --rounds;
@@ -350,8 +330,7 @@ __global__ void __launch_bounds__(32 * kW4Warps, 2) w4_few_kernel(const FewArgs 
       }
   }
   if (f.wk > 1) {
-#pragma unroll
-    for (int n = 0; n < NT; ++n) x_step[n] = 0;
+    x_step = 0;
     while (rounds > 0) end_tile();   // a warp without a tile in the last round, or without chunks, still meets the others
   }
 }
@@ -912,7 +891,7 @@ cudaError_t launch_tc(const W4Args& a, cudaStream_t s) {
 template <int G>
 cudaError_t launch_group(const W4Args& a, cudaStream_t s) {
   const int tokens = (a.M + 7) / 8;
-  if constexpr (G > 32) if (tokens == 1) {   // groups of 32 take the stream longer: 1 token of 3648 x 14402 18 us against 14
+  if constexpr (G > 32) if (tokens == 1) {   // groups of 32: 1 token of 3648 x 14402 18.1 us from the stream against 14.8, of 4096 x 4096 7.0 against 7.7
     constexpr int PG = kChunk / G;   // groups of a chunk
     if (PG == 1 || (a.K % kChunk == 0 && reinterpret_cast<uintptr_t>(a.scale) % (2 * PG) == 0 && reinterpret_cast<uintptr_t>(a.zero) % PG == 0))
       return launch_few<G, true>(a, s);
