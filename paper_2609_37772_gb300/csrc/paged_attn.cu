@@ -1060,11 +1060,9 @@ cudaError_t launch_dh(const PagedAttnArgs& a, cudaStream_t s) {
     else e = launch_f32<DH, 2>(a, s);
   } else if (a.row_tiles == 1) {
     e = launch_tc<DH, 1>(a, s);
-  } else if (a.row_tiles == 2) {
-    e = launch_tc<DH, 2>(a, s);
   } else {
-    if constexpr (DH < 256) e = launch_tc<DH, 4>(a, s);
-    else e = cudaErrorInvalidValue;
+    if constexpr (DH == 256) e = launch_tc<DH, 2>(a, s);   // 16 rows at most
+    else e = a.row_tiles == 2 ? launch_tc<DH, 2>(a, s) : launch_tc<DH, 4>(a, s);
   }
   if (e != cudaSuccess || a.pieces == 1 || a.clustered) return e;
   const dim3 grid((unsigned)a.n_heads * a.p.max_new, DH / 64, a.p.n_seqs);
