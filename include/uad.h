@@ -417,7 +417,7 @@ int uad_set_prefix_paged(uad_ctx* ctx, int32_t robot, const uad_kv_pages* layers
  * first, which has to stay within fp32 by itself, and then scaled. A row of x with infinities gives infinities or NaN. x and q
  * 16-byte aligned. 1 <= M <= UAD_W4_MAX_ROWS, N >= 1, K % group == 0,
  * group 32, 64 or 128, K <= 2^30, N * K <= 2^35. Asynchronous on `stream` and in its order; allocates nothing; may be captured.
- * Errors: UAD_EINVAL, UAD_ETOOBIG (M: dequantise and use uad_linear), UAD_ECUDA. */
+ * Errors: UAD_EINVAL, UAD_ETOOBIG (M: give the rows to several calls), UAD_ECUDA. */
 #define UAD_W4_MAX_ROWS 64
 int uad_linear_w4(const void* x, const uint8_t* q, const uint16_t* scale, const uint8_t* zero, const float* bias,
                   float* out, int32_t M, int32_t N, int32_t K, int32_t group, void* stream);

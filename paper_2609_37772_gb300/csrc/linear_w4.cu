@@ -58,6 +58,7 @@ __device__ __forceinline__ uint32_t sub2(uint32_t x, uint32_t y) {
 // q - zero (0x4300 | q is 128 + q; less 128 + zero). The tokens stay as they are, but for their order. A group's products are exact and
 // summed in fp32, and the sum is then scaled. Products of q itself would save the subtractions, but sums of q x cancel against zero
 // times the tokens' sum: a large token whose weights are all zero would take the small ones' bits.
+// 1 token: 2048 x 32768 in groups of 128 13.3 us (2.65 TB/s), 4096 x 4096 6.3, 1024 x 2560 3.1; 8 of 2048 x 32768 14.4.
 //
 // A tile of 16 rows is walked by wk of a CTA's warps, which take its chunks in turn and add up in shared memory: one, where
 // there are tiles enough for every warp, which saves the adding. A warp's copies run on from tile to tile. Where
