@@ -257,7 +257,7 @@ int uad_kv_append(const uad_kv_pages* pages, const uad_kv_seqs* seqs, const uad_
   const bool in32 = rows->dtype == UAD_DTYPE_F32, out32 = a.p.dtype == F32;
   const cudaError_t e = in32 ? (out32 ? launch_k(append_kernel<F32, F32>, grid, 256, 0, s, a, r) : launch_k(append_kernel<F32, BF16>, grid, 256, 0, s, a, r))
                              : (out32 ? launch_k(append_kernel<BF16, F32>, grid, 256, 0, s, a, r) : launch_k(append_kernel<BF16, BF16>, grid, 256, 0, s, a, r));
-  return e == cudaSuccess ? UAD_OK : UAD_ECUDA;
+  return launched(e);
 }
 
 }  // extern "C"

@@ -50,5 +50,11 @@ int paged_args(const uad_kv_pages* pages, const uad_kv_seqs* seqs, int n_rows, b
 cudaError_t launch_kv_gather(const PagedArgs& p, const int* table, int n, void* k, void* v, cudaStream_t s);
 // Whether p is memory of the current device.
 bool on_current_device(const void* p);
+// What an entry returns for its launches. Their error is this call's: the next one, which may ask for the last error, does not find it.
+inline int launched(cudaError_t e) {
+  if (e == cudaSuccess) return UAD_OK;
+  cudaGetLastError();
+  return UAD_ECUDA;
+}
 
 }  // namespace uad

@@ -941,7 +941,7 @@ int uad_linear_w4(const void* x, const uint8_t* q, const uint16_t* scale, const 
   const W4Args a{static_cast<const __nv_bfloat16*>(x), q, reinterpret_cast<const __nv_bfloat16*>(scale), zero, bias, out, M, N, K, group};
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const cudaError_t e = group == 32 ? launch_group<32>(a, s) : group == 64 ? launch_group<64>(a, s) : launch_group<128>(a, s);
-  return e == cudaSuccess ? UAD_OK : UAD_ECUDA;
+  return launched(e);
 }
 
 int uad_quantize_w4(const float* w, int32_t K, int32_t N, int32_t group, uint8_t* q, uint16_t* scale, uint8_t* zero) {

@@ -1092,7 +1092,7 @@ int uad_paged_attention(const uad_kv_pages* pages, const uad_kv_seqs* seqs, cons
   a.part_ml = reinterpret_cast<float2*>(a.part_o + (int64_t)a.p.n_rows * a.n_heads * a.pieces * a.p.dh);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const cudaError_t e = a.p.dh == 64 ? launch_dh<64>(a, s) : a.p.dh == 128 ? launch_dh<128>(a, s) : launch_dh<256>(a, s);
-  return e == cudaSuccess ? UAD_OK : UAD_ECUDA;
+  return launched(e);
 }
 
 }  // extern "C"

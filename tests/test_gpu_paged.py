@@ -8,6 +8,7 @@ step; the scaling rounds once): d. Probabilities then are off by a factor e^d at
 denominator), by exp's own error (2^-20 with the scores' magnitudes here) and by 2^-16 where they are the sum of two bf16;
 sums of n terms by n 2^-23. The output is off by that much of sum p |v|, then by the type's half step.
 """
+import ctypes as C
 import math
 
 import numpy as np
@@ -641,3 +642,36 @@ def test_a_scale_of_zero_is_not_the_default(scale, dtype):
             tol = 2 * (2.0 ** -20 + 2.0 ** -16 + n * 2.0 ** -23) * size + HALF[dtype] * np.abs(want) + TINY
             assert np.all(np.abs(out[t, h * 64:(h + 1) * 64].double().cpu().numpy() - want) <= tol)
             assert abs(float(lse[t, h]) - math.log(n)) <= 2.0 ** -20 + n * 2.0 ** -23 + 2.0 ** -22 * math.log(n)
+
+
+def test_a_call_that_cannot_be_launched_leaves_no_error_behind():
+    """A call on the legacy stream while a stream that it waits for is captured is refused by the runtime. The error is that call's alone: uad_linear,
+    which asks for the last error, does not find it."""
+    rt = C.CDLL(next(m.split()[-1] for m in open("/proc/self/maps") if "libcudart.so" in m))   # the runtime that torch has loaded
+    c = Case((8, 2, 64), 16, [40], [1], seed=19, rows_behind=0)
+    s, cache, rope = c.sequences(), uad.PagedCache(c.k, c.v), uad.rope(10000.0, 64)
+    q, k = c.randn(1, 512), c.randn(1, 128)
+    out = torch.empty_like(q)
+    ws = torch.empty(max(1, cache.attention_workspace(s, 1, 8)), dtype=torch.uint8, device="cuda")
+    w, scale, y = torch.zeros(32, 256, dtype=torch.uint8, device="cuda"), torch.ones(32, 8, device="cuda").bfloat16(), torch.empty(1, 32, device="cuda")
+    tiled = torch.from_numpy(uad.tile_weight(np.zeros((512, 128), np.float32)).view(np.int16)).cuda()
+    z = torch.full((1, 128), 7.5, device="cuda")
+    st, graph = C.c_void_p(), C.c_void_p()
+    assert rt.cudaStreamCreate(C.byref(st)) == 0   # a blocking stream: the legacy stream waits for it, which a capture cannot have
+    calls = [lambda: cache.append(s, k, k, q=q, q_out=out, rope=rope), lambda: cache.attention(s, q, out, ws), lambda: uad.linear_w4(q, w, scale, y)]
+    for call in calls:
+        call()
+    torch.cuda.synchronize()
+    for call in calls:
+        assert rt.cudaStreamBeginCapture(st, 0) == 0
+        try:
+            with pytest.raises(uad.UADError) as e:
+                call()
+            assert e.value.code == uad.UAD_ECUDA
+        finally:
+            rt.cudaStreamEndCapture(st, C.byref(graph))
+            rt.cudaGetLastError()
+        assert uad.uad_linear(q.data_ptr(), tiled.data_ptr(), None, z.fill_(7.5).data_ptr(), 1, 128, 512, torch.cuda.current_stream().cuda_stream) == 0
+        torch.cuda.synchronize()
+        assert bool((z == 0).all())
+    assert rt.cudaStreamDestroy(st) == 0
