@@ -46,6 +46,7 @@ extern "C" {
 
 #define UAD_DTYPE_F32 0
 #define UAD_DTYPE_BF16 1
+#define UAD_DTYPE_E4M3 2 /* pages of an 8-bit cache (uad_kv_pages8) alone */
 
 #define UAD_MAX_STEPS 64     /* largest step budget N_i */
 
@@ -398,6 +399,85 @@ int64_t uad_paged_attention_workspace(const uad_kv_pages* pages, const uad_kv_se
  * Errors: UAD_EINVAL (arguments, workspace too small), UAD_ECUDA. */
 int uad_paged_attention(const uad_kv_pages* pages, const uad_kv_seqs* seqs, const uad_attn* attn, void* workspace,
                         size_t workspace_bytes, int32_t* status, void* stream);
+
+/* ---- The paged cache held in 8 bits ------------------------------------------------------------------
+ * Keys and values as e4m3 codes with a scale for each block of tokens and head: token = scale * code. Half the memory
+ * and the reading of a bf16 cache, for many or long episodes. A block is `block` slots of a page from a multiple of it on (the last one
+ * of a page ends with the page: blocks never span pages), and the scale of head h of block i of page p is at
+ * k_scale + p * scale_page_stride + i * scale_block_stride + h * scale_head_stride, of the values at the same place of v_scale. Any scale
+ * that is finite and above 0 is read as it is (those below 2^-100 cost precision); the append writes powers of two. The code
+ * 0x7f or 0xff is NaN. */
+typedef struct uad_kv_pages8 {
+  uad_kv_pages pages;    /* dtype UAD_DTYPE_E4M3; strides in elements, which are bytes */
+  float *k_scale, *v_scale;   /* 4-byte aligned */
+  int64_t scale_page_stride, scale_block_stride, scale_head_stride;   /* > 0, in elements */
+  int32_t block;         /* 16, 32 or 64 tokens */
+  int32_t pad;
+} uad_kv_pages8;
+
+/* uad_kv_append into an 8-bit cache: queries are rotated into q_out in bf16, keys and values rounded to the nearest code (ties to even)
+ * of their block's scale: the least power of two s (2^-100 at the least) with 448 s >= the largest of the block's new values, for keys
+ * that are rotated twice the largest before the rotation (which grows no value by more than sqrt(2)). Infinities and NaN do not count
+ * and are stored as NaN. Where the block holds earlier tokens of the sequence, its scale does not fall below theirs, and where it
+ * grows they are rounded to it: exactly but for values 2^-15 of the block's largest and below, so that what a cache holds hardly depends on how many
+ * calls wrote it. A block that is written therefore belongs to one sequence: it must not stand in another table of the same append, nor
+ * be read meanwhile; whole blocks before it may be shared. Errors: UAD_EINVAL (arguments), UAD_ECUDA. */
+int uad_kv_append8(const uad_kv_pages8* pages, const uad_kv_seqs* seqs, const uad_kv_rows* rows, const uad_rope* rope,
+                   int32_t* status, void* stream);
+
+/* Attention through a window that leaves the first `sinks` tokens of a sequence visible: uad_paged_attention but that a token at
+ * position p sees, with window > 0, the keys j > p - window and the keys j < sinks (causal, len and key_mask hold as before). What lies
+ * between is not read, nor is its place in the table. sinks 0 or window 0: uad_paged_attention. A workspace without a window is enough for
+ * every window and sinks. */
+int64_t uad_paged_attention_sinks_workspace(const uad_kv_pages* pages, const uad_kv_seqs* seqs, const uad_attn* attn, int32_t sinks);
+int uad_paged_attention_sinks(const uad_kv_pages* pages, const uad_kv_seqs* seqs, const uad_attn* attn, int32_t sinks, void* workspace,
+                              size_t workspace_bytes, int32_t* status, void* stream);
+
+/* The same over an 8-bit cache; q and out are bf16. Products of codes and queries (as f16 with a power of two a row) are exact, sums and softmax
+ * in fp32, weights rounded to 2^-12 (f16). */
+int64_t uad_paged_attention8_workspace(const uad_kv_pages8* pages, const uad_kv_seqs* seqs, const uad_attn* attn, int32_t sinks);
+int uad_paged_attention8(const uad_kv_pages8* pages, const uad_kv_seqs* seqs, const uad_attn* attn, int32_t sinks, void* workspace,
+                         size_t workspace_bytes, int32_t* status, void* stream);
+
+/* ---- The pages' bookkeeping on the GPU -----------------------------------------------------------------
+ * Free pages of a cache (of all its layers: one table serves them) as a ring: ring[(first + i) % n_pages], i < count, with
+ * state = {first, count}. Every page is on it once at most. */
+typedef struct uad_page_pool {
+  int32_t* ring;           /* [n_pages] page numbers */
+  const int32_t* state;    /* [2] */
+  int32_t* state_out;      /* [2] after the call; may be state */
+  int32_t n_pages;         /* 1..2^30 */
+  int32_t page_size;       /* 1..65536 */
+} uad_page_pool;
+/* Sequence b has len[b] tokens and shall have want[b]. The arrays are device memory. */
+typedef struct uad_kv_wanted {
+  int32_t* table;          /* [n_seqs][table_stride], of which table_width entries: pages that a sequence takes are written behind those that it
+                              has; those that it gives back stay where they are */
+  const int32_t* len;
+  const int32_t* want;     /* [n_seqs], 0..table_width * page_size */
+  int32_t* len_out;        /* [n_seqs] after the call: want, or len where nothing was done; may be len or want */
+  int32_t* start;          /* [n_seqs + 1] first rows of the new tokens, as uad_kv_seqs takes them */
+  int64_t* slot;           /* [n_rows] page * page_size + slot of each new token, -1 for rows of nobody; NULL: not wanted */
+  int32_t* row_seq;        /* [n_rows] the sequence of each row, -1 for rows of nobody; NULL: not wanted */
+  int32_t* row_pos;        /* [n_rows] its position, -1 for rows of nobody; NULL: not wanted */
+  int64_t table_stride;
+  int32_t n_seqs;          /* 0..65535 */
+  int32_t table_width;     /* as in uad_kv_seqs */
+  int32_t n_rows;          /* rows that the token tensors hold */
+  int32_t pad;
+} uad_kv_wanted;
+/* More findings for the status word: */
+#define UAD_KV_NO_ROOM 4  /* no page or no row for a sequence that shall grow: it stays as it was */
+#define UAD_KV_BAD_POOL 8 /* state outside of the ring, or more pages given back than it has places: they are dropped */
+
+/* Give each sequence the pages of want[b] tokens, from the front of the ring in the order of the sequences, or its last pages back to
+ * the end of the ring (want below len: a rejected draft, an episode's end); pages that others share must not be given back. With it the lengths,
+ * first rows and slot maps of the step, so that a captured graph needs nothing from the host. Sequences are served in order: one whose pages,
+ * summed with those asked for before it, are more than were free before the call, or whose rows likewise do not fit n_rows, stays as it was
+ * (UAD_KV_NO_ROOM). A sequence with a length or want outside its table stays as it was too (UAD_KV_BAD_SEQ). Whole numbers, the same in
+ * every run. Asynchronous on `stream` and in its order; allocates nothing; may be captured. No two calls on one ring at the same time.
+ * Errors: UAD_EINVAL, UAD_ECUDA. */
+int uad_kv_resize(const uad_page_pool* pool, const uad_kv_wanted* wanted, int32_t* status, void* stream);
 
 /* Bind robot `robot`'s prefix from pages: uad_set_prefix_kv of the first arch.prefix_len tokens of a sequence whose keys and
  * values a vision-language model has appended layer by layer. layers: the caches of the arch's n_layers layers, of one type and

@@ -19,4 +19,5 @@ Modules
   clock.py  action availability latency under the control-time alignment clock
             (Sec. 5.1 Metrics, App. C.3) and the latency model (App. B, Eqs. 11-12)
   paged.py  the paged key-value cache's rotation and attention and the 4-bit projection's weights, which the paper has not
+  paged8.py the paged cache in 8 bits (codes, scales, append) and the bookkeeping of its pages, which the paper has not
 """

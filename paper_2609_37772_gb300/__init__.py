@@ -21,6 +21,7 @@ _lib = C.CDLL(LIB_PATH)
 UAD_OK, UAD_EINVAL, UAD_ESTATE, UAD_ENOMEM, UAD_ECUDA, UAD_ETIMEDOUT, UAD_ENONFINITE = 0, -22, -1, -12, -5, -110, -33
 KIND = {"adarms": 0, "dit": 1, "concat": 2}
 DTYPE = {"f32": 0, "bf16": 1}
+UAD_DTYPE_E4M3 = 2
 MAX_STEPS = 64
 
 _I32, _P = C.c_int32, C.c_void_p
@@ -72,6 +73,20 @@ class uad_attn(C.Structure):
                 ("window", _I32), ("pad", _I32)]
 
 
+class uad_kv_pages8(C.Structure):
+    _fields_ = [("pages", uad_kv_pages), ("k_scale", _P), ("v_scale", _P), ("scale_page_stride", C.c_int64),
+                ("scale_block_stride", C.c_int64), ("scale_head_stride", C.c_int64), ("block", _I32), ("pad", _I32)]
+
+
+class uad_page_pool(C.Structure):
+    _fields_ = [("ring", _P), ("state", _P), ("state_out", _P), ("n_pages", _I32), ("page_size", _I32)]
+
+
+class uad_kv_wanted(C.Structure):
+    _fields_ = [(n, _P) for n in ("table", "len", "want", "len_out", "start", "slot", "row_seq", "row_pos")] + \
+               [("table_stride", C.c_int64), ("n_seqs", _I32), ("table_width", _I32), ("n_rows", _I32), ("pad", _I32)]
+
+
 def _fn(name, res, *args):
     f = getattr(_lib, name)
     f.restype = res
@@ -105,6 +120,13 @@ uad_kv_append = _fn("uad_kv_append", C.c_int, _PAGES, _SEQS, C.POINTER(uad_kv_ro
 uad_paged_attention_workspace = _fn("uad_paged_attention_workspace", C.c_int64, _PAGES, _SEQS, C.POINTER(uad_attn))
 uad_paged_attention = _fn("uad_paged_attention", C.c_int, _PAGES, _SEQS, C.POINTER(uad_attn), _P, C.c_size_t, _P, _P)
 uad_set_prefix_paged = _fn("uad_set_prefix_paged", C.c_int, _P, _I32, _PAGES, _I32, _P, _I32)
+_ATTN, _PAGES8 = C.POINTER(uad_attn), C.POINTER(uad_kv_pages8)
+uad_paged_attention_sinks_workspace = _fn("uad_paged_attention_sinks_workspace", C.c_int64, _PAGES, _SEQS, _ATTN, _I32)
+uad_paged_attention_sinks = _fn("uad_paged_attention_sinks", C.c_int, _PAGES, _SEQS, _ATTN, _I32, _P, C.c_size_t, _P, _P)
+uad_kv_append8 = _fn("uad_kv_append8", C.c_int, _PAGES8, _SEQS, C.POINTER(uad_kv_rows), C.POINTER(uad_rope), _P, _P)
+uad_paged_attention8_workspace = _fn("uad_paged_attention8_workspace", C.c_int64, _PAGES8, _SEQS, _ATTN, _I32)
+uad_paged_attention8 = _fn("uad_paged_attention8", C.c_int, _PAGES8, _SEQS, _ATTN, _I32, _P, C.c_size_t, _P, _P)
+uad_kv_resize = _fn("uad_kv_resize", C.c_int, C.POINTER(uad_page_pool), C.POINTER(uad_kv_wanted), _P, _P)
 uad_linear_w4 = _fn("uad_linear_w4", C.c_int, _P, _P, _P, _P, _P, _P, _I32, _I32, _I32, _I32, _P)
 uad_quantize_w4 = _fn("uad_quantize_w4", C.c_int, _P, _I32, _I32, _I32, _P, _P, _P)
 # The same entries for the wrappers below, with structures as addresses or packed bytes: a decoding step makes several such
@@ -114,11 +136,19 @@ _append.restype = _attention.restype = _w4.restype = C.c_int
 _append.argtypes = [_P] * 6
 _attention.argtypes = [_P] * 4 + [C.c_size_t, _P, _P]
 _w4.argtypes = uad_linear_w4.argtypes
+_append8, _attention8, _attention_sinks, _resize = (_lib[n] for n in ("uad_kv_append8", "uad_paged_attention8", "uad_paged_attention_sinks",
+                                                                      "uad_kv_resize"))
+_append8.restype = _attention8.restype = _attention_sinks.restype = _resize.restype = C.c_int
+_append8.argtypes = _append.argtypes
+_attention8.argtypes = _attention_sinks.argtypes = [_P] * 3 + [_I32, _P, C.c_size_t, _P, _P]
+_resize.argtypes = [_P] * 4
+_pack_wanted = struct.Struct("@8Pq4i").pack    # uad_kv_wanted
+_pack_pool = struct.Struct("@3P2i").pack       # uad_page_pool
 _pack_rows = struct.Struct("@3P3qPq4i").pack   # uad_kv_rows
 _pack_attn = struct.Struct("@4P3qf5i").pack    # uad_attn
 _LEAST = 2.0 ** -149   # fp32's least number above 0
 UAD_ETOOBIG = -7
-UAD_KV_BAD_PAGE, UAD_KV_BAD_SEQ = 1, 2
+UAD_KV_BAD_PAGE, UAD_KV_BAD_SEQ, UAD_KV_NO_ROOM, UAD_KV_BAD_POOL = 1, 2, 4, 8
 UAD_W4_MAX_ROWS = 64
 
 EXPORTS = ["uad_version", "uad_last_error", "uad_init", "uad_set_prefix_kv", "uad_prepare_times",
@@ -126,7 +156,9 @@ EXPORTS = ["uad_version", "uad_last_error", "uad_init", "uad_set_prefix_kv", "ua
            "uad_launches_per_chunk", "uad_destroy", "uad_plan_step", "uad_profile_chunk",
            "uad_tile_weight", "uad_linear", "uad_linear_static_scratch", "uad_set_wait_limit",
            "uad_linear_status", "uad_linear_check", "uad_so3_check", "uad_rope_init", "uad_kv_append",
-           "uad_paged_attention_workspace", "uad_paged_attention", "uad_set_prefix_paged", "uad_linear_w4", "uad_quantize_w4"]
+           "uad_paged_attention_workspace", "uad_paged_attention", "uad_set_prefix_paged", "uad_linear_w4", "uad_quantize_w4",
+           "uad_kv_append8", "uad_paged_attention8_workspace", "uad_paged_attention8", "uad_paged_attention_sinks_workspace",
+           "uad_paged_attention_sinks", "uad_kv_resize"]
 
 
 def tile_weight(w):
@@ -219,7 +251,7 @@ def _tensor(t, what, dtype, shape, device=None, rows=False):
     (rows: its rows alone, which may be apart) and on `device` (the GPU of the tensors beside it)."""
     if not _dtypes:
         import torch
-        _dtypes.update({n: getattr(torch, n) for n in ("float32", "bfloat16", "int32", "uint8")})
+        _dtypes.update({n: getattr(torch, n) for n in ("float32", "bfloat16", "int32", "uint8", "int64", "float8_e4m3fn")})
     if t.dtype is not _dtypes[dtype]:
         raise ValueError(f"{what}: expected {dtype} elements, got {t.dtype}")
     if t.shape != shape and (t.dim() != len(shape) or any(a is not None and a != b for a, b in zip(shape, t.shape))):
@@ -263,29 +295,53 @@ class Sequences:
 
 
 class PagedCache:
-    """One layer's paged key-value cache on the GPU: k and v [n_pages][page_size][n_kv_heads][head_dim], float32 or
-    bfloat16, the last dimension contiguous, the others in any order (a view of [pages][heads][slots][dim], or of keys and
-    values in one tensor), both with the same strides. The tensors stay the caller's. Calls are asynchronous on `stream`
+    """One layer's paged key-value cache on the GPU: k and v [n_pages][page_size][n_kv_heads][head_dim], float32, bfloat16 or
+    float8_e4m3fn, the last dimension contiguous, the others in any order (a view of [pages][heads][slots][dim], or of keys and
+    values in one tensor), both with the same strides. float8_e4m3fn pages have their scales in k_scale and v_scale, float32
+    [n_pages][blocks of a page][n_kv_heads] in any order, both with the same strides: one for each `block` (16, 32 or 64) slots of a page
+    and head; their queries and outputs are bfloat16. The tensors stay the caller's. Calls are asynchronous on `stream`
     (None: the legacy default stream); `status`: an int32 tensor of one element that device-side findings
     (UAD_KV_BAD_PAGE, UAD_KV_BAD_SEQ) are added to. On a stream of their own, the caller keeps the tensors until the work is done."""
 
-    def __init__(self, k, v):
+    def __init__(self, k, v, k_scale=None, v_scale=None, block=16):
         if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.stride() != v.stride() or k.device != v.device:
             raise ValueError("pages: k and v must be [n_pages][page_size][n_kv_heads][head_dim] of one type, device and strides")
         name = str(k.dtype)[6:]
-        if name not in ("float32", "bfloat16"):
-            raise ValueError(f"pages: expected float32 or bfloat16 elements, got {k.dtype}")
+        if name not in ("float32", "bfloat16", "float8_e4m3fn"):
+            raise ValueError(f"pages: expected float32 or bfloat16 elements, or float8_e4m3fn with scales, got {k.dtype}")
         if k.stride(3) != 1 or min(k.stride()) < 1:
             raise ValueError("pages: the last dimension must be contiguous")
+        eight = name == "float8_e4m3fn"
+        if (k_scale is not None) != eight or (v_scale is not None) != eight:
+            raise ValueError("pages: float8_e4m3fn goes with k_scale and v_scale, other types without")
+        if eight:
+            if block not in (16, 32, 64):
+                raise ValueError(f"pages: a block has 16, 32 or 64 tokens, not {block}")
+            shape = (k.shape[0], -(-k.shape[1] // block), k.shape[2])
+            for x, what in ((k_scale, "k_scale"), (v_scale, "v_scale")):
+                if str(x.dtype) != "torch.float32" or x.shape != shape or x.device != k.device or x.stride() != k_scale.stride() or min(x.stride()) < 1:
+                    raise ValueError(f"{what}: expected float32 elements of shape {list(shape)} beside the pages, k_scale and v_scale of the same "
+                                     f"strides, got {x.dtype} {list(x.shape)}")
         if k.device.type != "cuda":
             raise ValueError(f"pages: must be on the GPU, is on {k.device}")
-        self.k, self.v, self.device, self.dtype = k, v, k.device, k.dtype
+        self.k, self.v, self.device = k, v, k.device
+        self.k_scale, self.v_scale, self.block = k_scale, v_scale, block if eight else None
         self._gpu = k.get_device()
         self.page_size, self.n_kv_heads, self.head_dim = k.shape[1], k.shape[2], k.shape[3]
         self.pages = uad_kv_pages(k=k.data_ptr(), v=v.data_ptr(), page_stride=k.stride(0), slot_stride=k.stride(1),
-                                  head_stride=k.stride(2), dtype=DTYPE["f32" if name == "float32" else "bf16"],
+                                  head_stride=k.stride(2), dtype=UAD_DTYPE_E4M3 if eight else DTYPE["f32" if name == "float32" else "bf16"],
                                   n_pages=k.shape[0], page_size=k.shape[1], n_kv_heads=k.shape[2], head_dim=k.shape[3])
-        self._at = C.addressof(self.pages)
+        self._append = _append
+        if eight:
+            import torch
+            self.dtype = torch.bfloat16   # of queries and outputs
+            self.pages8 = uad_kv_pages8(pages=self.pages, k_scale=k_scale.data_ptr(), v_scale=v_scale.data_ptr(),
+                                        scale_page_stride=k_scale.stride(0), scale_block_stride=k_scale.stride(1),
+                                        scale_head_stride=k_scale.stride(2), block=block)
+            self._append = _append8
+        else:
+            self.dtype = k.dtype
+        self._at = C.addressof(self.pages8 if eight else self.pages)
 
     def _rows(self, t, what, dtype, n, width):
         """Address and row stride of a [n][width] tensor of `dtype` whose rows may be apart."""
@@ -316,7 +372,9 @@ class PagedCache:
     def append(self, seqs, k=None, v=None, q=None, q_out=None, rope=None, status=None, stream=None):
         """Write the new tokens' keys and values [rows][n_kv_heads * head_dim] into their pages and their queries
         [rows][n_heads * head_dim] into q_out, keys and queries rotated by `rope` (None: not). float32 or bfloat16 rows,
-        which may be parts of a fused projection; q_out in the cache's type (q itself only where that is the rows')."""
+        which may be parts of a fused projection; q_out in the cache's type, bfloat16 beside 8 bits (q itself only where that is the rows').
+        An 8-bit cache's blocks get the least power of two as scale that holds their tokens; a block that is written belongs to one
+        sequence."""
         g = self._gpu
         if seqs._gpu != g:
             raise ValueError(f"sequences: must be on {self.device}, are on {seqs.device}")
@@ -356,23 +414,25 @@ class PagedCache:
                 heads = self._heads(q)
                 qp, ql = self._rows(q, "q", kind, n, wide[1])
                 op, ol = self._rows(q_out, "q_out", self.dtype, n, wide[1])
-        rc = _append(self._at, seqs._at, _pack_rows(qp, kp, vp, ql, kl, vl, op, ol, code, heads, n, 0),
+        rc = self._append(self._at, seqs._at, _pack_rows(qp, kp, vp, ql, kl, vl, op, ol, code, heads, n, 0),
                      None if rope is None else C.addressof(rope), self._status(status), _stream_handle(stream))
         if rc:
             self._refused(rc, "append")
 
-    def attention_workspace(self, seqs, rows, n_heads, window=0):
-        """Bytes of the workspace that attention of these sizes needs (0 is possible). Without a window: enough for every window."""
-        n = uad_paged_attention_workspace(self.pages, seqs.seqs, uad_attn(n_heads=n_heads, n_rows=rows, window=window))
+    def attention_workspace(self, seqs, rows, n_heads, window=0, sinks=0):
+        """Bytes of the workspace that attention of these sizes needs (0 is possible). Without a window: enough for every window and sinks."""
+        attn = uad_attn(n_heads=n_heads, n_rows=rows, window=window)
+        n = uad_paged_attention_sinks_workspace(self.pages, seqs.seqs, attn, sinks) if self.block is None else \
+            uad_paged_attention8_workspace(self.pages8, seqs.seqs, attn, sinks)
         if n < 0:
             self._refused(n, "attention_workspace")
         return n
 
     def attention(self, seqs, q, out, workspace=None, scale=None, causal=True, window=0, key_mask=None, lse=None, status=None,
-                  stream=None):
+                  stream=None, sinks=0):
         """out = softmax(scale q k) v of the new tokens' queries [rows][n_heads * head_dim] over their sequences' pages
-        (scale None: 1 / sqrt(head_dim); 0: all keys alike). causal: a token sees the keys up to its own; window > 0: no more than so many; key_mask
-        uint8 [sequences][tokens that the table holds]: only where it is not 0. Where a token sees nothing, out is 0 and lse
+        (scale None: 1 / sqrt(head_dim); 0: all keys alike). causal: a token sees the keys up to its own; window > 0: no more than so many, and the
+        sequence's first `sinks`; key_mask uint8 [sequences][tokens that the table holds]: only where it is not 0. Where a token sees nothing, out is 0 and lse
         (float32 [rows][n_heads]) -inf. workspace: a uint8 tensor of attention_workspace bytes, not shared by calls that may
         run at the same time."""
         g = self._gpu
@@ -409,10 +469,67 @@ class PagedCache:
                 wp = _tensor(workspace, "workspace", "uint8", (None,), g)
         # uad_attn takes 0 for the default: a scale of 0, or one that fp32 does not hold, is the least that it does
         factor = 0.0 if scale is None else _LEAST if abs(scale) < _LEAST else scale
-        rc = _attention(self._at, seqs._at, _pack_attn(qp, op, lp, mp, ql, ol, ml, factor, heads, n, 1 if causal else 0, window, 0),
-                        wp, wn, self._status(status), _stream_handle(stream))
+        attn = _pack_attn(qp, op, lp, mp, ql, ol, ml, factor, heads, n, 1 if causal else 0, window, 0)
+        if self.block is not None:
+            rc = _attention8(self._at, seqs._at, attn, sinks, wp, wn, self._status(status), _stream_handle(stream))
+        elif sinks:
+            rc = _attention_sinks(self._at, seqs._at, attn, sinks, wp, wn, self._status(status), _stream_handle(stream))
+        else:
+            rc = _attention(self._at, seqs._at, attn, wp, wn, self._status(status), _stream_handle(stream))
         if rc:
             self._refused(rc, "attention")
+
+
+class PagePool:
+    """The free pages of a cache (of all its layers, which share a table) on the GPU: ring int32 [n_pages] holds their numbers at
+    (first + i) % n_pages, i < count; state int32 [2] = first, count. The tensors stay the caller's: ring = arange(n_pages) and state =
+    [0, n_pages] say that every page is free."""
+
+    def __init__(self, ring, state, page_size):
+        if ring.dim() != 1 or ring.shape[0] < 1:
+            raise ValueError(f"ring: expected the numbers of one or more pages, got shape {list(ring.shape)}")
+        self._ring = _tensor(ring, "ring", "int32", (None,))
+        self._gpu = ring.get_device()
+        self._state = _tensor(state, "state", "int32", (2,), self._gpu)
+        self.ring, self.state, self.page_size, self.n_pages = ring, state, page_size, ring.shape[0]
+
+    def resize(self, table, length, want, start, length_out=None, state_out=None, slot=None, row_seq=None, row_pos=None, rows=None, status=None,
+               stream=None):
+        """Give every sequence the pages of want tokens: table int32 [n][pages], length and want int32 [n] (tokens that it has and shall
+        have), start int32 [n + 1] (out: first rows of the new tokens, as Sequences takes them). length_out, state_out: where the new lengths and
+        the pool's new state go (None: in place). slot int64, row_seq and row_pos int32 [rows]: each new token's place in the cache
+        (page * page_size + slot), sequence and position, -1 behind the last one. rows: what the token tensors hold (None: the
+        slot maps' length; without one, no limit). Sequences that find no page or row stay as they were (UAD_KV_NO_ROOM in `status`);
+        want below length gives pages back."""
+        g, n = self._gpu, length.shape[0] if length.dim() else -1
+        whole = _dtypes["int32"]
+        # the usual tensors checked at once; where a check fails, _tensor says which or finds them sound
+        if (table.dtype is whole and table.dim() == 2 and table.shape[0] == n and table.is_contiguous() and length.dtype is whole and
+                length.dim() == 1 and length.is_contiguous() and want.dtype is whole and want.shape == (n,) and want.is_contiguous() and
+                start.dtype is whole and start.shape == (n + 1,) and start.is_contiguous() and
+                table.get_device() == g == length.get_device() and want.get_device() == g == start.get_device()):
+            tp, lp, wp, sp = table.data_ptr(), length.data_ptr(), want.data_ptr(), start.data_ptr()
+        else:
+            tp = _tensor(table, "table", "int32", (n, None), g, True)
+            lp = _tensor(length, "length", "int32", (n,), g)
+            wp = _tensor(want, "want", "int32", (n,), g)
+            sp = _tensor(start, "start", "int32", (n + 1,), g)
+        op = lp if length_out is None else _tensor(length_out, "length_out", "int32", (n,), g)
+        qp = self._state if state_out is None else _tensor(state_out, "state_out", "int32", (2,), g)
+        maps = []
+        for t, what, kind in ((slot, "slot", "int64"), (row_seq, "row_seq", "int32"), (row_pos, "row_pos", "int32")):
+            if t is not None:
+                if rows is None:
+                    rows = t.shape[0] if t.dim() else -1
+                maps.append(_tensor(t, what, kind, (rows,), g))
+            else:
+                maps.append(None)
+        rc = _resize(_pack_pool(self._ring, self._state, qp, self.n_pages, self.page_size),
+                     _pack_wanted(tp, lp, wp, op, sp, *[m or 0 for m in maps], table.stride(0) if n > 1 else max(1, table.shape[1]), n, table.shape[1],
+                                  0x7fffffff if rows is None else rows, 0),
+                     None if status is None else _tensor(status, "status", "int32", (1,), g), _stream_handle(stream))
+        if rc:
+            raise UADError(rc, "resize: the arguments break a rule of include/uad.h, or the ring is not on the current device")
 
 
 def quantize_w4(w, group=64, symmetric=False):

@@ -8,8 +8,6 @@ using namespace uad;
 
 namespace {
 
-constexpr int kItem = 16;   // dimensions that a thread takes of a head: 8 pairs, or 16 that are not rotated
-
 struct AppendArgs {
   PagedArgs p;
   const void *q, *k, *v;
@@ -18,52 +16,6 @@ struct AppendArgs {
   int n_heads, rot, groups, log_chunks, block_rows;
   FastDiv row_threads, row_blocks;   // threads of a row, blocks of a row
 };
-
-// cos and sin of position * turn / 2^64 turns. The product wraps at whole turns, which is exact; what is left is
-// taken to the nearest quarter, so that its rounding to fp32 is below 2^-28 of a turn.
-__device__ __forceinline__ void rotation(uint32_t pos, uint64_t turn, float* c, float* s) {
-  const uint64_t ph = (uint64_t)pos * turn + (1ull << 61);
-  const int quarter = (int)(ph >> 62);
-  const int64_t rest = (int64_t)(ph & ((1ull << 62) - 1)) - (1ll << 61);   // within an eighth of a turn
-  float cr, sr;
-  sincospif((float)(int32_t)(rest >> 32) * 4.656612873077393e-10f, &sr, &cr);   // 2^-31: half turns of 2^-32 turns
-  const float a = quarter & 1 ? -sr : cr, b = quarter & 1 ? cr : sr;
-  *c = quarter & 2 ? -a : a;
-  *s = quarter & 2 ? -b : b;
-}
-
-template <int T>
-__device__ __forceinline__ void load8(const void* base, int64_t e, float* x) {
-  if constexpr (T == F32) {
-    const float4* f = reinterpret_cast<const float4*>(static_cast<const float*>(base) + e);
-    const float4 a = f[0], b = f[1];
-    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-  } else {
-    const uint4 u = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(base) + e);
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[2 * i] = __uint_as_float(w[i] << 16);
-      x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
-  }
-}
-template <int T>
-__device__ __forceinline__ void store8(void* base, int64_t e, const float* x) {
-  if constexpr (T == F32) {
-    float4* f = reinterpret_cast<float4*>(static_cast<float*>(base) + e);
-    f[0] = make_float4(x[0], x[1], x[2], x[3]);
-    f[1] = make_float4(x[4], x[5], x[6], x[7]);
-  } else {
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
-      w[i] = *reinterpret_cast<const uint32_t*>(&h);
-    }
-    *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(base) + e) = make_uint4(w[0], w[1], w[2], w[3]);
-  }
-}
 
 // One thread: a chunk of 16 dimensions (8 pairs) of one row, in every a.groups-th of its heads. Eight sines and cosines cost
 // about as many cycles as 150 bytes of memory, so that with one head a thread they bound the kernel; they depend on the
@@ -151,10 +103,6 @@ __global__ void __launch_bounds__(256) gather_kernel(const PagedArgs p, const in
   }
 }
 
-bool bad_address(const void* p, int64_t stride, int es) {
-  return reinterpret_cast<uintptr_t>(p) % 16 != 0 || stride < 0 || (stride * es) % 16 != 0;
-}
-
 }  // namespace
 
 bool uad::on_current_device(const void* p) {
@@ -171,10 +119,10 @@ cudaError_t uad::launch_kv_gather(const PagedArgs& p, const int* table, int n, v
   return launch_k(gather_kernel, dim3((unsigned)n), 256, 0, s, p, table, static_cast<char*>(k), static_cast<char*>(v));
 }
 
-int uad::paged_args(const uad_kv_pages* g, const uad_kv_seqs* s, int n_rows, bool device, PagedArgs* p) {
+int uad::paged_args(const uad_kv_pages* g, const uad_kv_seqs* s, int n_rows, bool device, PagedArgs* p, bool eight) {
   if (!g || !s || !g->k || !g->v) return UAD_EINVAL;
-  if (g->dtype != UAD_DTYPE_F32 && g->dtype != UAD_DTYPE_BF16) return UAD_EINVAL;
-  const int es = g->dtype == UAD_DTYPE_F32 ? 4 : 2;
+  if (eight ? g->dtype != UAD_DTYPE_E4M3 : g->dtype != UAD_DTYPE_F32 && g->dtype != UAD_DTYPE_BF16) return UAD_EINVAL;
+  const int es = eight ? 1 : g->dtype == UAD_DTYPE_F32 ? 4 : 2;
   if (g->head_dim != 64 && g->head_dim != 128 && g->head_dim != 256) return UAD_EINVAL;
   if (g->n_pages < 1 || g->page_size < 1 || g->page_size > 65536 || g->n_kv_heads < 1 || g->n_kv_heads > 1024) return UAD_EINVAL;
   if (g->page_stride < 1 || g->slot_stride < 1 || g->head_stride < 1) return UAD_EINVAL;
@@ -191,7 +139,7 @@ int uad::paged_args(const uad_kv_pages* g, const uad_kv_seqs* s, int n_rows, boo
   p->page_stride = g->page_stride; p->slot_stride = g->slot_stride; p->head_stride = g->head_stride;
   p->table = s->table; p->len = s->len; p->start = s->start; p->table_stride = s->table_stride;
   p->page = FastDiv((uint32_t)g->page_size);
-  p->n_pages = g->n_pages; p->n_kv = g->n_kv_heads; p->dh = g->head_dim; p->dtype = g->dtype == UAD_DTYPE_F32 ? F32 : BF16;
+  p->n_pages = g->n_pages; p->n_kv = g->n_kv_heads; p->dh = g->head_dim; p->dtype = eight ? E4M3 : g->dtype == UAD_DTYPE_F32 ? F32 : BF16;
   p->n_seqs = s->n_seqs; p->n_rows = n_rows; p->max_new = s->max_new < n_rows ? s->max_new : (n_rows > 0 ? n_rows : 1);
   p->capacity = s->table_width * g->page_size;
   return UAD_OK;

@@ -10,7 +10,7 @@ namespace uad {
 constexpr int kMaxSteps = 64;              // = UAD_MAX_STEPS
 constexpr int kFlagStride = kMaxSteps + 1;  // host flag slots per robot (steps 1..64)
 
-enum DType { F32 = 0, BF16 = 1 };
+enum DType { F32 = 0, BF16 = 1, E4M3 = 2 };   // E4M3: pages of a cache alone
 
 // Programmatic dependent launch. Kernels of the step loop are launched so that the next kernel's CTAs may start
 // while the previous kernel drains. Every kernel calls pdl_trigger() once it has started, and pdl_wait() before
