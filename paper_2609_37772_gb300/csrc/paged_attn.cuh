@@ -77,7 +77,7 @@ __device__ __forceinline__ float weight(float m, float top) { return ex2_approx(
 // takes the slices kw, kw + wk, ...
 struct Piece {
   SeqRows s;
-  int r0, rows, kvh, piece, k0, k1, kw, wk;
+  int b, r0, rows, kvh, piece, k0, k1, kw, wk;   // b: the sequence
   int first_pos, last_pos;   // positions of the first and the last row
   // Where a window leaves the first tokens visible (SINKS), keys are counted without those that it hides from every row: key i is
   // token i of the sequence below a.sinks and token i + shift from there on. Positions are lowered by shift too.
@@ -90,12 +90,12 @@ struct Found {
   int token;
 };
 template <bool SINKS>
-__device__ __forceinline__ Found find_key(const PagedAttnArgs& a, int shift, int key) {
+__device__ __forceinline__ Found find_key(const PagedAttnArgs& a, int b, int shift, int key) {
   const int token = SINKS && key >= a.sinks ? key + shift : key;
   Found f{key, -1, false, token};
   if (SINKS ? (unsigned)token < (unsigned)a.p.capacity : token < a.p.capacity) {
-    f.page = a.p.table[blockIdx.z * a.p.table_stride + a.p.page.div(token)];
-    f.shown = !a.mask || a.mask[blockIdx.z * a.mask_stride + token] != 0;
+    f.page = a.p.table[b * a.p.table_stride + a.p.page.div(token)];
+    f.shown = !a.mask || a.mask[b * a.mask_stride + token] != 0;
   }
   return f;
 }
@@ -116,6 +116,7 @@ __device__ __forceinline__ bool find_piece(const PagedAttnArgs& a, int block_row
   const int b = blockIdx.z, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int x = (int)a.by_x.div(blockIdx.x), rest = blockIdx.x - x * (int)a.by_x.d;
   const int rb = a.clustered ? x : rest;
+  c->b = b;
   c->piece = a.clustered ? rest : x;
   c->kvh = a.warp_heads ? blockIdx.y * kWarps + warp : blockIdx.y;
   c->kw = a.warp_heads ? 0 : warp;
@@ -130,7 +131,7 @@ __device__ __forceinline__ bool find_piece(const PagedAttnArgs& a, int block_row
   const int64_t from = (SINKS ? 0 : lo) + (int64_t)c->piece * a.piece_keys;
   c->k0 = (int)(from < p.capacity - c->shift ? from : p.capacity - c->shift);
 #pragma unroll
-  for (int i = 0; i < N; ++i) found[i] = find_key<SINKS>(a, c->shift, c->k0 + (i * c->wk + c->kw) * slice + lane % slice);
+  for (int i = 0; i < N; ++i) found[i] = find_key<SINKS>(a, b, c->shift, c->k0 + (i * c->wk + c->kw) * slice + lane % slice);
   if (c->s.n < 0) {
     if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) kv_report(p, UAD_KV_BAD_SEQ);
     return false;

@@ -107,7 +107,7 @@ __global__ void __launch_bounds__(kThreads, tc_ctas<DH, NR>()) paged_attn_tc_ker
   };
   const auto next_k = [&](int i) {
     copy_k(i, AHEAD - 1, found);
-    if (i + 1 < mine) found = find_key<SINKS>(a, c.shift, slice_key(i + 1) + (lane & (KEYS - 1)));
+    if (i + 1 < mine) found = find_key<SINKS>(a, blockIdx.z, c.shift, slice_key(i + 1) + (lane & (KEYS - 1)));
   };
   const auto copy_v = [&](int i) { copy(i, a.p.v); };
 #pragma unroll
@@ -429,7 +429,7 @@ __global__ void __launch_bounds__(kThreads, CTAS) paged_attn_f32_kernel(const Pa
   };
   const auto next_k = [&](int i) {
     copy_k(i, AHEAD - 1, found);
-    if (i + 1 < mine) found = find_key<SINKS>(a, c.shift, slice_key(i + 1) + lane % KEYS);
+    if (i + 1 < mine) found = find_key<SINKS>(a, blockIdx.z, c.shift, slice_key(i + 1) + lane % KEYS);
   };
   const auto copy_v = [&](int i) { copy(i, a.p.v); };
 #pragma unroll

@@ -460,6 +460,42 @@ def test_long_caches_are_split_and_joined(heads, max_len):
     check_attention(c, q, out, lse)
 
 
+@pytest.mark.parametrize("heads,new", [((8, 1, 256), 1), ((8, 1, 256), 3), ((32, 8, 128), 1), ((8, 2, 128), 4), ((8, 2, 128), 8), ((24, 24, 64), 1), ((8, 2, 64), 3),
+                                       ((16, 2, 64), 4), ((21, 1, 64), 5)], ids=lambda h: str(h))
+@pytest.mark.parametrize("causal,window,sinks,masked", [(True, 0, 0, False), (False, 0, 0, True), (True, 90, 5, False), (True, 300, 0, True)])
+def test_keys_that_are_shared_evenly(heads, new, causal, window, sinks, masked):
+    """Tables so wide that the work is split for long sequences: parts that end inside of sequences, at their ends and behind the last one, sequences
+    without new tokens, with fewer rows than others, shorter than a chunk, and one that several parts share."""
+    c = Case8(heads, 16, [1500, 40, 0, 128, 257, 1, 700, 64, 33, 2900], [new, 1, 0, new, 0, 1, new, 1, new, new], seed=new, width=60000)
+    mask = None
+    if masked:
+        mask = torch.ones((c.n, c.width * c.page), dtype=torch.uint8, device="cuda")
+        mask[0, 100:1400] = 0
+        mask[3] = 0
+        mask[9, ::3] = 0
+    q, out, lse, status = run_attention(c, causal, window, sinks, mask, max_len=900000)
+    assert status == 0
+    check_attention(c, q, out, lse, causal, window, sinks, mask)
+
+
+def test_keys_that_are_shared_evenly_with_bad_sequences():
+    """Many sequences, one of which has a length that its table does not hold: it is left out, the others are served."""
+    lens = [1 + 37 * i % 400 for i in range(140)]
+    c = Case8((8, 4, 64), 16, lens, [1] * 140, seed=3, width=30000)
+    s, cache = c.sequences(400000), c.on_gpu()
+    c.dev[1][77] = -5
+    q = torch.from_numpy(c.rng.normal(size=(c.rows, 512))).cuda().bfloat16()
+    out, lse = torch.full((c.rows, 512), 7.5, device="cuda", dtype=torch.bfloat16), torch.full((c.rows, 8), 7.5, device="cuda")
+    ws = torch.empty(cache.attention_workspace(s, c.rows, 8), dtype=torch.uint8, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    cache.attention(s, q, out, ws, lse=lse, status=status)
+    torch.cuda.synchronize()
+    assert int(status) == uad.UAD_KV_BAD_SEQ and bool((out[77] == 7.5).all()) and bool((lse[77] == 7.5).all())
+    keep = [i for i in range(140) if i != 77]
+    c.table, c.lens, c.n, c.start = c.table[keep], [lens[i] for i in keep], 139, np.arange(140)
+    check_attention(c, q[keep], out[keep], lse[keep])
+
+
 @pytest.mark.parametrize("heads", [(8, 1, 64), (24, 24, 64), (8, 4, 128), (8, 8, 256)], ids=lambda h: "x".join(map(str, h)))
 def test_many_sequences(heads):
     """Enough short sequences that warps have heads of their own, and enough that one CTA has a sequence."""
