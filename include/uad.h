@@ -418,8 +418,8 @@ typedef struct uad_kv_pages8 {
 /* uad_kv_append into an 8-bit cache: queries are rotated into q_out in bf16, keys and values rounded to the nearest code (ties to even)
  * of their block's scale: the least power of two s (2^-100 at the least) with 448 s >= the largest of the block's new values, for keys
  * that are rotated twice the largest before the rotation (which grows no value by more than sqrt(2)). Infinities and NaN do not count
- * and are stored as NaN. Where the block holds earlier tokens of the sequence, its scale does not fall below theirs, and where it
- * grows they are rounded to it: exactly but for values 2^-15 of the block's largest and below, so that what a cache holds hardly depends on how many
+ * and are stored as NaN. Where the block holds earlier tokens of the sequence, its scale does not fall below theirs (nor below the power of two above it), and where
+ * it grows they are rounded to it: exactly but for values 2^-15 of the block's largest and below, so that what a cache holds hardly depends on how many
  * calls wrote it. A block that is written therefore belongs to one sequence: it must not stand in another table of the same append, nor
  * be read meanwhile; whole blocks before it may be shared. Errors: UAD_EINVAL (arguments), UAD_ECUDA. */
 int uad_kv_append8(const uad_kv_pages8* pages, const uad_kv_seqs* seqs, const uad_kv_rows* rows, const uad_rope* rope,

@@ -63,7 +63,7 @@ def append(codes, scales, table, lens, start, page, block, rows, theta=None, dim
             s0 = sub * block
             if first % page > s0:
                 before = scales[pg, sub].copy()
-                fresh = np.maximum(fresh, before)
+                fresh = np.maximum(fresh, 2.0 ** np.ceil(np.log2(before)))   # powers of two, whatever the earlier tokens came with
                 at = slice(s0, first % page)
                 grown = fresh != before
                 old = VALUES[codes[pg, at]] * before[None, :, None]

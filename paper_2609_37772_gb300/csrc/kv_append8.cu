@@ -7,7 +7,7 @@ using namespace uad;
 
 namespace {
 
-constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kMostThreads = 1024;   // of a CTA: 256 to 1024, a new token's 16 dimensions each
 
 struct Append8Args {
   PagedArgs p;
@@ -16,50 +16,57 @@ struct Append8Args {
   int64_t q_stride, k_stride, v_stride, q_out_stride;
   void* q_out;
   int n_heads, rot, log_chunks;
-  // keys and values: blocks of the grid's x that are theirs; head groups of the keys (and of the values); threads of a head
-  int kv_blocks, kv_groups, log_items;
-  FastDiv by_group;   // of a block's number into block of tokens and head group: 2 kv_groups
+  // keys and values: blocks of the grid's x that are theirs; groups of their heads
+  int kv_blocks, kv_groups;
+  FastDiv by_group;   // of a block's number into block of tokens and group of heads
   // queries
   int groups, block_rows;
   FastDiv row_threads, row_blocks;
 };
 
-__device__ __forceinline__ float finite_abs(float x) {
-  const float a = fabsf(x);
-  return a <= 3.402823466e38f ? a : 0.f;
+constexpr uint32_t kInfinite = 0x7f800000u;   // bits of absolute values from here on are not finite
+// The largest of eight absolute values and m, by their bits.
+__device__ __forceinline__ uint32_t top_of(const float* x, uint32_t m) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(x[i]) & 0x7fffffffu);
+  return m;
 }
-// The least power of two that takes `top` (twice: 2 top) to 448 or below, 2^-100 at the least. From the bits: 448 is 1.75 2^8.
-__device__ __forceinline__ float scale_of(float top, bool twice) {
-  const uint32_t u = __float_as_uint(top);
+// The same of those that are finite.
+__device__ __forceinline__ uint32_t finite_top_of(const float* x, uint32_t m) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t u = __float_as_uint(x[i]) & 0x7fffffffu;
+    m = max(m, u < kInfinite ? u : 0);
+  }
+  return m;
+}
+// The least power of two that takes a value (twice: twice the value) to 448 or below, 2^-100 at the least. From its bits: 448 is 1.75 2^8.
+__device__ __forceinline__ float scale_of(uint32_t u, bool twice) {
   const int e = (int)(u >> 23) - 8 + ((u & 0x7fffffu) > 0x600000u) + (twice ? 1 : 0);
   return __uint_as_float((uint32_t)max(e, 27) << 23);
 }
-// Two values as e4m3, the first one lower: nearest, ties to even; not finite: NaN.
+// The least power of two that is no less (of a cache that was rounded elsewhere: this append's scales are powers of two).
+__device__ __forceinline__ float power_above(float s) { return __uint_as_float((__float_as_uint(s) + 0x7fffffu) & 0xff800000u); }
+// Two values as e4m3, the first one lower: nearest, ties to even; NaN stays.
 __device__ __forceinline__ uint32_t e4m3_2(float a, float b) {
-  a = fabsf(a) == INFINITY ? NAN : a;
-  b = fabsf(b) == INFINITY ? NAN : b;
   uint16_t r;
   asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(b), "f"(a));
   return r;
 }
-// x / s: a multiplication where s is a power of two, as the scales of this append are.
-__device__ __forceinline__ float over(float x, float s, float inv, bool exact) { return exact ? x * inv : __fdiv_rn(x, s); }
-__device__ __forceinline__ uint2 round8(const float* x, float s, float inv, bool exact) {
+// inv: one over the scale. bad: some of the thread's values are not finite; infinities become NaN.
+__device__ __forceinline__ uint2 round8(const float* x, float inv, bool bad) {
   float y[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) y[i] = over(x[i], s, inv, exact);
+  for (int i = 0; i < 8; ++i) y[i] = x[i] * inv;
+  if (bad)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] += y[i] - y[i];
   return make_uint2(e4m3_2(y[0], y[1]) | e4m3_2(y[2], y[3]) << 16, e4m3_2(y[4], y[5]) | e4m3_2(y[6], y[7]) << 16);
 }
-// Four codes of scale `from` as codes of scale s.
-__device__ __forceinline__ uint32_t rescale4(uint32_t w, float from, float s, float inv, bool exact) {
-  float y[4];
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const float2 f = e4m3_pair(h ? w >> 16 : w);
-    y[2 * h] = over(f.x * from, s, inv, exact);
-    y[2 * h + 1] = over(f.y * from, s, inv, exact);
-  }
-  return e4m3_2(y[0], y[1]) | e4m3_2(y[2], y[3]) << 16;
+// Four codes times f.
+__device__ __forceinline__ uint32_t rescale4(uint32_t w, float f) {
+  const float2 a = e4m3_pair(w), b = e4m3_pair(w >> 16);
+  return e4m3_2(a.x * f, a.y * f) | e4m3_2(b.x * f, b.y * f) << 16;
 }
 
 // The queries: one thread 16 dimensions of one row, in every a.groups-th of its heads, as in the append of the other types.
@@ -68,7 +75,7 @@ __device__ __forceinline__ void rotate_queries(const Append8Args& a, const uad_r
   const int bj = a.row_blocks.div(block), tj = a.row_threads.div(threadIdx.x);
   if (tj >= a.block_rows) return;
   const int64_t j = (int64_t)bj * a.block_rows + tj;
-  const int r = (block - bj * (int)a.row_blocks.d) * kThreads + threadIdx.x - tj * (int)a.row_threads.d;
+  const int r = (block - bj * (int)a.row_blocks.d) * (int)blockDim.x + threadIdx.x - tj * (int)a.row_threads.d;
   if (j >= s.n || r >= (int)a.row_threads.d) return;
   const int group = r >> a.log_chunks, c = r - (group << a.log_chunks), half = a.rot / 2, lo = c * 8;
   const int64_t row = s.first + j;
@@ -101,15 +108,16 @@ __device__ __forceinline__ void rotate_queries(const Append8Args& a, const uad_r
   }
 }
 
-// Keys and values: a CTA has one block of tokens and some heads of the keys or of the values. A thread holds 16 dimensions of one
-// token (ITEMS tokens where a head of the block has more than the threads), as 8 pairs where they are rotated; all
-// threads of a head find its largest value, which gives the scale before anything is rotated: a rotation grows no value by more than
-// sqrt(2), so keys take twice the largest, and the scale does not hang on how sines round. Earlier tokens of the block,
-// which the first block of a sequence can have, belong to threads of their own and are rounded again where the scale has grown:
+// Keys and values: a CTA has one block of tokens and some heads of the keys and of the values. A thread holds 16 dimensions of one new
+// token, as 8 pairs where they are rotated; a head has as many
+// threads as its new tokens need, rounded up to a power of two, and a CTA as many heads at a time as that leaves room for: a decoding step's single
+// token takes 4 to 16 threads a head, a prompt's block all of them. The threads of a head find its largest value, which gives the scale
+// before anything is rotated: a rotation grows no value by more than sqrt(2), so keys take twice the largest, and the scale does not
+// hang on how sines round. Where the scale of a block with earlier tokens has grown, the head's threads round those again:
 // exactly, as long as they stay normal numbers.
-template <int IN, int ITEMS>
-__global__ void __launch_bounds__(kThreads, ITEMS == 1 ? 4 : 2) append8_kernel(const Append8Args a, const __grid_constant__ uad_rope rope) {
-  __shared__ uint32_t s_top[2][kWarps];
+template <int IN>
+__global__ void __launch_bounds__(kMostThreads, 1) append8_kernel(const Append8Args a, const __grid_constant__ uad_rope rope) {
+  __shared__ uint32_t s_top[2][kMostThreads / 32];
   pdl_wait();
   pdl_trigger();
   const PagedArgs& p = a.p;
@@ -124,118 +132,107 @@ __global__ void __launch_bounds__(kThreads, ITEMS == 1 ? 4 : 2) append8_kernel(c
     return;
   }
   if (s.n == 0) return;
-  const int u = a.by_group.div(blockIdx.x), z = blockIdx.x - u * 2 * a.kv_groups;
-  const bool is_v = z >= a.kv_groups;
-  const int group = is_v ? z - a.kv_groups : z, p0 = s.len - s.n;
+  const int u = a.by_group.div(blockIdx.x), group = blockIdx.x - u * a.kv_groups, p0 = s.len - s.n;
   const int i0 = (int)p.page.div(p0), in_page = p0 - i0 * (int)p.page.d;
   const int number = (in_page >> a.sc.log_block) + u, ahead = (int)a.sc.per_page.div(number);
   const int sub = number - ahead * (int)a.sc.per_page.d, lo_slot = sub << a.sc.log_block;
   const int64_t first64 = (int64_t)(i0 + ahead) * p.page.d + lo_slot;
   if (first64 >= s.len) return;
-  const int first = (int)first64, slots = min(1 << a.sc.log_block, (int)p.page.d - lo_slot);
+  const int first = (int)first64, end = min(first + min(1 << a.sc.log_block, (int)p.page.d - lo_slot), s.len);
+  const int begin = max(first, p0), fresh = end - begin, old = begin - first;   // new tokens of the block, earlier ones
+  const int log_lanes = (fresh > 1 ? 32 - __clz(fresh - 1) : 0) + a.log_chunks, lanes = 1 << log_lanes;   // of a head
+  const int per_pass = (int)blockDim.x >> log_lanes, heads = 2 * p.n_kv;   // the keys', then the values'
+  if (group * per_pass >= heads) return;
   const int page = p.table[b * p.table_stride + i0 + ahead];
+  const int warp = threadIdx.x >> 5, mine = threadIdx.x & (lanes - 1), at_once = threadIdx.x >> log_lanes;
+  const int c = mine & ((1 << a.log_chunks) - 1), half = a.rot / 2, lo = c * 8;
+  const int token = mine >> a.log_chunks;   // of the new ones
+  const int64_t row = s.first + (int64_t)(begin - p0 + token);
+  const auto load = [&](int h, float* x, float* y) {
+    if (h >= heads || token >= fresh) return;
+    const bool is_v = h >= p.n_kv, turn = !is_v && lo < half;
+    const int64_t at = is_v ? row * a.v_stride + (h - p.n_kv) * p.dh : row * a.k_stride + h * p.dh;
+    const void* from = is_v ? a.v : a.k;
+    load8<IN>(from, at + (turn ? lo : c * kItem), x);
+    load8<IN>(from, at + (turn ? lo + half : c * kItem + 8), y);
+  };
+  float x[8], y[8];
+  load(group * per_pass + at_once, x, y);
   if ((unsigned)page >= (unsigned)p.n_pages) {
     if (threadIdx.x == 0) kv_report(p, UAD_KV_BAD_PAGE);
     return;
   }
-  const bool joins = first < p0;   // earlier tokens are in the block
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int items = 1 << a.log_items, per_pass = ITEMS > 1 ? 1 : kThreads >> a.log_items;
-  const int mine = ITEMS > 1 ? threadIdx.x : threadIdx.x & (items - 1), at_once = ITEMS > 1 ? 0 : threadIdx.x >> a.log_items;
-  const int c = mine & ((1 << a.log_chunks) - 1), half = a.rot / 2, lo = c * 8;
-  const bool turn = !is_v && lo < half, twice = !is_v && a.rot > 0;
-  const int e_lo = turn ? lo : c * kItem, e_hi = turn ? lo + half : c * kItem + 8;
-  const int warps = ITEMS > 1 ? kWarps : items >> 5, warp0 = warp & ~(warps - 1);   // those of this thread's head
-  int pos[ITEMS];
-  bool fresh[ITEMS], old[ITEMS];
-#pragma unroll
-  for (int i = 0; i < ITEMS; ++i) {
-    const int j = (i * kThreads + mine) >> a.log_chunks;
-    pos[i] = first + j;
-    fresh[i] = j < slots && pos[i] >= p0 && pos[i] < s.len;
-    old[i] = pos[i] < p0;
-  }
   float cs[8], sn[8];
-  if (ITEMS == 1 && turn && fresh[0])
+  if (lo < half && token < fresh && group * per_pass < p.n_kv)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) rotation((uint32_t)pos[0], rope.turn[lo + i], cs + i, sn + i);
-  char* const pool = static_cast<char*>(is_v ? p.v : p.k) + page * p.page_stride + lo_slot * p.slot_stride;
-  float* const scales = (is_v ? a.sc.v : a.sc.k) + page * a.sc.page + sub * a.sc.block;
-  const void* const from = is_v ? a.v : a.k;
-  const int64_t from_stride = is_v ? a.v_stride : a.k_stride;
+    for (int i = 0; i < 8; ++i) rotation((uint32_t)(begin + token), rope.turn[lo + i], cs + i, sn + i);
+  const int64_t place = page * p.page_stride + lo_slot * p.slot_stride, scale_place = page * a.sc.page + sub * a.sc.block;
   int buf = 0;
-  for (int h0 = group * per_pass; h0 < p.n_kv; h0 += a.kv_groups * per_pass) {
-    const int h = h0 + at_once;
-    const bool here = h < p.n_kv;
-    float x[ITEMS][8], y[ITEMS][8];
-    uint4 codes[ITEMS];
-    float top = 0.f, before = 0.f;
+  for (int h0 = group * per_pass; h0 < heads; h0 += a.kv_groups * per_pass) {
+    const int hh = h0 + at_once;
+    const bool here = hh < heads, is_v = hh >= p.n_kv, turn = !is_v && lo < half, mover = here && token < fresh;
+    const int h = is_v ? hh - p.n_kv : hh;
+    float* const held = (is_v ? a.sc.v : a.sc.k) + scale_place + h * a.sc.head;
+    uint32_t most = 0;
+    bool bad = false;
+    float before = 0.f;
+    if (here && old && (lanes > 32 || mine == 0)) before = *held;   // read by all before the barrier, or by the one that writes it
+    if (mover) {
+      most = top_of(y, top_of(x, 0));
+      bad = most >= kInfinite;
+      if (bad) most = finite_top_of(y, finite_top_of(x, 0));
+      if (turn)
+#pragma unroll
+        for (int d = 0; d < 8; ++d) {
+          const float v = x[d] * cs[d] - y[d] * sn[d], w = y[d] * cs[d] + x[d] * sn[d];
+          x[d] = v;
+          y[d] = w;
+        }
+    }
+    if (lanes < 32) {
+      for (int d = lanes / 2; d > 0; d /= 2) most = max(most, __shfl_xor_sync(0xffffffffu, most, d));
+    } else {
+      most = __reduce_max_sync(0xffffffffu, most);
+    }
+    if (lanes <= 32) {
+      before = __shfl_sync(0xffffffffu, before, threadIdx.x & 31 & ~(lanes - 1));
+    } else {
+      if ((threadIdx.x & 31) == 0) s_top[buf][warp] = most;
+      __syncthreads();   // this buffer is written again after the next barrier
+      const int warp0 = warp & ~(lanes / 32 - 1);
+      for (int w = 0; w < lanes / 32; ++w) most = max(most, s_top[buf][warp0 + w]);
+      buf ^= 1;
+    }
     if (here) {
-      if (joins) before = scales[h * a.sc.head];
-#pragma unroll
-      for (int i = 0; i < ITEMS; ++i) {
-        if (fresh[i]) {
-          const int64_t at = (s.first + (int64_t)(pos[i] - p0)) * from_stride + h * p.dh;
-          load8<IN>(from, at + e_lo, x[i]);
-          load8<IN>(from, at + e_hi, y[i]);
-#pragma unroll
-          for (int d = 0; d < 8; ++d) top = fmaxf(top, fmaxf(finite_abs(x[i][d]), finite_abs(y[i][d])));
-        } else if (old[i]) {
-          codes[i] = *reinterpret_cast<const uint4*>(pool + (pos[i] - first) * p.slot_stride + h * p.head_stride + c * kItem);
-        }
-      }
-    }
-    const uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(top));
-    if (lane == 0) s_top[buf][warp] = most;
-    __syncthreads();   // this buffer is written again after the next barrier
-    uint32_t all = 0;
-    for (int w = 0; w < warps; ++w) all = max(all, s_top[buf][warp0 + w]);
-    buf ^= 1;
-    if (!here) continue;
-    float scale = scale_of(__uint_as_float(all), twice);
-    if (joins) scale = fmaxf(scale, before);
-    const bool exact = (__float_as_uint(scale) & 0x7fffffu) == 0;
-    const float inv = 1.f / scale;
-    if (mine == 0 && (!joins || scale != before)) scales[h * a.sc.head] = scale;
-#pragma unroll
-    for (int i = 0; i < ITEMS; ++i) {
-      char* const to = pool + (pos[i] - first) * p.slot_stride + h * p.head_stride;
-      if (fresh[i]) {
+      float scale = scale_of(most, !is_v && a.rot > 0);
+      if (old) scale = fmaxf(scale, power_above(before));
+      const float inv = __uint_as_float((254u << 23) - __float_as_uint(scale));   // a power of two as well
+      char* const head = static_cast<char*>(is_v ? p.v : p.k) + place + h * p.head_stride;
+      if (mover) {
+        const uint2 r0 = round8(x, inv, bad), r1 = round8(y, inv, bad);
+        char* const to = head + (old + token) * p.slot_stride;
         if (turn) {
-          if constexpr (ITEMS > 1)
-#pragma unroll
-            for (int d = 0; d < 8; ++d) rotation((uint32_t)pos[i], rope.turn[lo + d], cs + d, sn + d);
-#pragma unroll
-          for (int d = 0; d < 8; ++d) {
-            const float v = x[i][d] * cs[d] - y[i][d] * sn[d], w = y[i][d] * cs[d] + x[i][d] * sn[d];
-            x[i][d] = v;
-            y[i][d] = w;
-          }
-        }
-        const uint2 r0 = round8(x[i], scale, inv, exact), r1 = round8(y[i], scale, inv, exact);
-        if (turn) {
-          *reinterpret_cast<uint2*>(to + e_lo) = r0;
-          *reinterpret_cast<uint2*>(to + e_hi) = r1;
+          *reinterpret_cast<uint2*>(to + lo) = r0;
+          *reinterpret_cast<uint2*>(to + lo + half) = r1;
         } else {
-          *reinterpret_cast<uint4*>(to + e_lo) = make_uint4(r0.x, r0.y, r1.x, r1.y);
+          *reinterpret_cast<uint4*>(to + c * kItem) = make_uint4(r0.x, r0.y, r1.x, r1.y);
         }
-      } else if (old[i] && scale != before) {
-        uint4 w = codes[i];
-        w.x = rescale4(w.x, before, scale, inv, exact);
-        w.y = rescale4(w.y, before, scale, inv, exact);
-        w.z = rescale4(w.z, before, scale, inv, exact);
-        w.w = rescale4(w.w, before, scale, inv, exact);
-        *reinterpret_cast<uint4*>(to + c * kItem) = w;
+      }
+      if (!old || scale != before) {
+        for (int i = mine; i < old << a.log_chunks; i += lanes) {
+          uint4* const at = reinterpret_cast<uint4*>(head + (i >> a.log_chunks) * p.slot_stride + c * kItem);
+          uint4 w = *at;
+          w.x = rescale4(w.x, before * inv);
+          w.y = rescale4(w.y, before * inv);
+          w.z = rescale4(w.z, before * inv);
+          w.w = rescale4(w.w, before * inv);
+          *at = w;
+        }
+        if (mine == 0) *held = scale;
       }
     }
+    load(hh + a.kv_groups * per_pass, x, y);
   }
-}
-
-template <int IN>
-cudaError_t launch_items(int items, dim3 grid, cudaStream_t s, const Append8Args& a, const uad_rope& r) {
-  return items <= kThreads       ? launch_k(append8_kernel<IN, 1>, grid, kThreads, 0, s, a, r)
-         : items == 2 * kThreads ? launch_k(append8_kernel<IN, 2>, grid, kThreads, 0, s, a, r)
-                                 : launch_k(append8_kernel<IN, 4>, grid, kThreads, 0, s, a, r);
 }
 
 int log2_of(int n) {
@@ -283,9 +280,10 @@ extern "C" int uad_kv_append8(const uad_kv_pages8* pages, const uad_kv_seqs* seq
   a.q_out = rows->q_out; a.q_out_stride = rows->q_out_stride;
   a.n_heads = rows->n_heads; a.rot = rope ? rope->dim : 0;
   const uad_rope none{};
-  const int chunks = a.p.dh / kItem, block = pages->block, page = pages->pages.page_size, items = block * chunks;
+  const int chunks = a.p.dh / kItem, block = pages->block, page = pages->pages.page_size;
+  // a head's threads: those of the most new tokens that a block gets
+  const int lanes = (1 << log2_of(std::min({a.p.max_new, block, page}))) * chunks, threads = std::max(lanes, 256);
   a.log_chunks = log2_of(chunks);
-  a.log_items = log2_of(items);
   int64_t kv_blocks = 0, q_blocks = 0;
   if (a.k) {
     // the most blocks that max_new tokens in a row can touch
@@ -293,19 +291,19 @@ extern "C" int uad_kv_append8(const uad_kv_pages8* pages, const uad_kv_seqs* seq
     const int64_t touched = page % block == 0 ? (n + block - 2) / block + 1 : (n - 1) / page * per_page + std::min<int64_t>(per_page + 1, (n - 1) % page + 1);
     // Heads of a CTA: those that it holds at once, and up to five times as many where that leaves the SMs eight CTAs: they
     // share sines and cosines.
-    const int per_pass = std::max(1, kThreads / items), all = (a.p.n_kv + per_pass - 1) / per_pass;
-    const int64_t ctas = std::min<int64_t>(touched * a.p.n_seqs, (int64_t)a.p.n_rows + a.p.n_seqs) * 2 * all;
-    const int passes = (int)std::min<int64_t>({5, all, std::max<int64_t>(1, ctas / (152 * 8))});
+    const int per_pass = threads / lanes, all = (2 * a.p.n_kv + per_pass - 1) / per_pass;
+    const int64_t ctas = std::min<int64_t>(touched * a.p.n_seqs, (int64_t)a.p.n_rows + a.p.n_seqs) * all;
+    const int passes = (int)std::min<int64_t>({5, all, std::max<int64_t>(1, ctas * threads / (152 * 2048))});
     a.kv_groups = (all + passes - 1) / passes;
-    a.by_group = FastDiv((uint32_t)(2 * a.kv_groups));
-    kv_blocks = touched * 2 * a.kv_groups;
+    a.by_group = FastDiv((uint32_t)a.kv_groups);
+    kv_blocks = touched * a.kv_groups;
   }
   if (a.q) {
     const int64_t tokens = std::min<int64_t>((int64_t)a.p.max_new * a.p.n_seqs, a.p.n_rows);
     const int per = (int)std::min<int64_t>({5, a.n_heads, std::max<int64_t>(1, tokens * a.n_heads * chunks / (152 * 192))});
     a.groups = (a.n_heads + per - 1) / per;
-    const int row_threads = a.groups * chunks, row_blocks = (row_threads + kThreads - 1) / kThreads;
-    a.block_rows = row_threads < kThreads ? kThreads / row_threads : 1;
+    const int row_threads = a.groups * chunks, row_blocks = (row_threads + threads - 1) / threads;
+    a.block_rows = row_threads < threads ? threads / row_threads : 1;
     a.row_threads = FastDiv((uint32_t)row_threads);
     a.row_blocks = FastDiv((uint32_t)row_blocks);
     q_blocks = ((int64_t)a.p.max_new + a.block_rows - 1) / a.block_rows * row_blocks;
@@ -315,5 +313,5 @@ extern "C" int uad_kv_append8(const uad_kv_pages8* pages, const uad_kv_seqs* seq
   const dim3 grid((unsigned)(kv_blocks + q_blocks), (unsigned)a.p.n_seqs);
   const uad_rope& r = rope ? *rope : none;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  return launched(es == 4 ? launch_items<F32>(items, grid, s, a, r) : launch_items<BF16>(items, grid, s, a, r));
+  return launched(es == 4 ? launch_k(append8_kernel<F32>, grid, dim3(threads), 0, s, a, r) : launch_k(append8_kernel<BF16>, grid, dim3(threads), 0, s, a, r));
 }

@@ -8,7 +8,7 @@ using namespace uad;
 
 namespace {
 
-constexpr int kThreads = 512, kOwn = 4, kChunk = kThreads * kOwn;   // sequences of a thread, of a chunk
+constexpr int kThreads = 1024, kOwn = 2, kChunk = kThreads * kOwn;   // sequences of a thread, of a chunk
 
 struct ResizeArgs {
   int* table;
@@ -27,37 +27,37 @@ struct ResizeArgs {
   FastDiv page;
   int n_seqs, capacity, n_rows, n_pages;
   int fill, update;   // what this launch writes: tables, ring and rows; lengths and the ring's state
+  int maps, wide;     // whether slot maps are wanted; whether they are 16-byte aligned
 };
 
-__device__ __forceinline__ int64_t shfl_up64(int64_t v, int d) { return __shfl_up_sync(0xffffffffu, v, d); }
-
+static_assert(kThreads == 1024, "a lane for each warp's total");
 // Exclusive sums over the block's threads of N values each, and the block's totals. s: [kThreads / 32][N].
-template <int N>
-__device__ __forceinline__ void block_scan(int64_t* v, int64_t* total, int64_t (*s)[N]) {
+template <int N, typename T>
+__device__ __forceinline__ void block_scan(T* v, T* total, T (*s)[N]) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  int64_t mine[N];
+  T mine[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     mine[i] = v[i];
 #pragma unroll
     for (int d = 1; d < 32; d *= 2) {
-      const int64_t u = shfl_up64(v[i], d);
+      const T u = __shfl_up_sync(0xffffffffu, v[i], d);
       if (lane >= d) v[i] += u;
     }
     if (lane == 31) s[warp][i] = v[i];
   }
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    int64_t before = 0, all = 0;
+  for (int i = 0; i < N; ++i) {   // every warp sums the warps' totals up, lane w that of warp w
+    const T own = s[lane][i];
+    T upto = own;
 #pragma unroll
-    for (int w = 0; w < kThreads / 32; ++w) {
-      const int64_t x = s[w][i];
-      if (w < warp) before += x;
-      all += x;
+    for (int d = 1; d < 32; d *= 2) {
+      const T u = __shfl_up_sync(0xffffffffu, upto, d);
+      if (lane >= d) upto += u;
     }
-    v[i] += before - mine[i];
-    total[i] = all;
+    v[i] += __shfl_sync(0xffffffffu, upto - own, warp) - mine[i];
+    total[i] = __shfl_sync(0xffffffffu, upto, 31);
   }
 }
 
@@ -72,24 +72,57 @@ __device__ __forceinline__ int owner_of(const int* off, int n, int item) {
   return lo;
 }
 
+// Four rows from r of which those from..to - 1 are written: slot, sequence, position.
+struct Rows4 {
+  int64_t slot[4];
+  int seq[4], pos[4];
+};
+__device__ __forceinline__ void put_rows(const ResizeArgs& a, int r, int from, int to, const Rows4& x) {
+  if (a.wide && from <= r && r + 4 <= to) {
+    if (a.slot) {
+      longlong2* at = reinterpret_cast<longlong2*>(a.slot + r);
+      at[0] = make_longlong2(x.slot[0], x.slot[1]);
+      at[1] = make_longlong2(x.slot[2], x.slot[3]);
+    }
+    if (a.row_seq) *reinterpret_cast<int4*>(a.row_seq + r) = make_int4(x.seq[0], x.seq[1], x.seq[2], x.seq[3]);
+    if (a.row_pos) *reinterpret_cast<int4*>(a.row_pos + r) = make_int4(x.pos[0], x.pos[1], x.pos[2], x.pos[3]);
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (r + i < from || r + i >= to) continue;
+    if (a.slot) a.slot[r + i] = x.slot[i];
+    if (a.row_seq) a.row_seq[r + i] = x.seq[i];
+    if (a.row_pos) a.row_pos[r + i] = x.pos[i];
+  }
+}
+
 // Sums over the sequences give everybody's place. A block holds the sums of 2048 sequences in shared memory, and every block works
 // them out for itself, which takes it 1 to 2 us a chunk and spares an exchange. The items (pages taken, pages given back,
-// rows) are then spread evenly over all blocks' threads, each finding its owner by bisection, so that one long sequence costs
-// no more than many short ones.
+// rows in fours) are then spread evenly over all blocks' threads, each finding its owner by bisection, so that one long sequence costs
+// no more than many short ones. T: what the sums of a chunk fit in.
+template <typename T>
 __global__ void __launch_bounds__(kThreads) resize_kernel(const ResizeArgs a) {
   __shared__ int take_at[kChunk], give_at[kChunk], row_at[kChunk], had[kChunk], kept[kChunk];   // kept: pages that it shall have
-  __shared__ int64_t sums[kThreads / 32][3], row_sums[kThreads / 32][1];
+  __shared__ T sums[kThreads / 32][3], row_sums[kThreads / 32][1];
   __shared__ int taken_end;
   if (threadIdx.x == 0) taken_end = 0;
   pdl_wait();
   pdl_trigger();
+  int len[kOwn], want[kOwn];
+  const auto load = [&](int base) {
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i) {
+      const int b = base + threadIdx.x * kOwn + i;
+      len[i] = b < a.n_seqs ? a.len[b] : 0;
+      want[i] = b < a.n_seqs ? a.want[b] : 0;
+    }
+  };
+  load(0);
   const bool lead = blockIdx.x == 0;
-  const int first = a.state[0], n = a.n_pages;
-  int count = a.state[1];
-  const bool sound = first >= 0 && first < n && count >= 0 && count <= n;
-  const int full = count;
-  if (!sound) count = 0;
-  const int room = sound ? n - count : 0;   // free places of the ring
+  const int first = a.state[0], n = a.n_pages, full = a.state[1];
+  const bool sound = first >= 0 && first < n && full >= 0 && full <= n;
+  const int count = sound ? full : 0, room = sound ? n - full : 0;   // pages, and free places of the ring
   int64_t asked_pages = 0, asked_rows = 0, given = 0;   // of the chunks before
   int rows = 0, taken = 0;
   int report = sound ? 0 : UAD_KV_BAD_POOL;
@@ -99,93 +132,102 @@ __global__ void __launch_bounds__(kThreads) resize_kernel(const ResizeArgs a) {
     return x >= (uint32_t)n ? x - n : x;
   };
   const auto pages_of = [&](int tokens) { return tokens > 0 ? (int)a.page.div(tokens - 1) + 1 : 0; };
-  __syncthreads();   // taken_end; the state has been read
+  if (a.n_seqs == 0) __syncthreads();   // the state has been read
   for (int base = 0; base < a.n_seqs; base += kChunk) {
-    int len[kOwn], want[kOwn];
-    int64_t v[3] = {0, 0, 0}, total[3];   // pages to take, pages to give back, rows
+    T v[3] = {0, 0, 0}, total[3];   // pages to take, pages to give back, rows
+    int held[kOwn], need[kOwn];
     bool bad = false;
 #pragma unroll
     for (int i = 0; i < kOwn; ++i) {
-      const int b = base + threadIdx.x * kOwn + i;
-      len[i] = want[i] = 0;
-      if (b >= a.n_seqs) continue;
-      len[i] = a.len[b];
-      want[i] = a.want[b];
       if ((unsigned)len[i] > (unsigned)a.capacity || (unsigned)want[i] > (unsigned)a.capacity) {
         bad = true;
         want[i] = len[i];   // stays as it is
       }
-      const int d = want[i] == len[i] ? 0 : pages_of(want[i]) - pages_of(len[i]);
-      if (d > 0) v[0] += d;
-      else v[1] -= d;
-      if (want[i] > len[i]) v[2] += want[i] - len[i];
+      const bool moves = want[i] != len[i];
+      held[i] = moves ? pages_of(len[i]) : 0;
+      need[i] = moves ? pages_of(want[i]) : 0;
+      v[0] += max(need[i] - held[i], 0);
+      v[1] += max(held[i] - need[i], 0);
+      if (moves) v[2] += max(want[i] - len[i], 0);
     }
     if (bad) report |= UAD_KV_BAD_SEQ;
-    block_scan<3>(v, total, sums);   // its barrier: the chunk before has been read by all
+    block_scan<3, T>(v, total, sums);   // its barrier: the chunk before has been read by all
     // Who is served: in order, as far as pages and rows go. The sums count everybody, so that behind one who is not served nobody
     // is who needs more of the same: the pages taken are the first ones without a gap.
     int64_t pages_end = asked_pages + v[0], back = given + v[1], rows_end = asked_rows + v[2];
-    int64_t served[1] = {0}, all_served[1];
+    T served[1] = {0}, all_served[1];
     bool ok[kOwn];
     int most = 0;
 #pragma unroll
     for (int i = 0; i < kOwn; ++i) {
-      const int k = threadIdx.x * kOwn + i, add = want[i] - len[i];
-      const int held = add ? pages_of(len[i]) : 0, need = add ? pages_of(want[i]) : 0;
+      const int k = threadIdx.x * kOwn + i, add = want[i] == len[i] ? 0 : want[i] - len[i];
       ok[i] = true;
       had[k] = len[i];
-      kept[k] = need;
+      kept[k] = need[i];
       take_at[k] = (int)min(pages_end, (int64_t)0x7fffffff);
       give_at[k] = (int)min(back, (int64_t)0x7fffffff);
       if (add > 0) {
-        pages_end += need - held;
+        pages_end += need[i] - held[i];
         rows_end += add;
-        ok[i] = (need == held || pages_end <= count) && rows_end <= a.n_rows;
+        ok[i] = (need[i] == held[i] || pages_end <= count) && rows_end <= a.n_rows;
         if (!ok[i]) report |= UAD_KV_NO_ROOM;
         else served[0] += add;
-        if (ok[i] && need > held) most = (int)pages_end;
+        if (ok[i] && need[i] > held[i]) most = (int)pages_end;
       } else {
-        back += held - need;
-        if (back > room && held > need) report |= UAD_KV_BAD_POOL;
+        back += held[i] - need[i];
+        if (back > room && held[i] > need[i]) report |= UAD_KV_BAD_POOL;
       }
     }
     most = (int)__reduce_max_sync(0xffffffffu, (unsigned)most);
     if (most && (threadIdx.x & 31) == 0) atomicMax(&taken_end, most);
-    block_scan<1>(served, all_served, row_sums);
-    int64_t at = rows + served[0];
+    block_scan<1, T>(served, all_served, row_sums);
+    int at = rows + (int)served[0];
 #pragma unroll
     for (int i = 0; i < kOwn; ++i) {
       const int k = threadIdx.x * kOwn + i, b = base + k;
-      row_at[k] = (int)at;
+      row_at[k] = at;
       if (b < a.n_seqs && lead) {
-        if (a.fill) a.start[b] = (int)at;
+        if (a.fill) a.start[b] = at;
         if (a.update) a.len_out[b] = ok[i] ? want[i] : len[i];
       }
       if (ok[i] && want[i] > len[i]) at += want[i] - len[i];
     }
     __syncthreads();   // places and taken_end
+    load(base + kChunk);   // the next chunk, on its way meanwhile
     const int m = min(kChunk, a.n_seqs - base), rows_to = rows + (int)all_served[0], taken_to = taken_end;
-    const int given_from = (int)min(given, (int64_t)room), given_to = (int)min(given + total[1], (int64_t)room);
+    const int given_from = (int)min(given, (int64_t)room), given_to = (int)min((int64_t)(given + total[1]), (int64_t)room);
     if (a.fill) {
-      for (uint32_t i = id; i < (uint32_t)(taken_to - taken); i += step) {
+      // Rows, pages taken and pages given back begin with different threads, so that few of each are worked on at the same time.
+      for (uint32_t i = step - 1 - id; i < (uint32_t)(taken_to - taken); i += step) {
         const int t = taken + (int)i, k = owner_of(take_at, m, t);
         a.table[(base + k) * a.table_stride + pages_of(had[k]) + t - take_at[k]] = a.ring[on_ring(t)];
       }
-      for (uint32_t i = id; i < (uint32_t)(given_to - given_from); i += step) {
+      for (uint32_t i = id < step / 2 ? id + step / 2 : id - step / 2; i < (uint32_t)(given_to - given_from); i += step) {
         const int t = given_from + (int)i, k = owner_of(give_at, m, t);
         a.ring[on_ring(count + t)] = a.table[(base + k) * a.table_stride + kept[k] + t - give_at[k]];
       }
-      if (a.slot || a.row_seq || a.row_pos) {
-        for (uint32_t i = id; i < (uint32_t)(rows_to - rows); i += step) {
-          const int r = rows + (int)i, k = owner_of(row_at, m, r), pos = had[k] + r - row_at[k];
-          if (a.row_seq) a.row_seq[r] = base + k;
-          if (a.row_pos) a.row_pos[r] = pos;
-          if (!a.slot) continue;
-          const int pi = (int)a.page.div(pos), held = pages_of(had[k]);
-          const int page = pi < held ? a.table[(base + k) * a.table_stride + pi] : a.ring[on_ring(take_at[k] + pi - held)];
-          const bool there = (unsigned)page < (unsigned)n;
-          if (!there) report |= UAD_KV_BAD_PAGE;
-          a.slot[r] = there ? (int64_t)page * a.page.d + (pos - pi * (int)a.page.d) : -1;
+      if (a.maps) {
+        for (uint32_t i = (uint32_t)rows / 4 + id; i < ((uint32_t)rows_to + 3) / 4; i += step) {
+          const int r0 = (int)i * 4, begin = max(r0, rows);
+          int k = owner_of(row_at, m, begin), last = -1, page = 0;
+          Rows4 x;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int r = r0 + j;
+            if (r < begin || r >= rows_to) continue;
+            while (k + 1 < m && row_at[k + 1] <= r) ++k, last = -1;   // past those without rows
+            const int pos = had[k] + r - row_at[k], pi = (int)a.page.div(pos);
+            if (a.slot && pi != last) {
+              const int own = pages_of(had[k]);
+              page = pi < own ? a.table[(base + k) * a.table_stride + pi] : a.ring[on_ring(take_at[k] + pi - own)];
+              last = pi;
+              if ((unsigned)page >= (unsigned)n) report |= UAD_KV_BAD_PAGE;
+            }
+            x.seq[j] = base + k;
+            x.pos[j] = pos;
+            x.slot[j] = (unsigned)page < (unsigned)n ? (int64_t)page * a.page.d + (pos - pi * (int)a.page.d) : -1;
+          }
+          put_rows(a, r0, rows, rows_to, x);
         }
       }
     }
@@ -196,13 +238,9 @@ __global__ void __launch_bounds__(kThreads) resize_kernel(const ResizeArgs a) {
     taken = taken_to;
   }
   if (a.fill) {
-    if (a.slot || a.row_seq || a.row_pos) {   // rows of nobody
-      for (uint32_t i = id; i < (uint32_t)(a.n_rows - rows); i += step) {
-        const int r = rows + (int)i;
-        if (a.slot) a.slot[r] = -1;
-        if (a.row_seq) a.row_seq[r] = -1;
-        if (a.row_pos) a.row_pos[r] = -1;
-      }
+    if (a.maps) {   // rows of nobody
+      const Rows4 none = {{-1, -1, -1, -1}, {-1, -1, -1, -1}, {-1, -1, -1, -1}};
+      for (uint32_t i = (uint32_t)rows / 4 + id; i < ((uint32_t)a.n_rows + 3) / 4; i += step) put_rows(a, (int)i * 4, rows, a.n_rows, none);
     }
     if (lead && threadIdx.x == 0) a.start[a.n_seqs] = rows;
     // what the lengths say is every block's finding: one tells it
@@ -214,6 +252,12 @@ __global__ void __launch_bounds__(kThreads) resize_kernel(const ResizeArgs a) {
     a.state_out[0] = head;
     a.state_out[1] = left;
   }
+}
+
+cudaError_t launch_resize(const ResizeArgs& a, int blocks, cudaStream_t s) {
+  // sums of 2048 lengths below 2^20 stay within 31 bits
+  return a.capacity < 1 << 20 ? launch_k(resize_kernel<int>, dim3(blocks), dim3(kThreads), 0, s, a)
+                              : launch_k(resize_kernel<int64_t>, dim3(blocks), dim3(kThreads), 0, s, a);
 }
 
 }  // namespace
@@ -234,16 +278,18 @@ extern "C" int uad_kv_resize(const uad_page_pool* pool, const uad_kv_wanted* w, 
   a.n_seqs = w->n_seqs; a.capacity = w->table_width * pool->page_size; a.n_rows = w->n_rows; a.n_pages = pool->n_pages;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const bool maps = w->slot || w->row_seq || w->row_pos;
-  const int blocks = std::max(1, std::min(152, maps ? (int)(((int64_t)w->n_rows + 2047) / 2048) : w->n_seqs / 64));
+  a.maps = maps;
+  a.wide = (reinterpret_cast<uintptr_t>(w->slot) | reinterpret_cast<uintptr_t>(w->row_seq) | reinterpret_cast<uintptr_t>(w->row_pos)) % 16 == 0;
+  const int blocks = std::max(1, std::min(152, maps ? (int)(((int64_t)w->n_rows + 4095) / 4096) : w->n_seqs / 64));
   // In place, blocks would read lengths or a state that another has already replaced: a launch of its own replaces them.
   const bool apart = blocks > 1 && (w->len_out == w->len || w->len_out == w->want || pool->state_out == pool->state);
   a.fill = 1;
   a.update = !apart;
-  cudaError_t e = launch_k(resize_kernel, dim3(blocks), dim3(kThreads), 0, s, a);
+  cudaError_t e = launch_resize(a, blocks, s);
   if (e == cudaSuccess && apart) {
     a.fill = 0;
     a.update = 1;
-    e = launch_k(resize_kernel, dim3(1), dim3(kThreads), 0, s, a);
+    e = launch_resize(a, 1, s);
   }
   return launched(e);
 }
