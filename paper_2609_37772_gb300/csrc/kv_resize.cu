@@ -8,7 +8,7 @@ using namespace uad;
 
 namespace {
 
-constexpr int kThreads = 1024, kOwn = 2, kChunk = kThreads * kOwn;   // sequences of a thread, of a chunk
+constexpr int kThreads = 1024, kOwn = 2, kChunk = kThreads * kOwn;   // the most of a block; sequences of a thread; the most of a chunk
 
 struct ResizeArgs {
   int* table;
@@ -49,7 +49,7 @@ __device__ __forceinline__ void block_scan(T* v, T* total, T (*s)[N]) {
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < N; ++i) {   // every warp sums the warps' totals up, lane w that of warp w
-    const T own = s[lane][i];
+    const T own = lane < (int)blockDim.x / 32 ? s[lane][i] : 0;
     T upto = own;
 #pragma unroll
     for (int d = 1; d < 32; d *= 2) {
@@ -126,14 +126,19 @@ __global__ void __launch_bounds__(kThreads) resize_kernel(const ResizeArgs a) {
   int64_t asked_pages = 0, asked_rows = 0, given = 0;   // of the chunks before
   int rows = 0, taken = 0;
   int report = sound ? 0 : UAD_KV_BAD_POOL;
-  const uint32_t id = blockIdx.x * kThreads + threadIdx.x, step = gridDim.x * kThreads;
+  const int chunk = (int)blockDim.x * kOwn;
+  // Chunks are worked out by every block in turn, and filled in by a share of the blocks each, at about the same time.
+  const uint32_t shares = min((a.n_seqs + chunk - 1) / chunk, (int)gridDim.x), share = shares > 1 ? blockIdx.x % shares : 0;
+  const uint32_t id = (shares > 1 ? blockIdx.x / shares : blockIdx.x) * blockDim.x + threadIdx.x;
+  const uint32_t step = (shares > 1 ? (gridDim.x - share + shares - 1) / shares : gridDim.x) * blockDim.x;
   const auto on_ring = [&](uint32_t i) {   // i <= n places behind the first
     const uint32_t x = (uint32_t)first + i;
     return x >= (uint32_t)n ? x - n : x;
   };
   const auto pages_of = [&](int tokens) { return tokens > 0 ? (int)a.page.div(tokens - 1) + 1 : 0; };
   if (a.n_seqs == 0) __syncthreads();   // the state has been read
-  for (int base = 0; base < a.n_seqs; base += kChunk) {
+  uint32_t turn = 0;
+  for (int base = 0; base < a.n_seqs; base += chunk) {
     T v[3] = {0, 0, 0}, total[3];   // pages to take, pages to give back, rows
     int held[kOwn], need[kOwn];
     bool bad = false;
@@ -154,8 +159,9 @@ __global__ void __launch_bounds__(kThreads) resize_kernel(const ResizeArgs a) {
     block_scan<3, T>(v, total, sums);   // its barrier: the chunk before has been read by all
     // Who is served: in order, as far as pages and rows go. The sums count everybody, so that behind one who is not served nobody
     // is who needs more of the same: the pages taken are the first ones without a gap.
+    const bool everybody = asked_pages + total[0] <= count && asked_rows + total[2] <= a.n_rows && asked_rows == rows;
     int64_t pages_end = asked_pages + v[0], back = given + v[1], rows_end = asked_rows + v[2];
-    T served[1] = {0}, all_served[1];
+    T served[1] = {0}, all_served = total[2];
     bool ok[kOwn];
     int most = 0;
 #pragma unroll
@@ -166,6 +172,7 @@ __global__ void __launch_bounds__(kThreads) resize_kernel(const ResizeArgs a) {
       kept[k] = need[i];
       take_at[k] = (int)min(pages_end, (int64_t)0x7fffffff);
       give_at[k] = (int)min(back, (int64_t)0x7fffffff);
+      row_at[k] = (int)rows_end;   // where everybody is served
       if (add > 0) {
         pages_end += need[i] - held[i];
         rows_end += add;
@@ -178,25 +185,33 @@ __global__ void __launch_bounds__(kThreads) resize_kernel(const ResizeArgs a) {
         if (back > room && held[i] > need[i]) report |= UAD_KV_BAD_POOL;
       }
     }
-    most = (int)__reduce_max_sync(0xffffffffu, (unsigned)most);
-    if (most && (threadIdx.x & 31) == 0) atomicMax(&taken_end, most);
-    block_scan<1, T>(served, all_served, row_sums);
-    int at = rows + (int)served[0];
+    if (!everybody) {   // rows and pages once more, of those who are served
+      most = (int)__reduce_max_sync(0xffffffffu, (unsigned)most);
+      if ((threadIdx.x & 31) == 0) atomicMax(&taken_end, max(most, taken));
+      T all[1];
+      block_scan<1, T>(served, all, row_sums);
+      all_served = all[0];
+      int at = rows + (int)served[0];
 #pragma unroll
-    for (int i = 0; i < kOwn; ++i) {
-      const int k = threadIdx.x * kOwn + i, b = base + k;
-      row_at[k] = at;
-      if (b < a.n_seqs && lead) {
-        if (a.fill) a.start[b] = at;
+      for (int i = 0; i < kOwn; ++i) {
+        row_at[threadIdx.x * kOwn + i] = at;
+        if (ok[i] && want[i] > len[i]) at += want[i] - len[i];
+      }
+    }
+    if (lead) {
+#pragma unroll
+      for (int i = 0; i < kOwn; ++i) {
+        const int k = threadIdx.x * kOwn + i, b = base + k;
+        if (b >= a.n_seqs) continue;
+        if (a.fill) a.start[b] = row_at[k];
         if (a.update) a.len_out[b] = ok[i] ? want[i] : len[i];
       }
-      if (ok[i] && want[i] > len[i]) at += want[i] - len[i];
     }
     __syncthreads();   // places and taken_end
-    load(base + kChunk);   // the next chunk, on its way meanwhile
-    const int m = min(kChunk, a.n_seqs - base), rows_to = rows + (int)all_served[0], taken_to = taken_end;
+    load(base + chunk);   // the next chunk, on its way meanwhile
+    const int m = min(chunk, a.n_seqs - base), rows_to = rows + (int)all_served, taken_to = everybody ? (int)(asked_pages + total[0]) : taken_end;
     const int given_from = (int)min(given, (int64_t)room), given_to = (int)min((int64_t)(given + total[1]), (int64_t)room);
-    if (a.fill) {
+    if (a.fill && turn == share) {
       // Rows, pages taken and pages given back begin with different threads, so that few of each are worked on at the same time.
       for (uint32_t i = step - 1 - id; i < (uint32_t)(taken_to - taken); i += step) {
         const int t = taken + (int)i, k = owner_of(take_at, m, t);
@@ -215,7 +230,11 @@ __global__ void __launch_bounds__(kThreads) resize_kernel(const ResizeArgs a) {
           for (int j = 0; j < 4; ++j) {
             const int r = r0 + j;
             if (r < begin || r >= rows_to) continue;
-            while (k + 1 < m && row_at[k + 1] <= r) ++k, last = -1;   // past those without rows
+            if (k + 1 < m && row_at[k + 1] <= r) {   // the next one, or behind a run of those without rows
+              ++k;
+              if (k + 1 < m && row_at[k + 1] <= r) k += 1 + owner_of(row_at + k + 1, m - k - 1, r);
+              last = -1;
+            }
             const int pos = had[k] + r - row_at[k], pi = (int)a.page.div(pos);
             if (a.slot && pi != last) {
               const int own = pages_of(had[k]);
@@ -231,6 +250,7 @@ __global__ void __launch_bounds__(kThreads) resize_kernel(const ResizeArgs a) {
         }
       }
     }
+    turn = turn + 1 >= shares ? 0 : turn + 1;
     asked_pages += total[0];
     given += total[1];
     asked_rows += total[2];
@@ -240,7 +260,7 @@ __global__ void __launch_bounds__(kThreads) resize_kernel(const ResizeArgs a) {
   if (a.fill) {
     if (a.maps) {   // rows of nobody
       const Rows4 none = {{-1, -1, -1, -1}, {-1, -1, -1, -1}, {-1, -1, -1, -1}};
-      for (uint32_t i = (uint32_t)rows / 4 + id; i < ((uint32_t)a.n_rows + 3) / 4; i += step) put_rows(a, (int)i * 4, rows, a.n_rows, none);
+      for (uint32_t i = (uint32_t)rows / 4 + blockIdx.x * blockDim.x + threadIdx.x; i < ((uint32_t)a.n_rows + 3) / 4; i += gridDim.x * blockDim.x) put_rows(a, (int)i * 4, rows, a.n_rows, none);
     }
     if (lead && threadIdx.x == 0) a.start[a.n_seqs] = rows;
     // what the lengths say is every block's finding: one tells it
@@ -255,9 +275,10 @@ __global__ void __launch_bounds__(kThreads) resize_kernel(const ResizeArgs a) {
 }
 
 cudaError_t launch_resize(const ResizeArgs& a, int blocks, cudaStream_t s) {
+  const int threads = blocks == 1 && a.n_seqs <= 512 && a.n_rows <= 1024 ? 256 : kThreads;   // a decoding step: fewer to wait for
   // sums of 2048 lengths below 2^20 stay within 31 bits
-  return a.capacity < 1 << 20 ? launch_k(resize_kernel<int>, dim3(blocks), dim3(kThreads), 0, s, a)
-                              : launch_k(resize_kernel<int64_t>, dim3(blocks), dim3(kThreads), 0, s, a);
+  return a.capacity < 1 << 20 ? launch_k(resize_kernel<int>, dim3(blocks), dim3(threads), 0, s, a)
+                              : launch_k(resize_kernel<int64_t>, dim3(blocks), dim3(threads), 0, s, a);
 }
 
 }  // namespace
