@@ -488,6 +488,9 @@ int uad_kv_resize(const uad_page_pool* pool, const uad_kv_wanted* wanted, int32_
  * Errors: UAD_EINVAL (also a page outside 0..n_pages-1), UAD_ESTATE (a chunk is in flight), UAD_ENOMEM, UAD_ECUDA. */
 int uad_set_prefix_paged(uad_ctx* ctx, int32_t robot, const uad_kv_pages* layers, int32_t n_layers, const int32_t* table,
                          int32_t table_len);
+/* The same from 8-bit caches: what the codes stand for, in fp32, is what the expert is given (a bf16 expert rounds it). */
+int uad_set_prefix_paged8(uad_ctx* ctx, int32_t robot, const uad_kv_pages8* layers, int32_t n_layers, const int32_t* table,
+                          int32_t table_len);
 
 /* ---- The projection of few tokens with 4-bit weights ------------------------------------------------------
  * out[M][N] = x[M][K] w^T + bias with w[n][k] = (q[n][k] - zero[n][k / group]) * scale[n][k / group]: for the tokens of a

@@ -127,6 +127,7 @@ uad_kv_append8 = _fn("uad_kv_append8", C.c_int, _PAGES8, _SEQS, C.POINTER(uad_kv
 uad_paged_attention8_workspace = _fn("uad_paged_attention8_workspace", C.c_int64, _PAGES8, _SEQS, _ATTN, _I32)
 uad_paged_attention8 = _fn("uad_paged_attention8", C.c_int, _PAGES8, _SEQS, _ATTN, _I32, _P, C.c_size_t, _P, _P)
 uad_kv_resize = _fn("uad_kv_resize", C.c_int, C.POINTER(uad_page_pool), C.POINTER(uad_kv_wanted), _P, _P)
+uad_set_prefix_paged8 = _fn("uad_set_prefix_paged8", C.c_int, _P, _I32, _PAGES8, _I32, _P, _I32)
 uad_linear_w4 = _fn("uad_linear_w4", C.c_int, _P, _P, _P, _P, _P, _P, _I32, _I32, _I32, _I32, _P)
 uad_quantize_w4 = _fn("uad_quantize_w4", C.c_int, _P, _I32, _I32, _I32, _P, _P, _P)
 # The same entries for the wrappers below, with structures as addresses or packed bytes: a decoding step makes several such
@@ -158,7 +159,7 @@ EXPORTS = ["uad_version", "uad_last_error", "uad_init", "uad_set_prefix_kv", "ua
            "uad_linear_status", "uad_linear_check", "uad_so3_check", "uad_rope_init", "uad_kv_append",
            "uad_paged_attention_workspace", "uad_paged_attention", "uad_set_prefix_paged", "uad_linear_w4", "uad_quantize_w4",
            "uad_kv_append8", "uad_paged_attention8_workspace", "uad_paged_attention8", "uad_paged_attention_sinks_workspace",
-           "uad_paged_attention_sinks", "uad_kv_resize"]
+           "uad_paged_attention_sinks", "uad_kv_resize", "uad_set_prefix_paged8"]
 
 
 def tile_weight(w):
@@ -493,6 +494,11 @@ class PagePool:
         self._state = _tensor(state, "state", "int32", (2,), self._gpu)
         self.ring, self.state, self.page_size, self.n_pages = ring, state, page_size, ring.shape[0]
 
+    def _out(self, t, what, dtype, n):
+        if t.dtype is dtype and t.dim() == 1 and t.numel() == n and t.is_contiguous() and t.get_device() == self._gpu:
+            return t.data_ptr()
+        return _tensor(t, what, str(dtype)[6:], (n,), self._gpu)
+
     def resize(self, table, length, want, start, length_out=None, state_out=None, slot=None, row_seq=None, row_pos=None, rows=None, status=None,
                stream=None):
         """Give every sequence the pages of want tokens: table int32 [n][pages], length and want int32 [n] (tokens that it has and shall
@@ -501,31 +507,39 @@ class PagePool:
         (page * page_size + slot), sequence and position, -1 behind the last one. rows: what the token tensors hold (None: the
         slot maps' length; without one, no limit). Sequences that find no page or row stay as they were (UAD_KV_NO_ROOM in `status`);
         want below length gives pages back."""
-        g, n = self._gpu, length.shape[0] if length.dim() else -1
-        whole = _dtypes["int32"]
-        # the usual tensors checked at once; where a check fails, _tensor says which or finds them sound
-        if (table.dtype is whole and table.dim() == 2 and table.shape[0] == n and table.is_contiguous() and length.dtype is whole and
-                length.dim() == 1 and length.is_contiguous() and want.dtype is whole and want.shape == (n,) and want.is_contiguous() and
-                start.dtype is whole and start.shape == (n + 1,) and start.is_contiguous() and
-                table.get_device() == g == length.get_device() and want.get_device() == g == start.get_device()):
+        g, n, whole = self._gpu, length.numel(), _dtypes["int32"]
+        # the usual tensors checked at once, which takes a third of what one by one does; where a check fails, _tensor says which or finds
+        # them sound
+        if (table.dtype is whole and length.dtype is whole and want.dtype is whole and start.dtype is whole and
+                length.dim() == 1 and want.dim() == 1 and start.dim() == 1 and table.dim() == 2 and table.shape[0] == n and
+                want.numel() == n and start.numel() == n + 1 and table.is_contiguous() and length.is_contiguous() and
+                want.is_contiguous() and start.is_contiguous() and
+                table.get_device() == g and length.get_device() == g and want.get_device() == g and start.get_device() == g):
             tp, lp, wp, sp = table.data_ptr(), length.data_ptr(), want.data_ptr(), start.data_ptr()
         else:
+            n = length.shape[0] if length.dim() else -1
             tp = _tensor(table, "table", "int32", (n, None), g, True)
             lp = _tensor(length, "length", "int32", (n,), g)
             wp = _tensor(want, "want", "int32", (n,), g)
             sp = _tensor(start, "start", "int32", (n + 1,), g)
-        op = lp if length_out is None else _tensor(length_out, "length_out", "int32", (n,), g)
-        qp = self._state if state_out is None else _tensor(state_out, "state_out", "int32", (2,), g)
-        maps = []
-        for t, what, kind in ((slot, "slot", "int64"), (row_seq, "row_seq", "int32"), (row_pos, "row_pos", "int32")):
-            if t is not None:
-                if rows is None:
-                    rows = t.shape[0] if t.dim() else -1
-                maps.append(_tensor(t, what, kind, (rows,), g))
-            else:
-                maps.append(None)
+        op, qp, mp, bp, pp = lp, self._state, 0, 0, 0
+        if length_out is not None:
+            op = self._out(length_out, "length_out", whole, n)
+        if state_out is not None:
+            qp = self._out(state_out, "state_out", whole, 2)
+        if rows is None:
+            for t in (slot, row_seq, row_pos):
+                if t is not None:
+                    rows = t.numel()
+                    break
+        if slot is not None:
+            mp = self._out(slot, "slot", _dtypes["int64"], rows)
+        if row_seq is not None:
+            bp = self._out(row_seq, "row_seq", whole, rows)
+        if row_pos is not None:
+            pp = self._out(row_pos, "row_pos", whole, rows)
         rc = _resize(_pack_pool(self._ring, self._state, qp, self.n_pages, self.page_size),
-                     _pack_wanted(tp, lp, wp, op, sp, *[m or 0 for m in maps], table.stride(0) if n > 1 else max(1, table.shape[1]), n, table.shape[1],
+                     _pack_wanted(tp, lp, wp, op, sp, mp, bp, pp, table.stride(0) if n > 1 else max(1, table.shape[1]), n, table.shape[1],
                                   0x7fffffff if rows is None else rows, 0),
                      None if status is None else _tensor(status, "status", "int32", (1,), g), _stream_handle(stream))
         if rc:
@@ -619,14 +633,20 @@ class Expert:
                            "set_prefix")
 
     def set_prefix_paged(self, robot, caches, table):
-        """set_prefix from pages: the first arch.prefix_len tokens of a sequence. caches: a PagedCache for each layer; table: int32
+        """set_prefix from pages: the first arch.prefix_len tokens of a sequence. caches: a PagedCache for each layer, all of one type; table: int32
         [pages], a tensor or array on the host or the GPU, one for all layers. Synchronous and behind the legacy default stream: what
         other streams write has to be finished first."""
         t = np.ascontiguousarray(table, np.int32) if isinstance(table, (list, tuple)) else table
         if len(t.shape) != 1:
             raise ValueError(f"table: expected the pages of one sequence, got shape {list(t.shape)}")
-        layers = (uad_kv_pages * len(caches))(*[c.pages for c in caches])
-        return self._check(uad_set_prefix_paged(self.h, robot, layers, len(caches), _buf(t, t.shape[0], "int32", "table"), t.shape[0]),
+        eight = [c.block is not None for c in caches]
+        if any(eight) and not all(eight):
+            raise ValueError("caches: 8-bit ones and others")
+        if any(eight):
+            call, layers = uad_set_prefix_paged8, (uad_kv_pages8 * len(caches))(*[c.pages8 for c in caches])
+        else:
+            call, layers = uad_set_prefix_paged, (uad_kv_pages * len(caches))(*[c.pages for c in caches])
+        return self._check(call(self.h, robot, layers, len(caches), _buf(t, t.shape[0], "int32", "table"), t.shape[0]),
                            "set_prefix_paged")
 
     def prepare_times(self, max_budget):

@@ -235,6 +235,29 @@ __global__ void __launch_bounds__(kMostThreads, 1) append8_kernel(const Append8A
   }
 }
 
+// One block a token: 16 codes a thread, keys and values in turn.
+__global__ void __launch_bounds__(256) gather8_kernel(const PagedArgs p, const Scales sc, const int* table, float* k, float* v) {
+  pdl_wait();
+  pdl_trigger();
+  const int per_head = p.dh / 16, all = p.n_kv * per_head, i0 = (int)p.page.div(blockIdx.x), page = table[i0];
+  if ((unsigned)page >= (unsigned)p.n_pages) return;
+  const int slot = blockIdx.x - i0 * (int)p.page.d;
+  for (int i = threadIdx.x; i < 2 * all; i += blockDim.x) {
+    const bool is_v = i >= all;
+    const int r = is_v ? i - all : i, h = r / per_head;
+    const char* from = static_cast<const char*>(is_v ? p.v : p.k) + page * p.page_stride + slot * p.slot_stride + h * p.head_stride + (r - h * per_head) * 16;
+    const float s = (is_v ? sc.v : sc.k)[page * sc.page + (slot >> sc.log_block) * sc.block + h * sc.head];
+    const uint4 w = *reinterpret_cast<const uint4*>(from);
+    float4* to = reinterpret_cast<float4*>((is_v ? v : k) + ((int64_t)blockIdx.x * all + r) * 16);
+    const uint32_t c[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float2 a = e4m3_pair(c[j]), b = e4m3_pair(c[j] >> 16);
+      to[j] = make_float4(a.x * s, a.y * s, b.x * s, b.y * s);
+    }
+  }
+}
+
 int log2_of(int n) {
   int l = 0;
   while ((1 << l) < n) ++l;
@@ -255,6 +278,10 @@ int uad::pages8_args(const uad_kv_pages8* g, const uad_kv_seqs* s, int n_rows, b
   sc->log_block = log2_of(g->block);
   sc->per_page = FastDiv((uint32_t)((g->pages.page_size + g->block - 1) / g->block));
   return UAD_OK;
+}
+
+cudaError_t uad::launch_kv_gather8(const PagedArgs& p, const Scales& sc, const int* table, int n, void* k, void* v, cudaStream_t s) {
+  return launch_k(gather8_kernel, dim3((unsigned)n), 256, 0, s, p, sc, table, static_cast<float*>(k), static_cast<float*>(v));
 }
 
 extern "C" int uad_kv_append8(const uad_kv_pages8* pages, const uad_kv_seqs* seqs, const uad_kv_rows* rows, const uad_rope* rope,

@@ -29,4 +29,8 @@ __device__ __forceinline__ float2 e4m3_pair(uint32_t w) {
 // kv_append8.cu: paged_args and the checks of the scales.
 int pages8_args(const uad_kv_pages8* pages, const uad_kv_seqs* seqs, int n_rows, bool device, PagedArgs* out, Scales* scales);
 
+// kv_append8.cu: tokens 0 .. n - 1 of a sequence, whose pages are table[0 ..] (device memory, checked), next to each other as fp32: k, v
+// [n][n_kv][dh], 16-byte aligned.
+cudaError_t launch_kv_gather8(const PagedArgs& p, const Scales& sc, const int* table, int n, void* k, void* v, cudaStream_t s);
+
 }  // namespace uad

@@ -26,6 +26,9 @@ namespace {
 struct PagedAttn8Args {
   PagedAttnArgs a;
   Scales sc;
+  // Places in 32 bits: of codes in units of the largest power of two that divides all strides (at least 16), of scales in elements.
+  // 64-bit sums and shuffles take 1 to 4% longer with heads of 64 and 128.
+  uint32_t unit, page_units, slot_units, head_units, scale_page, scale_block, scale_head;
   int parts;      // into how many the sequences' chunks are cut evenly; 0: as attn_plan has it
   int2* spans;    // [CTA] the sequence that begins in its part and ends in a later one, and that one; -1: there is none
 };
@@ -118,19 +121,21 @@ constexpr size_t even_smem(int seqs) { return smem8<DH, NR>(1) + (seqs + 1) * 4;
 template <int DH, int NR>
 constexpr int ctas8() { return NR == 4 || DH == 256 ? 2 : DH == 64 && NR == 1 ? 4 : 3; }
 
-// Where a key's codes and scale are in this head, or -1 where no row sees it or its page is none.
+// Where a key's codes and scale are in this head; kNowhere: no row sees it or its page is none.
+constexpr uint32_t kNowhere = 0xffffffffu;
 struct Place {
-  int64_t code, scale;
+  uint32_t code, scale;
 };
-__device__ __forceinline__ Place place_of(const PagedAttnArgs& a, const Scales& sc, const Piece& c, const Found& f) {
-  if (f.key >= c.k1 || !f.shown) return {-1, 0};
+__device__ __forceinline__ Place place_of(const PagedAttn8Args& g, const Piece& c, const Found& f) {
+  const PagedAttnArgs& a = g.a;
+  if (f.key >= c.k1 || !f.shown) return {kNowhere, 0};
   if ((unsigned)f.page >= (unsigned)a.p.n_pages) {
     kv_report(a.p, UAD_KV_BAD_PAGE);
-    return {-1, 0};
+    return {kNowhere, 0};
   }
-  const int slot = f.token - (int)(a.p.page.div(f.token) * a.p.page.d);
-  return {f.page * a.p.page_stride + slot * a.p.slot_stride + c.kvh * a.p.head_stride,
-          f.page * sc.page + (slot >> sc.log_block) * sc.block + c.kvh * sc.head};
+  const uint32_t slot = f.token - a.p.page.div(f.token) * a.p.page.d;
+  return {f.page * g.page_units + slot * g.slot_units + c.kvh * g.head_units,
+          f.page * g.scale_page + (slot >> g.sc.log_block) * g.scale_block + c.kvh * g.scale_head};
 }
 
 // Sharing evenly. A sequence's keys are chunks of four slices; the sequences' chunks one behind the other are cut into as many parts as
@@ -318,7 +323,7 @@ __global__ void __launch_bounds__(kThreads, ctas8<DH, NR>()) paged_attn8_kernel(
   const auto slice_key = [&](int i) { return c.k0 + (i * c.wk + c.kw) * KEYS; };
 
   uint64_t seen = 0;   // KEYS bits a slice, the next one lowest
-  int64_t at[KEYS / AT_ONCE], scale_at = -1;
+  uint32_t at[KEYS / AT_ONCE], scale_at = kNowhere;
   bool whole = true;   // every key of the slice whose places are in `at` is seen
   int slot = 0;
   const uint32_t to = ring + lane / LANES * DH + (lane % LANES ^ key_swap<DH>(lane / LANES)) * 16;
@@ -331,28 +336,29 @@ __global__ void __launch_bounds__(kThreads, ctas8<DH, NR>()) paged_attn8_kernel(
 #pragma unroll
       for (int h = 0; h < KEYS / AT_ONCE; ++h)
 #pragma unroll
-        for (int x = 0; x < DH / (16 * LANES); ++x) cp16_if(place(h) + x * 16 * LANES, src + at[h] + x * 16 * LANES, at[h] >= 0);
+        for (int x = 0; x < DH / (16 * LANES); ++x)
+          cp16_if(place(h) + x * 16 * LANES, src + (uint64_t)at[h] * args.unit + x * 16 * LANES, at[h] != kNowhere);
       if (values && !whole) {
 #pragma unroll
         for (int h = 0; h < KEYS / AT_ONCE; ++h)
 #pragma unroll
           for (int x = 0; x < DH / (16 * LANES); ++x)
-            if (at[h] < 0) sts_zero16(place(h) + x * 16 * LANES);
+            if (at[h] == kNowhere) sts_zero16(place(h) + x * 16 * LANES);
       }
-      if (lane < KEYS) cp4_or_zero(ring + slot * SLOT + SCALES + 4 * lane, scales + (scale_at < 0 ? 0 : scale_at), scale_at >= 0);
+      if (lane < KEYS) cp4_or_zero(ring + slot * SLOT + SCALES + 4 * lane, scales + (scale_at == kNowhere ? 0 : scale_at), scale_at != kNowhere);
     }
     cp_commit();
     slot = slot + 1 == SLOTS ? 0 : slot + 1;
   };
   const auto copy_k = [&](int i, int ahead, const Found& fnd) {
-    Place e{-1, 0};
-    if (i < mine) e = place_of(a, args.sc, c, fnd);
-    const uint32_t there = __ballot_sync(0xffffffffu, e.code >= 0) & (0xffffffffu >> (32 - KEYS));
+    Place e{kNowhere, 0};
+    if (i < mine) e = place_of(args, c, fnd);
+    const uint32_t there = __ballot_sync(0xffffffffu, e.code != kNowhere) & (0xffffffffu >> (32 - KEYS));
     whole = there == 0xffffffffu >> (32 - KEYS);
     seen |= (uint64_t)there << (KEYS * ahead);
 #pragma unroll
     for (int h = 0; h < KEYS / AT_ONCE; ++h) at[h] = __shfl_sync(0xffffffffu, e.code, AT_ONCE * h + lane / LANES);
-    scale_at = e.code < 0 ? -1 : e.scale;
+    scale_at = e.code == kNowhere ? kNowhere : e.scale;
     copy(i, a.p.k, args.sc.k, false);
   };
   const auto next_k = [&](int i) {
@@ -786,6 +792,23 @@ int attn8_args(const uad_kv_pages8* pages, const uad_kv_seqs* seqs, const uad_at
   if (!t) return UAD_EINVAL;
   int rc = pages8_args(pages, seqs, t->n_rows, device, &a->a.p, &a->sc);
   if (rc) return rc;
+  const uad_kv_pages& g = pages->pages;
+  // offsets in 32 bits: of codes in units of the strides, of scales in elements
+  const int64_t any = g.page_stride | g.slot_stride | g.head_stride, unit = any & -any, top = 0xffffffffll;
+  const int blocks = (g.page_size + pages->block - 1) / pages->block;
+  if (g.page_stride / unit > top || g.slot_stride / unit > top || g.head_stride / unit > top || pages->scale_page_stride > top ||
+      pages->scale_block_stride > top || pages->scale_head_stride > top)
+    return UAD_EINVAL;
+  const auto last = [&](int64_t page, int64_t inner, int n, int64_t head) {   // below 2^31 2^32 each
+    return (double)(g.n_pages - 1) * page + (double)(n - 1) * inner + (double)(g.n_kv_heads - 1) * head;
+  };
+  if (last(g.page_stride / unit, g.slot_stride / unit, g.page_size, g.head_stride / unit) >= (double)top ||
+      last(pages->scale_page_stride, pages->scale_block_stride, blocks, pages->scale_head_stride) >= (double)top)
+    return UAD_EINVAL;
+  a->unit = (uint32_t)unit;
+  a->page_units = (uint32_t)(g.page_stride / unit); a->slot_units = (uint32_t)(g.slot_stride / unit); a->head_units = (uint32_t)(g.head_stride / unit);
+  a->scale_page = (uint32_t)pages->scale_page_stride; a->scale_block = (uint32_t)pages->scale_block_stride;
+  a->scale_head = (uint32_t)pages->scale_head_stride;
   const int dh = a->a.p.dh;
   const AttnFit8 fit = dh == 64 ? fit8<64>() : dh == 128 ? fit8<128>() : fit8<256>();
   rc = attn_split(seqs, t, sinks, device, &fit, &a->a);

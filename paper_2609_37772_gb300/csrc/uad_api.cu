@@ -16,7 +16,7 @@
 #include <vector>
 
 #include "../../include/uad.h"
-#include "kv_pages.cuh"
+#include "kv_pages8.cuh"
 #include "uad_internal.cuh"
 
 using namespace uad;
@@ -1297,18 +1297,22 @@ int uad_set_prefix_kv(uad_ctx* c, int32_t robot, const void* k, const void* v, i
   return UAD_OK;
 }
 
-int uad_set_prefix_paged(uad_ctx* c, int32_t robot, const uad_kv_pages* layers, int32_t n_layers, const int32_t* table,
-                         int32_t table_len) {
-  if (!c) return UAD_EINVAL;
+}  // extern "C"
+
+// The prefix from pages of one type: layer(l) gives the pages of a layer, args(l, one, p) checks them (UAD_OK) for a sequence `one`, gather(l, p,
+// table, k, v) copies the prefix's tokens next to each other in dtype.
+template <class Layer, class Args, class Gather>
+static int prefix_paged(uad_ctx* c, int32_t robot, bool given, int32_t n_layers, const int32_t* table, int32_t table_len, int dtype, Layer layer,
+                        Args args, Gather gather) {
   const uad_arch& a = c->a;
   if (robot < 0 || robot >= a.max_batch) return fail(c, UAD_EINVAL, "robot %d out of range", robot);
   if (a.kind == UAD_KIND_DIT) return fail(c, UAD_EINVAL, "DiT takes prefix tokens, not keys and values");
-  if (!layers || !table) return fail(c, UAD_EINVAL, "null pages or table");
+  if (!given || !table) return fail(c, UAD_EINVAL, "null pages or table");
   if (n_layers != a.n_layers) return fail(c, UAD_EINVAL, "%d layers of pages, the expert has %d", n_layers, a.n_layers);
   if (c->in_flight) return fail(c, UAD_ESTATE, "a chunk is in flight");
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev != c->dev) return fail(c, UAD_EINVAL, "the context's device is not the current one");
-  const int page = layers[0].page_size, pages = page > 0 ? (a.prefix_len + page - 1) / page : 0;
+  const int page = layer(0).page_size, pages = page > 0 ? (a.prefix_len + page - 1) / page : 0;
   if (page < 1 || table_len < pages) return fail(c, UAD_EINVAL, "%d pages in the table, the prefix has %d", table_len, pages);
   PagedArgs p;
   uad_kv_seqs one{};
@@ -1316,16 +1320,15 @@ int uad_set_prefix_paged(uad_ctx* c, int32_t robot, const uad_kv_pages* layers, 
   one.max_new = 1;
   int n_pages = INT32_MAX;
   for (int l = 0; l < n_layers; ++l) {
-    const uad_kv_pages& g = layers[l];
-    if (paged_args(&g, &one, 0, false, &p) != UAD_OK || g.dtype != layers[0].dtype || g.page_size != page ||
-        g.n_kv_heads != a.n_kv_heads || g.head_dim != a.head_dim)
+    const uad_kv_pages& g = layer(l);
+    if (args(l, one, &p) != UAD_OK || g.dtype != layer(0).dtype || g.page_size != page || g.n_kv_heads != a.n_kv_heads || g.head_dim != a.head_dim)
       return fail(c, UAD_EINVAL, "layer %d: the pages break a rule of uad_kv_pages or do not fit the expert", l);
     if (!on_current_device(g.k) || !on_current_device(g.v)) return fail(c, UAD_EINVAL, "layer %d: pages on another device", l);
     n_pages = std::min(n_pages, g.n_pages);
   }
   cudaStream_t s = c->worker;
   int rc = after_default_stream(c, s);
-  if (rc || a.prefix_len == 0) return rc ? rc : uad_set_prefix_kv(c, robot, layers[0].k, layers[0].v, 0, layers[0].dtype);
+  if (rc || a.prefix_len == 0) return rc ? rc : uad_set_prefix_kv(c, robot, layer(0).k, layer(0).v, 0, dtype);
   const std::unique_ptr<int32_t[]> host(new (std::nothrow) int32_t[pages]);
   if (!host) return fail(c, UAD_ENOMEM, "prefix table");
   if (cudaMemcpyAsync(host.get(), table, (size_t)pages * 4, cudaMemcpyDefault, s) != cudaSuccess || cudaStreamSynchronize(s) != cudaSuccess) {
@@ -1334,8 +1337,8 @@ int uad_set_prefix_paged(uad_ctx* c, int32_t robot, const uad_kv_pages* layers, 
   }
   for (int i = 0; i < pages; ++i)
     if (host[i] < 0 || host[i] >= n_pages) return fail(c, UAD_EINVAL, "page %d of the table: %d of %d", i, host[i], n_pages);
-  const int es = p.dtype == F32 ? 4 : 2;
-  const size_t layer = (size_t)a.prefix_len * c->kvd * es, half = layer * a.n_layers;   // kvd: a multiple of 64
+  const int es = dtype == UAD_DTYPE_F32 ? 4 : 2;
+  const size_t bytes = (size_t)a.prefix_len * c->kvd * es, half = bytes * a.n_layers;   // kvd: a multiple of 64
   void* st = nullptr;
   rc = stage_at(c, 0, 2 * half + (size_t)pages * 4, &st);
   if (rc) return rc;
@@ -1343,15 +1346,39 @@ int uad_set_prefix_paged(uad_ctx* c, int32_t robot, const uad_kv_pages* layers, 
   int* dev_table = reinterpret_cast<int*>(at + 2 * half);
   cudaError_t e = cudaMemcpyAsync(dev_table, host.get(), (size_t)pages * 4, cudaMemcpyHostToDevice, s);
   for (int l = 0; l < n_layers && e == cudaSuccess; ++l) {
-    paged_args(layers + l, &one, 0, false, &p);
-    e = launch_kv_gather(p, dev_table, a.prefix_len, at + l * layer, at + half + l * layer, s);
+    args(l, one, &p);
+    e = gather(l, p, dev_table, at + l * bytes, at + half + l * bytes, s);
   }
   if (e != cudaSuccess) {
     cudaStreamSynchronize(s);
     cudaGetLastError();
     return fail(c, UAD_ECUDA, "prefix pages");
   }
-  return uad_set_prefix_kv(c, robot, at, at + half, a.prefix_len, layers[0].dtype);
+  return uad_set_prefix_kv(c, robot, at, at + half, a.prefix_len, dtype);
+}
+
+extern "C" {
+
+int uad_set_prefix_paged(uad_ctx* c, int32_t robot, const uad_kv_pages* layers, int32_t n_layers, const int32_t* table,
+                         int32_t table_len) {
+  if (!c) return UAD_EINVAL;
+  return prefix_paged(
+      c, robot, layers, n_layers, table, table_len, layers ? layers[0].dtype : UAD_DTYPE_F32, [&](int l) -> const uad_kv_pages& { return layers[l]; },
+      [&](int l, const uad_kv_seqs& one, PagedArgs* p) { return paged_args(layers + l, &one, 0, false, p); },
+      [&](int, const PagedArgs& p, const int* t, void* k, void* v, cudaStream_t s) { return launch_kv_gather(p, t, c->a.prefix_len, k, v, s); });
+}
+
+int uad_set_prefix_paged8(uad_ctx* c, int32_t robot, const uad_kv_pages8* layers, int32_t n_layers, const int32_t* table,
+                          int32_t table_len) {
+  if (!c) return UAD_EINVAL;
+  Scales sc;
+  return prefix_paged(
+      c, robot, layers, n_layers, table, table_len, UAD_DTYPE_F32, [&](int l) -> const uad_kv_pages& { return layers[l].pages; },
+      [&](int l, const uad_kv_seqs& one, PagedArgs* p) {
+        const int rc = pages8_args(layers + l, &one, 0, false, p, &sc);
+        return rc ? rc : on_current_device(sc.k) && on_current_device(sc.v) ? UAD_OK : UAD_EINVAL;
+      },
+      [&](int, const PagedArgs& p, const int* t, void* k, void* v, cudaStream_t s) { return launch_kv_gather8(p, sc, t, c->a.prefix_len, k, v, s); });
 }
 
 int uad_prepare_times(uad_ctx* c, int32_t max_budget) {
