@@ -499,15 +499,10 @@ __global__ void __launch_bounds__(kThreads, ctas8<DH, NR>()) paged_attn8_kernel(
     __syncwarp();
     // the values' scales: a power of two that none is above goes before the sums
     const float own_scale = lds_f(ring + use * SLOT + SCALES + 4 * (lane & (KEYS - 1)));
-    float raised = 1.f;
-    if (__any_sync(0xffffffffu, own_scale > ref)) {
-      const uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(own_scale));
-      const float now = __uint_as_float(min((most + 0x7fffffu) & 0xff800000u, 254u << 23));
-      raised = ref / now;
+    if (__any_sync(0xffffffffu, grew || own_scale > ref)) {
+      const uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(fmaxf(own_scale, ref)));
+      const float now = __uint_as_float(min((most + 0x7fffffu) & 0xff800000u, 254u << 23)), raised = ref / now;
       ref = now;
-      grew = true;
-    }
-    if (i > 0 && __any_sync(0xffffffffu, grew)) {
 #pragma unroll
       for (int n = 0; n < NR; ++n) {
         const float f0 = __shfl_sync(0xffffffffu, f[n], 8 * t) * raised, f1 = __shfl_sync(0xffffffffu, f[n], 8 * t + 4) * raised;
@@ -662,8 +657,8 @@ __global__ void __launch_bounds__(kThreads, ctas8<DH, NR>()) paged_attn8_kernel(
 template <int DH, int NR>
 __global__ void __launch_bounds__(kThreads) paged_join8_kernel(const PagedAttn8Args args) {
   const PagedAttnArgs& a = args.a;
-  // No early start for the kernel behind it: beside CTAs of a kernel without shared memory, an SM has no room for three of the attention's,
-  // and stays so (64 x 4000 keys of 32 heads over 8 of 128, call after call: 137 us against 96).
+  // No early start for the kernel behind it: where this one's CTAs are still there, an SM does not take as many of the next attention's as it
+  // could, and the one wave of those becomes two (64 x 4000 keys of 32 heads over 8 of 128, call after call: 137 us against 96).
   pdl_wait();
   constexpr int FOURS = 8 * NR / kWarps;
   const int head = blockIdx.y / (DH / 64), column = blockIdx.y % (DH / 64), block = blockIdx.z / FOURS;
@@ -739,13 +734,7 @@ cudaError_t launch8(const PagedAttn8Args& a, cudaStream_t s) {
   });
   if (e != cudaSuccess) return e;
   const dim3 grid(a.parts, a.a.p.n_kv, a.a.row_blocks);
-  // Behind the kernel before it, not into its end: its one wave of CTAs has to find the SMs as it fills them.
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = grid;
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = even_smem<DH, NR>(a.a.p.n_seqs);
-  cfg.stream = s;
-  e = cudaLaunchKernelEx(&cfg, kernel, a);
+  e = launch_k(kernel, grid, dim3(kThreads), even_smem<DH, NR>(a.a.p.n_seqs), s, a);
   return e != cudaSuccess ? e : launch_k(paged_join8_kernel<DH, NR>, dim3(a.parts, a.a.p.n_kv * (DH / 64), a.a.row_blocks * (8 * NR / kWarps)), kThreads, 0, s, a);
 }
 
@@ -768,8 +757,7 @@ int64_t attn8_bytes(const PagedAttn8Args& a) {
   return a.parts ? even_ctas(a) * (2 * 8 * a.a.row_tiles * (a.a.p.dh + 2) * 4 + 8) + 8 : attn_bytes(a.a);
 }
 
-// Into how many parts the chunks are cut; 0: not evenly. Evenly, a call costs about 6 us more (the sums, a second kernel, no start beside the
-// kernel before it) and a CTA about 4 us for each further sequence, and it gains what SMs idle otherwise: pieces in waves of which the last
+// Into how many parts the chunks are cut; 0: not evenly. Evenly, a call costs about 6 us more (the sums, a second kernel) and a CTA about 4 us for each further sequence, and it gains what SMs idle otherwise: pieces in waves of which the last
 // is part-filled, and lengths that differ. So the CTAs' shares have to last some 24 us at the rates (keys a microsecond and CTA) at
 // which they come, and to be half a sequence long at least. In us, evenly / as attn_plan has it, for equal lengths and for a
 // quarter of the longest and more:
