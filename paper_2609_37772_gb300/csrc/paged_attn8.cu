@@ -316,9 +316,11 @@ __global__ void __launch_bounds__(kThreads, ctas8<DH, NR>()) paged_attn8_kernel(
       sts_u32(sq + r * QPITCH + 2 * ((d & ~15) + (x >> 2) * 2 + (x & 2) * 4), pack_f16(__uint_as_float(w[i] << 16) * f, __uint_as_float(w[i] & 0xffff0000u) * f));
     }
   };
-  uint32_t qw[2 * NR][W];
+  // a warp's share of the CTA's rows, or the first half of its own
+  uint32_t qw[4 * NR][W];
 #pragma unroll
-  for (int i = 0; i < 2 * NR; ++i) get_query(a.warp_heads ? i : warp + kWarps * i, qw[i]);
+  for (int i = 0; i < 4 * NR; ++i)
+    if (i < 2 * NR || a.warp_heads) get_query(a.warp_heads ? i : warp + kWarps * i, qw[i]);
   const int slices = (c.k1 - c.k0 + KEYS - 1) / KEYS, mine = (slices - c.kw + c.wk - 1) / c.wk;
   const auto slice_key = [&](int i) { return c.k0 + (i * c.wk + c.kw) * KEYS; };
 
@@ -374,14 +376,14 @@ __global__ void __launch_bounds__(kThreads, ctas8<DH, NR>()) paged_attn8_kernel(
   found = first[AHEAD];
 
 #pragma unroll
-  for (int i = 0; i < 2 * NR; ++i) put_query(a.warp_heads ? i : warp + kWarps * i, qw[i]);
-  if (a.warp_heads)
-#pragma unroll 1
-    for (int r = 2 * NR; r < 8 * NR; ++r) {
-      uint32_t w[W];
-      get_query(r, w);
-      put_query(r, w);
-    }
+  for (int i = 0; i < 4 * NR; ++i)
+    if (i < 2 * NR || a.warp_heads) put_query(a.warp_heads ? i : warp + kWarps * i, qw[i]);
+  if (a.warp_heads) {
+#pragma unroll
+    for (int i = 0; i < 4 * NR; ++i) get_query(4 * NR + i, qw[i]);
+#pragma unroll
+    for (int i = 0; i < 4 * NR; ++i) put_query(4 * NR + i, qw[i]);
+  }
   float o[STEPS][NR][4] = {}, m[2 * MT], l[2 * MT], rf[2 * MT];
 #pragma unroll
   for (int i = 0; i < 2 * MT; ++i) m[i] = -INFINITY, l[i] = 0.f;

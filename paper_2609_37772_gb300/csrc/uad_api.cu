@@ -1363,7 +1363,7 @@ int uad_set_prefix_paged(uad_ctx* c, int32_t robot, const uad_kv_pages* layers, 
                          int32_t table_len) {
   if (!c) return UAD_EINVAL;
   return prefix_paged(
-      c, robot, layers, n_layers, table, table_len, layers ? layers[0].dtype : UAD_DTYPE_F32, [&](int l) -> const uad_kv_pages& { return layers[l]; },
+      c, robot, layers, n_layers, table, table_len, layers && n_layers > 0 ? layers[0].dtype : UAD_DTYPE_F32, [&](int l) -> const uad_kv_pages& { return layers[l]; },
       [&](int l, const uad_kv_seqs& one, PagedArgs* p) { return paged_args(layers + l, &one, 0, false, p); },
       [&](int, const PagedArgs& p, const int* t, void* k, void* v, cudaStream_t s) { return launch_kv_gather(p, t, c->a.prefix_len, k, v, s); });
 }
