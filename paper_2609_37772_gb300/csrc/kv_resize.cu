@@ -105,8 +105,9 @@ template <typename T>
 __global__ void __launch_bounds__(kThreads) resize_kernel(const ResizeArgs a) {
   __shared__ int take_at[kChunk], give_at[kChunk], row_at[kChunk], had[kChunk], kept[kChunk];   // kept: pages that it shall have
   __shared__ T sums[kThreads / 32][3], row_sums[kThreads / 32][1];
-  __shared__ int taken_end;
-  if (threadIdx.x == 0) taken_end = 0;
+  __shared__ int taken_here;
+  constexpr int64_t most_of_t = sizeof(T) == 4 ? 0x7fffffff : 0x7fffffffffffffff;
+  const auto clip = [](T x) { return sizeof(T) == 4 ? (int)x : (int)min((int64_t)x, (int64_t)0x7fffffff); };
   pdl_wait();
   pdl_trigger();
   int len[kOwn], want[kOwn];
@@ -159,8 +160,10 @@ __global__ void __launch_bounds__(kThreads) resize_kernel(const ResizeArgs a) {
     block_scan<3, T>(v, total, sums);   // its barrier: the chunk before has been read by all
     // Who is served: in order, as far as pages and rows go. The sums count everybody, so that behind one who is not served nobody
     // is who needs more of the same: the pages taken are the first ones without a gap.
+    // Places are counted from the chunk's beginning.
     const bool everybody = asked_pages + total[0] <= count && asked_rows + total[2] <= a.n_rows && asked_rows == rows;
-    int64_t pages_end = asked_pages + v[0], back = given + v[1], rows_end = asked_rows + v[2];
+    const T pages_left = (T)max(min(count - asked_pages, most_of_t), (int64_t)-1), rows_left = (T)max(min(a.n_rows - asked_rows, most_of_t), (int64_t)-1);
+    const T room_left = (T)max(room - given, (int64_t)-1);
     T served[1] = {0}, all_served = total[2];
     bool ok[kOwn];
     int most = 0;
@@ -170,28 +173,30 @@ __global__ void __launch_bounds__(kThreads) resize_kernel(const ResizeArgs a) {
       ok[i] = true;
       had[k] = len[i];
       kept[k] = need[i];
-      take_at[k] = (int)min(pages_end, (int64_t)0x7fffffff);
-      give_at[k] = (int)min(back, (int64_t)0x7fffffff);
-      row_at[k] = (int)rows_end;   // where everybody is served
-      if (add > 0) {
-        pages_end += need[i] - held[i];
-        rows_end += add;
-        ok[i] = (need[i] == held[i] || pages_end <= count) && rows_end <= a.n_rows;
+      take_at[k] = clip(v[0]);
+      give_at[k] = clip(v[1]);
+      row_at[k] = clip(v[2]);   // where everybody is served
+      v[0] += max(need[i] - held[i], 0);
+      v[1] += max(held[i] - need[i], 0);
+      v[2] += max(add, 0);
+      if (add > 0 && !everybody) {
+        ok[i] = (need[i] == held[i] || v[0] <= pages_left) && v[2] <= rows_left;
         if (!ok[i]) report |= UAD_KV_NO_ROOM;
         else served[0] += add;
-        if (ok[i] && need[i] > held[i]) most = (int)pages_end;
-      } else {
-        back += held[i] - need[i];
-        if (back > room && held[i] > need[i]) report |= UAD_KV_BAD_POOL;
+        if (ok[i] && need[i] > held[i]) most = (int)v[0];
       }
+      if (held[i] > need[i] && v[1] > room_left) report |= UAD_KV_BAD_POOL;
     }
     if (!everybody) {   // rows and pages once more, of those who are served
       most = (int)__reduce_max_sync(0xffffffffu, (unsigned)most);
-      if ((threadIdx.x & 31) == 0) atomicMax(&taken_end, max(most, taken));
+      if (base > 0) __syncthreads();   // the chunk before has read it
+      if (threadIdx.x == 0) taken_here = 0;
+      __syncthreads();
+      if ((threadIdx.x & 31) == 0) atomicMax(&taken_here, most);
       T all[1];
       block_scan<1, T>(served, all, row_sums);
       all_served = all[0];
-      int at = rows + (int)served[0];
+      int at = (int)served[0];
 #pragma unroll
       for (int i = 0; i < kOwn; ++i) {
         row_at[threadIdx.x * kOwn + i] = at;
@@ -203,33 +208,33 @@ __global__ void __launch_bounds__(kThreads) resize_kernel(const ResizeArgs a) {
       for (int i = 0; i < kOwn; ++i) {
         const int k = threadIdx.x * kOwn + i, b = base + k;
         if (b >= a.n_seqs) continue;
-        if (a.fill) a.start[b] = row_at[k];
+        if (a.fill) a.start[b] = rows + row_at[k];
         if (a.update) a.len_out[b] = ok[i] ? want[i] : len[i];
       }
     }
-    __syncthreads();   // places and taken_end
+    __syncthreads();   // places and taken_here
     load(base + chunk);   // the next chunk, on its way meanwhile
-    const int m = min(chunk, a.n_seqs - base), rows_to = rows + (int)all_served, taken_to = everybody ? (int)(asked_pages + total[0]) : taken_end;
-    const int given_from = (int)min(given, (int64_t)room), given_to = (int)min((int64_t)(given + total[1]), (int64_t)room);
+    const int m = min(chunk, a.n_seqs - base), n_rows = (int)all_served, n_taken = everybody ? (int)total[0] : taken_here;
+    const int n_given = (int)max(min((int64_t)total[1], (int64_t)room_left), (int64_t)0);
     if (a.fill && turn == share) {
       // Rows, pages taken and pages given back begin with different threads, so that few of each are worked on at the same time.
-      for (uint32_t i = step - 1 - id; i < (uint32_t)(taken_to - taken); i += step) {
-        const int t = taken + (int)i, k = owner_of(take_at, m, t);
-        a.table[(base + k) * a.table_stride + pages_of(had[k]) + t - take_at[k]] = a.ring[on_ring(t)];
+      for (uint32_t i = step - 1 - id; i < (uint32_t)n_taken; i += step) {
+        const int k = owner_of(take_at, m, (int)i);
+        a.table[(base + k) * a.table_stride + pages_of(had[k]) + (int)i - take_at[k]] = a.ring[on_ring(taken + i)];
       }
-      for (uint32_t i = id < step / 2 ? id + step / 2 : id - step / 2; i < (uint32_t)(given_to - given_from); i += step) {
-        const int t = given_from + (int)i, k = owner_of(give_at, m, t);
-        a.ring[on_ring(count + t)] = a.table[(base + k) * a.table_stride + kept[k] + t - give_at[k]];
+      for (uint32_t i = id < step / 2 ? id + step / 2 : id - step / 2; i < (uint32_t)n_given; i += step) {
+        const int k = owner_of(give_at, m, (int)i);
+        a.ring[on_ring(count + (uint32_t)given + i)] = a.table[(base + k) * a.table_stride + kept[k] + (int)i - give_at[k]];
       }
       if (a.maps) {
-        for (uint32_t i = (uint32_t)rows / 4 + id; i < ((uint32_t)rows_to + 3) / 4; i += step) {
+        for (uint32_t i = (uint32_t)rows / 4 + id; i < ((uint32_t)(rows + n_rows) + 3) / 4; i += step) {
           const int r0 = (int)i * 4, begin = max(r0, rows);
-          int k = owner_of(row_at, m, begin), last = -1, page = 0;
+          int k = owner_of(row_at, m, begin - rows), last = -1, page = 0;
           Rows4 x;
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const int r = r0 + j;
-            if (r < begin || r >= rows_to) continue;
+            const int r = r0 + j - rows;
+            if (r < 0 || r >= n_rows) continue;
             if (k + 1 < m && row_at[k + 1] <= r) {   // the next one, or behind a run of those without rows
               ++k;
               if (k + 1 < m && row_at[k + 1] <= r) k += 1 + owner_of(row_at + k + 1, m - k - 1, r);
@@ -238,7 +243,7 @@ __global__ void __launch_bounds__(kThreads) resize_kernel(const ResizeArgs a) {
             const int pos = had[k] + r - row_at[k], pi = (int)a.page.div(pos);
             if (a.slot && pi != last) {
               const int own = pages_of(had[k]);
-              page = pi < own ? a.table[(base + k) * a.table_stride + pi] : a.ring[on_ring(take_at[k] + pi - own)];
+              page = pi < own ? a.table[(base + k) * a.table_stride + pi] : a.ring[on_ring(taken + take_at[k] + pi - own)];
               last = pi;
               if ((unsigned)page >= (unsigned)n) report |= UAD_KV_BAD_PAGE;
             }
@@ -246,7 +251,7 @@ __global__ void __launch_bounds__(kThreads) resize_kernel(const ResizeArgs a) {
             x.pos[j] = pos;
             x.slot[j] = (unsigned)page < (unsigned)n ? (int64_t)page * a.page.d + (pos - pi * (int)a.page.d) : -1;
           }
-          put_rows(a, r0, rows, rows_to, x);
+          put_rows(a, r0, rows, rows + n_rows, x);
         }
       }
     }
@@ -254,8 +259,8 @@ __global__ void __launch_bounds__(kThreads) resize_kernel(const ResizeArgs a) {
     asked_pages += total[0];
     given += total[1];
     asked_rows += total[2];
-    rows = rows_to;
-    taken = taken_to;
+    rows += n_rows;
+    taken += n_taken;
   }
   if (a.fill) {
     if (a.maps) {   // rows of nobody
