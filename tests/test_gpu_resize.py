@@ -190,3 +190,23 @@ def test_a_captured_loop_of_steps():
         assert np.array_equal(table.cpu().numpy(), p.table) and np.array_equal(lens.cpu().numpy(), p.lens) and state.tolist() == list(p.state)
         assert start.tolist() == made[4] and slot.tolist() == [m[0] for m in made[5]] + [-1] * (4 - len(made[5]))
     assert int(status) == bits == uad.UAD_KV_NO_ROOM | uad.UAD_KV_BAD_SEQ
+
+
+def test_the_binding_refuses_tensors_that_do_not_fit():
+    ring, state = torch.arange(9, dtype=torch.int32, device="cuda"), torch.tensor([0, 9], dtype=torch.int32, device="cuda")
+    pool = uad.PagePool(ring, state, 4)
+    fine = dict(table=torch.full((2, 4), -1, dtype=torch.int32, device="cuda"), length=torch.zeros(2, dtype=torch.int32, device="cuda"),
+                want=torch.ones(2, dtype=torch.int32, device="cuda"), start=torch.zeros(3, dtype=torch.int32, device="cuda"))
+    slot = torch.zeros(4, dtype=torch.int64, device="cuda")
+    for kw in (dict(table=fine["table"].long()), dict(table=fine["table"][:1]), dict(table=fine["table"].t()), dict(length=fine["length"].cpu()),
+               dict(want=fine["want"][:1]), dict(start=fine["start"][:2]), dict(want=torch.ones(4, dtype=torch.int32, device="cuda")[::2]),
+               dict(length_out=fine["start"]), dict(state_out=fine["start"]), dict(slot=slot.int()), dict(slot=slot, row_seq=fine["start"]),
+               dict(slot=slot, rows=5), dict(slot=slot, row_pos=slot), dict(status=fine["want"]), dict(status=slot[:1])):
+        with pytest.raises(ValueError):
+            pool.resize(**(fine | kw))
+    with pytest.raises(uad.UADError):
+        pool.resize(**(fine | dict(table=torch.zeros((2, 0), dtype=torch.int32, device="cuda"))))
+    torch.cuda.synchronize()
+    assert state.tolist() == [0, 9] and fine["length"].tolist() == [0, 0]
+    with pytest.raises(uad.UADError):
+        uad.PagePool(ring, state, 0).resize(**fine)
