@@ -139,6 +139,23 @@ def test_queries_in_place_need_bf16_rows_of_one_stride():
         assert call_append(pages8(), seqs(n_seqs=0), r) == (uad.UAD_OK if sound else uad.UAD_EINVAL)
 
 
+def test_offsets_of_32_bits():
+    """Codes in units of the strides' common power of two, scales in elements; what lies beyond is refused by the attention."""
+    def need(inner=None, **kw):
+        return uad.uad_paged_attention8_workspace(pages8(inner, **kw), seqs(), attn(), 0)
+
+    assert need(dict(n_pages=1 << 24, page_stride=16 * 1024, slot_stride=1024, head_stride=64)) >= 0            # 256 GiB in units of 64 bytes
+    assert need(dict(n_pages=(1 << 24) + 1, page_stride=16 * 1024, slot_stride=1024, head_stride=64)) == uad.UAD_EINVAL
+    assert need(dict(n_pages=1 << 21, page_stride=16 * 2000, slot_stride=2000, head_stride=80)) >= 0            # 62.5 GiB in units of 16
+    assert need(dict(n_pages=1 << 22, page_stride=16 * 2000, slot_stride=2000, head_stride=80)) == uad.UAD_EINVAL
+    for kw in (dict(page_stride=1 << 62), dict(slot_stride=1 << 62), dict(head_stride=1 << 62), dict(page_stride=1 << 62, n_pages=(1 << 31) - 1)):
+        assert need(dict(dict(n_pages=4), **kw)) in (0, uad.UAD_EINVAL)   # counted without overflow
+    for kw in (dict(scale_page_stride=1 << 33), dict(scale_block_stride=1 << 32), dict(scale_head_stride=1 << 40)):
+        assert need(**kw) == uad.UAD_EINVAL
+    assert need(dict(n_pages=1 << 20), scale_page_stride=1 << 11) >= 0
+    assert need(dict(n_pages=1 << 21), scale_page_stride=1 << 12) == uad.UAD_EINVAL
+
+
 def test_a_workspace_without_a_window_holds_for_every_window_and_sinks():
     rng = np.random.default_rng(0)
     heads = [(8, 1, 256), (4, 1, 128), (8, 2, 64), (24, 24, 64), (32, 8, 128), (4, 2, 64)]

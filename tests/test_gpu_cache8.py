@@ -518,6 +518,43 @@ def test_attention_leaves_out_bad_pages():
     check_attention(c, q, out, lse, mask=mask)
 
 
+@pytest.mark.parametrize("layout", ["apart", "joint"])
+def test_offsets_past_32_bits(layout):
+    """The same tokens in the first pages of a small pool and the last ones of pools of more than 2^32 bytes: the same bits."""
+    c = Case8((8, 1, 256), 64, [200, 65, 333], [5, 1, 70], 32, seed=21)
+    cache = c.on_gpu()
+    n = 300000   # pages of 16 KiB
+    if layout == "apart":
+        k, v = (torch.empty((n, 64, 1, 256), dtype=torch.uint8, device="cuda").view(CODES) for _ in range(2))
+    else:
+        both = torch.empty((n, 2, 64, 1, 256), dtype=torch.uint8, device="cuda").view(CODES)
+        k, v = both[:, 0], both[:, 1]
+    ks, vs = (torch.empty((n, 2, 1), device="cuda") for _ in range(2))
+    shift = n - c.pages
+    for far, near in ((k, cache.k), (v, cache.v)):
+        far[shift:].view(torch.uint8).copy_(near.view(torch.uint8))
+    ks[shift:], vs[shift:] = cache.k_scale, cache.v_scale
+    big = uad.PagedCache(k, v, ks, vs, block=32)
+    small, seqs = c.sequences(), c.dev
+    table = torch.where(seqs[0] >= 0, seqs[0] + shift, seqs[0])
+    large = uad.Sequences(table, seqs[1], seqs[2], max_new=70)
+    x = torch.randn(c.rows, 10 * 256, device="cuda")
+    got = []
+    for kv, s in ((cache, small), (big, large)):
+        q = torch.zeros(c.rows, 2048, device="cuda", dtype=torch.bfloat16)
+        out = torch.zeros_like(q)
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        kv.append(s, x[:, 2048:2304], x[:, 2304:], q=x[:, :2048], q_out=q, rope=uad.rope(10000.0, 256), status=status)
+        ws = torch.empty(kv.attention_workspace(s, c.rows, 8), dtype=torch.uint8, device="cuda")
+        kv.attention(s, q, out, ws, status=status)
+        torch.cuda.synchronize()
+        assert int(status) == 0
+        got.append((out, kv.k.view(torch.uint8)[-c.pages:].clone(), kv.v.view(torch.uint8)[-c.pages:].clone(), kv.k_scale[-c.pages:].clone(), kv.v_scale[-c.pages:].clone()))
+    assert torch.equal(got[0][0], got[1][0])
+    for a, b in zip(got[0][1:], got[1][1:]):
+        assert torch.equal(a.nan_to_num() if a.is_floating_point() else a, b.nan_to_num() if b.is_floating_point() else b)
+
+
 def test_the_same_every_time():
     c = Case8((8, 1, 256), 16, [4000, 17, 900], [3, 1, 2], seed=12)
     s, cache = c.sequences(), c.on_gpu()
