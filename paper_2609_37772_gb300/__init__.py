@@ -507,20 +507,21 @@ class PagePool:
         (page * page_size + slot), sequence and position, -1 behind the last one. rows: what the token tensors hold (None: the
         slot maps' length; without one, no limit). Sequences that find no page or row stay as they were (UAD_KV_NO_ROOM in `status`);
         want below length gives pages back."""
-        g, n, whole = self._gpu, length.numel(), _dtypes["int32"]
+        g, n, whole, shape = self._gpu, length.numel(), _dtypes["int32"], table.shape
         # the usual tensors checked at once, which takes a third of what one by one does; where a check fails, _tensor says which or finds
         # them sound
         if (table.dtype is whole and length.dtype is whole and want.dtype is whole and start.dtype is whole and
-                length.dim() == 1 and table.dim() == 2 and table.shape[0] == n and want.numel() == n and start.numel() == n + 1 and
+                length.dim() == 1 and len(shape) == 2 and shape[0] == n == want.numel() and start.numel() == n + 1 and
                 table.is_contiguous() and length.is_contiguous() and want.is_contiguous() and start.is_contiguous() and
-                table.get_device() == g and length.get_device() == g and want.get_device() == g and start.get_device() == g):
-            tp, lp, wp, sp = table.data_ptr(), length.data_ptr(), want.data_ptr(), start.data_ptr()
+                table.get_device() == g == length.get_device() and want.get_device() == g == start.get_device()):
+            tp, lp, wp, sp, ld = table.data_ptr(), length.data_ptr(), want.data_ptr(), start.data_ptr(), shape[1]
         else:
             n = length.shape[0] if length.dim() else -1
             tp = _tensor(table, "table", "int32", (n, None), g, True)
             lp = _tensor(length, "length", "int32", (n,), g)
             wp = _tensor(want, "want", "int32", (n,), g)
             sp = _tensor(start, "start", "int32", (n + 1,), g)
+            ld = table.stride(0) if n > 1 else max(1, shape[1])
         op, qp, mp, bp, pp = lp, self._state, 0, 0, 0
         if length_out is not None:
             op = self._out(length_out, "length_out", whole, n)
@@ -538,8 +539,7 @@ class PagePool:
         if row_pos is not None:
             pp = self._out(row_pos, "row_pos", whole, rows)
         rc = _resize(_pack_pool(self._ring, self._state, qp, self.n_pages, self.page_size),
-                     _pack_wanted(tp, lp, wp, op, sp, mp, bp, pp, table.stride(0) if n > 1 else max(1, table.shape[1]), n, table.shape[1],
-                                  0x7fffffff if rows is None else rows, 0),
+                     _pack_wanted(tp, lp, wp, op, sp, mp, bp, pp, ld, n, shape[1], 0x7fffffff if rows is None else rows, 0),
                      None if status is None else _tensor(status, "status", "int32", (1,), g), _stream_handle(stream))
         if rc:
             raise UADError(rc, "resize: the arguments break a rule of include/uad.h, or the ring is not on the current device")
