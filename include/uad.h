@@ -405,7 +405,7 @@ int uad_paged_attention(const uad_kv_pages* pages, const uad_kv_seqs* seqs, cons
  * and the reading of a bf16 cache, for many or long episodes. A block is `block` slots of a page from a multiple of it on (the last one
  * of a page ends with the page: blocks never span pages), and the scale of head h of block i of page p is at
  * k_scale + p * scale_page_stride + i * scale_block_stride + h * scale_head_stride, of the values at the same place of v_scale. Any scale
- * that is finite and above 0 is read as it is (those below 2^-100 cost precision); the append writes powers of two. The code
+ * above 0 and up to 2^120 is read as it is (those below 2^-100 cost precision); the append writes powers of two, up to 2^121. The code
  * 0x7f or 0xff is NaN. */
 typedef struct uad_kv_pages8 {
   uad_kv_pages pages;    /* dtype UAD_DTYPE_E4M3; strides in elements, which are bytes */
@@ -418,7 +418,7 @@ typedef struct uad_kv_pages8 {
 /* uad_kv_append into an 8-bit cache: queries are rotated into q_out in bf16, keys and values rounded to the nearest code (ties to even)
  * of their block's scale: the least power of two s (2^-100 at the least) with 448 s >= the largest of the block's new values, for keys
  * that are rotated twice the largest before the rotation (which grows no value by more than sqrt(2)). Infinities and NaN do not count
- * and are stored as NaN. Where the block holds earlier tokens of the sequence, its scale does not fall below theirs (nor below the power of two above it), and where
+ * and are stored as NaN (a finite value that a rotation takes past fp32's largest as the largest code). Where the block holds earlier tokens of the sequence, its scale does not fall below theirs (nor below the power of two above it), and where
  * it grows they are rounded to it: exactly but for values 2^-15 of the block's largest and below, so that what a cache holds hardly depends on how many
  * calls wrote it. A block that is written therefore belongs to one sequence: it must not stand in another table of the same append, nor
  * be read meanwhile; whole blocks before it may be shared. Errors: UAD_EINVAL (arguments), UAD_ECUDA. */

@@ -13,7 +13,7 @@ namespace {
 // SMs idle once there are many of them or they are large. Long pieces are cut further, up to four waves, so that
 // sequences of different lengths even out; but less than 1.75 waves cost more than one. In us, pieces with / without a
 // cluster:
-//   1 x 817 keys, 8 heads over 1 of 256:   13: 7.1 / 9.1,  7: 8.3 / 9.6
+//   1 x 817 keys, 8 heads over 1 of 256:   13: 6.7 / 9.1,  7: 8.3 / 9.6
 //   64 x 282..1129, the same:               4: 16.3 / 18.4,  8: 23.3 / 17.1
 //   6 x 2001..8003, 5 new tokens:          12: 31.8 / 32.8,  16: 48.1 / 27.5
 //   2 x 32768, 131071, 32 over 8 of 128:   28: - / 130,  80: - / 117
@@ -40,8 +40,8 @@ struct Split {
   int pieces, piece_keys, clustered;
 };
 // `keys` in at most n pieces.
-Split cut_keys(int64_t keys, int64_t n, int64_t units, int64_t slots) {
-  const int64_t piece = ((keys + n - 1) / n + 63) / 64 * 64;
+Split cut_keys(int64_t keys, int64_t n, int64_t units, int64_t slots, int64_t round) {
+  const int64_t piece = ((keys + n - 1) / n + round - 1) / round * round;
   Split c;
   c.piece_keys = (int)(piece < (1ll << 30) ? piece : 1ll << 30);
   c.pieces = (int)((keys + c.piece_keys - 1) / c.piece_keys);
@@ -49,11 +49,11 @@ Split cut_keys(int64_t keys, int64_t n, int64_t units, int64_t slots) {
   c.clustered = c.pieces > 1 && ((c.pieces <= kMaxCluster && ctas <= kAttnSms) || (c.pieces <= 8 && ctas * 20 <= slots * 17));
   return c;
 }
-Split split_keys(int64_t keys, int64_t units, int64_t slots, int64_t least) {
+Split split_keys(int64_t keys, int64_t units, int64_t slots, int64_t least, int64_t round) {
   const auto most = [&](int64_t n) { return (keys + n - 1) / n; };   // pieces of at least n keys
   int64_t n;
-  if (keys <= kMaxCluster * 256 && units * (most(64) < kMaxCluster ? most(64) : kMaxCluster) <= kAttnSms) {
-    n = most(64) < kMaxCluster ? most(64) : kMaxCluster;
+  if (keys <= kMaxCluster * 256 && units * (most(round) < kMaxCluster ? most(round) : kMaxCluster) <= kAttnSms) {
+    return cut_keys(keys, most(round) < kMaxCluster ? most(round) : kMaxCluster, units, slots, round);
   } else {
     n = units * 5 >= slots * 3 ? 1 : units * 2 > slots ? 2 : slots / units;
     if (n > 1 && n <= 8 && units * n * 20 > slots * 17) n = slots * 17 / (units * 20) > 1 ? slots * 17 / (units * 20) : n;
@@ -62,10 +62,12 @@ Split split_keys(int64_t keys, int64_t units, int64_t slots, int64_t least) {
     if (waves > n) n = waves;
     if (n > 2 && units * n > slots && units * n * 4 < slots * 7) n = slots / units > 1 ? slots / units : n;
   }
-  return cut_keys(keys, n, units, slots);
+  return cut_keys(keys, n, units, slots, 64);
 }
-// warp_smem: shared memory of a CTA whose warps have heads of their own (0: there is no such form).
-void attn_plan(const uad_kv_seqs* s, int ctas_per_sm, size_t warp_smem, PagedAttnArgs* a) {
+// warp_smem: shared memory of a CTA whose warps have heads of their own (0: there is no such form). round: keys that the warps of a CTA take at
+// once, of which the pieces of a small call are multiples (8-bit caches, 128 / 64 in us: 1 x 817 of 8 heads over 1 of 256 7.0 / 7.5, 1 x 100 of 24
+// heads of 64 3.7 / 5.1).
+void attn_plan(const uad_kv_seqs* s, int ctas_per_sm, size_t warp_smem, int round, PagedAttnArgs* a) {
   const int64_t all = s->max_len > 0 && s->max_len < a->p.capacity ? s->max_len : a->p.capacity;
   const int64_t near = (int64_t)a->window + a->sinks + a->p.max_new - 1;
   const int64_t keys = a->window > 0 && near < all ? near : all;
@@ -79,12 +81,12 @@ void attn_plan(const uad_kv_seqs* s, int ctas_per_sm, size_t warp_smem, PagedAtt
     const int64_t without = (units + slots - 1) / slots * round + (units + kAttnSms - 1) / kAttnSms * keys * 8;
     a->warp_heads = with < without;
   }
-  Split c = split_keys(keys, units, slots, least);
+  Split c = split_keys(keys, units, slots, least, round);
   if (keys < all && c.pieces > 1 && !c.clustered) {
     // Fewer keys can be more pieces, or as many that are no cluster: no more than there are without the window, so that what
     // a call without one needs is enough for every window. (What makes a cluster of so many pieces makes one of fewer.)
-    const int most = split_keys(all, units, slots, least).pieces;
-    if (most < c.pieces) c = cut_keys(keys, most, units, slots);
+    const int most = split_keys(all, units, slots, least, round).pieces;
+    if (most < c.pieces) c = cut_keys(keys, most, units, slots, 64);
   }
   a->pieces = c.pieces;
   a->piece_keys = c.piece_keys;
@@ -140,9 +142,9 @@ int uad::attn_split(const uad_kv_seqs* seqs, const uad_attn* t, int sinks, bool 
   const int64_t units = (int64_t)a->p.n_seqs * a->p.n_kv * a->row_blocks;
   a->f32_ctas = dh == 64 && (units > 304 || units * 5 < 304 * 3) ? 3 : 2;
   const int log_tiles = a->row_tiles == 4 ? 2 : a->row_tiles - 1;
-  if (eight) attn_plan(seqs, eight->ctas[log_tiles], eight->smem[log_tiles], a);
-  else if (a->p.dtype == F32) attn_plan(seqs, a->f32_ctas, 0, a);
-  else attn_plan(seqs, a->row_tiles == 4 || dh == 256 ? 2 : dh == 64 && a->row_tiles == 1 ? 4 : 3, warp_heads_smem(dh, a->row_tiles), a);
+  if (eight) attn_plan(seqs, eight->ctas[log_tiles], eight->smem[log_tiles], eight->round[log_tiles], a);
+  else if (a->p.dtype == F32) attn_plan(seqs, a->f32_ctas, 0, 64, a);
+  else attn_plan(seqs, a->row_tiles == 4 || dh == 256 ? 2 : dh == 64 && a->row_tiles == 1 ? 4 : 3, warp_heads_smem(dh, a->row_tiles), 64, a);
   a->by_group = FastDiv((uint32_t)a->group);
   a->by_x = FastDiv((uint32_t)(a->clustered ? a->pieces : a->row_blocks));
   return UAD_OK;

@@ -41,6 +41,7 @@ constexpr int kAttnSms = 152;
 struct AttnFit8 {
   int ctas[3];
   size_t smem[3];
+  int round[3];   // keys that the warps of a CTA take at once
 };
 // paged_attn.cu: the checks of the arguments and how the work is split; attn_split: behind the checks of the pages, of an 8-bit
 // cache with what its kernels hold.
@@ -236,7 +237,7 @@ __device__ __forceinline__ void finish(const PagedAttnArgs& a, const Piece& c, c
   using S = Sums<DH, ROWS>;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   if (a.clustered) cluster_wait();   // every CTA's receiving place is free
-  const int share = a.clustered ? (S::kGroups + a.pieces - 1) / a.pieces : 0;
+  const int share = a.clustered ? (int)a.by_x.div(S::kGroups + a.pieces - 1) : 0;
 #pragma unroll 2
   for (int gr = warp; gr < S::kGroups; gr += kWarps) {
     const int r = S::row(gr, lane), d = S::dim(gr, lane);
@@ -248,7 +249,8 @@ __device__ __forceinline__ void finish(const PagedAttnArgs& a, const Piece& c, c
       x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
     }
     if (a.clustered) {   // group i goes to CTA i % pieces, [from][i / pieces]
-      put_peer(peer(su32(receive + (c.piece * share + gr / a.pieces) * 32 + lane), gr % a.pieces), x);
+      const int at_peer = (int)a.by_x.div(gr);
+      put_peer(peer(su32(receive + (c.piece * share + at_peer) * 32 + lane), gr - at_peer * a.pieces), x);
     } else if (r < c.rows) {
       const float2 ml = e->ml[r];
       put_row<T>(a, c, r, d, x, ml.x, ml.y, a.pieces == 1);
@@ -263,6 +265,7 @@ __device__ __forceinline__ void finish(const PagedAttnArgs& a, const Piece& c, c
     if (gr >= S::kGroups) break;
     const int r = S::row(gr, lane), d = S::dim(gr, lane);
     float top = -INFINITY, sum = 0.f;
+#pragma unroll 8
     for (int k = 0; k < a.pieces; ++k) top = fmaxf(top, e->ml_of[k][r].x);
     float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4

@@ -748,8 +748,11 @@ cudaError_t launch8(const PagedAttn8Args& a, cudaStream_t s) {
 
 template <int DH>
 AttnFit8 fit8() {
-  if constexpr (DH == 256) return {{ctas8<DH, 1>(), ctas8<DH, 2>(), 0}, {smem8<DH, 1>(kWarps), smem8<DH, 2>(kWarps), 0}};
-  else return {{ctas8<DH, 1>(), ctas8<DH, 2>(), ctas8<DH, 4>()}, {smem8<DH, 1>(kWarps), smem8<DH, 2>(kWarps), smem8<DH, 4>(kWarps)}};
+  if constexpr (DH == 256)
+    return {{ctas8<DH, 1>(), ctas8<DH, 2>(), 0}, {smem8<DH, 1>(kWarps), smem8<DH, 2>(kWarps), 0}, {chunk_keys<DH, 1>(), chunk_keys<DH, 2>(), 0}};
+  else
+    return {{ctas8<DH, 1>(), ctas8<DH, 2>(), ctas8<DH, 4>()}, {smem8<DH, 1>(kWarps), smem8<DH, 2>(kWarps), smem8<DH, 4>(kWarps)},
+            {chunk_keys<DH, 1>(), chunk_keys<DH, 2>(), chunk_keys<DH, 4>()}};
 }
 
 template <int DH>
