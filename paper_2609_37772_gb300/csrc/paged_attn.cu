@@ -13,7 +13,7 @@ namespace {
 // SMs idle once there are many of them or they are large. Long pieces are cut further, up to four waves, so that
 // sequences of different lengths even out; but less than 1.75 waves cost more than one. In us, pieces with / without a
 // cluster:
-//   1 x 817 keys, 8 heads over 1 of 256:   13: 6.7 / 9.1,  7: 8.3 / 9.6
+//   1 x 817 keys, 8 heads over 1 of 256:   13: 7.1 / 9.1,  7: 8.3 / 9.6
 //   64 x 282..1129, the same:               4: 16.3 / 18.4,  8: 23.3 / 17.1
 //   6 x 2001..8003, 5 new tokens:          12: 31.8 / 32.8,  16: 48.1 / 27.5
 //   2 x 32768, 131071, 32 over 8 of 128:   28: - / 130,  80: - / 117
