@@ -78,7 +78,7 @@ struct Rows4 {
   int seq[4], pos[4];
 };
 __device__ __forceinline__ void put_rows(const ResizeArgs& a, int r, int from, int to, const Rows4& x) {
-  if (a.wide && from <= r && r + 4 <= to) {
+  if (a.wide && from <= r && r <= to - 4) {   // r + 4 may pass 31 bits
     if (a.slot) {
       longlong2* at = reinterpret_cast<longlong2*>(a.slot + r);
       at[0] = make_longlong2(x.slot[0], x.slot[1]);

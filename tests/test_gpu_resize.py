@@ -210,3 +210,19 @@ def test_the_binding_refuses_tensors_that_do_not_fit():
     assert state.tolist() == [0, 9] and fine["length"].tolist() == [0, 0]
     with pytest.raises(uad.UADError):
         uad.PagePool(ring, state, 0).resize(**fine)
+
+
+@pytest.mark.parametrize("behind", [1, 2, 3])
+def test_a_map_as_long_as_31_bits_hold_ends_where_it_ends(behind):
+    """2^31 - behind rows end inside four of a store, whose end is past 31 bits."""
+    rows = 2 ** 31 - behind
+    buf = torch.full((2 ** 31 + 64,), 7, dtype=torch.int32, device="cuda")
+    whole = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    lens, start, status = whole(2), whole(-9, -9), whole(0)
+    uad.PagePool(torch.arange(4, dtype=torch.int32, device="cuda"), whole(0, 4), 16).resize(
+        whole(3, 2).view(1, 2), lens, whole(7), start, row_pos=buf[:rows], status=status)
+    torch.cuda.synchronize()
+    assert lens.tolist() == [7] and start.tolist() == [0, 5] and int(status) == 0
+    assert buf[:8].tolist() == [2, 3, 4, 5, 6, -1, -1, -1]
+    assert buf[rows - 64:rows].tolist() == [-1] * 64
+    assert buf[rows:].tolist() == [7] * (2 ** 31 + 64 - rows)
