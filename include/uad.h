@@ -450,7 +450,7 @@ typedef struct uad_page_pool {
   int32_t n_pages;         /* 1..2^30 */
   int32_t page_size;       /* 1..65536 */
 } uad_page_pool;
-/* Sequence b has len[b] tokens and shall have want[b]. The arrays are device memory. */
+/* Sequence b has len[b] tokens and shall have want[b]. The arrays are device memory, aligned to their elements. */
 typedef struct uad_kv_wanted {
   int32_t* table;          /* [n_seqs][table_stride], of which table_width entries: pages that a sequence takes are written behind those that it
                               has; those that it gives back stay where they are */

@@ -296,6 +296,10 @@ extern "C" int uad_kv_resize(const uad_page_pool* pool, const uad_kv_wanted* w, 
   if (w->n_seqs < 0 || w->n_seqs > 65535 || w->table_width < 1 || w->table_stride < w->table_width || w->n_rows < 0) return UAD_EINVAL;
   if ((int64_t)w->table_width * pool->page_size > (1ll << 31) - (1 << 17)) return UAD_EINVAL;
   if (!w->start || (w->n_seqs > 0 && (!w->table || !w->len || !w->want || !w->len_out))) return UAD_EINVAL;
+  const auto at = [](const void* p) { return reinterpret_cast<uintptr_t>(p); };
+  if ((at(pool->ring) | at(pool->state) | at(pool->state_out) | at(w->table) | at(w->len) | at(w->want) | at(w->len_out) | at(w->start) | at(w->row_seq) |
+       at(w->row_pos) | at(status)) % 4 || at(w->slot) % 8)
+    return UAD_EINVAL;
   if (!on_current_device(pool->ring)) return UAD_EINVAL;
   ResizeArgs a{};
   a.table = w->table; a.len = w->len; a.want = w->want; a.len_out = w->len_out; a.start = w->start;

@@ -226,3 +226,20 @@ def test_a_map_as_long_as_31_bits_hold_ends_where_it_ends(behind):
     assert buf[:8].tolist() == [2, 3, 4, 5, 6, -1, -1, -1]
     assert buf[rows - 64:rows].tolist() == [-1] * 64
     assert buf[rows:].tolist() == [7] * (2 ** 31 + 64 - rows)
+
+
+def test_arrays_off_their_elements_are_refused():
+    buf = {n: torch.zeros(64, dtype=torch.int64, device="cuda") for n in ("ring", "state", "state_out", "table", "len", "want", "len_out", "start", "slot",
+                                                                          "row_seq", "row_pos", "status")}
+    at = {n: t.data_ptr() for n, t in buf.items()}
+
+    def call(x):
+        return uad.uad_kv_resize(uad.uad_page_pool(ring=x["ring"], state=x["state"], state_out=x["state_out"], n_pages=4, page_size=16),
+                                 uad.uad_kv_wanted(**{n: x[n] for n in ("table", "len", "want", "len_out", "start", "slot", "row_seq", "row_pos")}, table_stride=4,
+                                                   n_seqs=1, table_width=4, n_rows=4), x["status"], None)
+
+    for n in at:
+        assert call(at | {n: at[n] + (4 if n == "slot" else 2)}) == uad.UAD_EINVAL, n
+    assert call(at) == uad.UAD_OK
+    torch.cuda.synchronize()
+    assert buf["start"].view(torch.int32)[:2].tolist() == [0, 0] and int(buf["status"][0]) == 0
