@@ -422,6 +422,8 @@ class PagedCache:
 
     def attention_workspace(self, seqs, rows, n_heads, window=0, sinks=0):
         """Bytes of the workspace that attention of these sizes needs (0 is possible). Without a window: enough for every window and sinks."""
+        if not 0 <= sinks <= 0x7fffffff:   # which the call would cut to 32 bits
+            raise ValueError(f"sinks: expected 0 to 2^31 - 1, got {sinks}")
         attn = uad_attn(n_heads=n_heads, n_rows=rows, window=window)
         n = uad_paged_attention_sinks_workspace(self.pages, seqs.seqs, attn, sinks) if self.block is None else \
             uad_paged_attention8_workspace(self.pages8, seqs.seqs, attn, sinks)
@@ -468,6 +470,8 @@ class PagedCache:
                 wp = workspace.data_ptr()
             else:
                 wp = _tensor(workspace, "workspace", "uint8", (None,), g)
+        if not 0 <= sinks <= 0x7fffffff:
+            raise ValueError(f"sinks: expected 0 to 2^31 - 1, got {sinks}")
         # uad_attn takes 0 for the default: a scale of 0, or one that fp32 does not hold, is the least that it does
         factor = 0.0 if scale is None else _LEAST if abs(scale) < _LEAST else scale
         attn = _pack_attn(qp, op, lp, mp, ql, ol, ml, factor, heads, n, 1 if causal else 0, window, 0)

@@ -119,3 +119,17 @@ def test_no_sinks_is_the_call_without():
         cache.attention(s, q, b, ws, window=window, sinks=sinks)
         torch.cuda.synchronize()
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("sinks", [-1, 1 << 31, (1 << 32) + 4])
+def test_sinks_past_32_bits_are_refused(sinks):
+    k = torch.zeros(2, 16, 1, 64, device="cuda")
+    whole = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    q, out = torch.zeros(1, 64, device="cuda"), torch.full((1, 64), 7.5, device="cuda")
+    seqs, cache = uad.Sequences(whole(0, 1).view(1, 2), whole(20), max_new=1), uad.PagedCache(k, k)
+    with pytest.raises(ValueError, match="sinks"):
+        cache.attention_workspace(seqs, 1, 1, 4, sinks)
+    with pytest.raises(ValueError, match="sinks"):
+        cache.attention(seqs, q, out, window=4, sinks=sinks)
+    torch.cuda.synchronize()
+    assert bool((out == 7.5).all())
