@@ -76,9 +76,9 @@ void attn_plan(const uad_kv_seqs* s, int ctas_per_sm, size_t warp_smem, int roun
   a->warp_heads = 0;
   if (warp_smem > 0 && a->p.n_kv % kWarps == 0 && keys <= 512) {
     const int64_t fit = 228 * 1024 / ((int64_t)warp_smem + 1024);   // an SM's, and what it keeps of each CTA's
-    const int64_t ctas = units / kWarps, held = kAttnSms * (fit < ctas_per_sm ? fit : ctas_per_sm), round = 8 * (40000 / a->p.dh);
-    const int64_t with = (ctas + held - 1) / held * round + (ctas + kAttnSms - 1) / kAttnSms * kWarps * keys * (a->row_tiles == 4 ? 12 : 9);
-    const int64_t without = (units + slots - 1) / slots * round + (units + kAttnSms - 1) / kAttnSms * keys * 8;
+    const int64_t ctas = units / kWarps, held = kAttnSms * (fit < ctas_per_sm ? fit : ctas_per_sm), lap = 8 * (40000 / a->p.dh);
+    const int64_t with = (ctas + held - 1) / held * lap + (ctas + kAttnSms - 1) / kAttnSms * kWarps * keys * (a->row_tiles == 4 ? 12 : 9);
+    const int64_t without = (units + slots - 1) / slots * lap + (units + kAttnSms - 1) / kAttnSms * keys * 8;
     a->warp_heads = with < without;
   }
   Split c = split_keys(keys, units, slots, least, round);
