@@ -13,8 +13,9 @@
 // - queries: f16 after a power of two that takes each row's largest value to 2^13..2^14: bf16 has fewer bits, and what falls below
 //   f16's least is 2^-38 of the largest;
 // - scales come through the ring beside the codes. A key's multiplies its scores; a value's multiplies the weights, which are f16
-//   of 2^11 p sv / r: r is a power of two, the largest sv so far, as m is the largest score so far. Rounding weights to f16 is an
-//   error of 2^-12 at most, an eighth of what the output's own rounding to bf16 is, and 2^-36 of the largest weight for small ones.
+//   of 2^11 p sv / r: r is a power of two of the row, the largest p sv so far, as m is its largest score so far (p is 2^(score - m)): keys that the row does
+//   not see, or gives no weight, have no part in it, whatever their scale. Rounding weights to f16 is an
+//   error of 2^-11 at most, an eighth of what the output's own rounding to bf16 is, and 2^-35 of the row's largest for small ones.
 //
 // One new token: 64 x 4000 keys of 32 heads over 8 of 128 take 95 us (524 MB, 5.5 TB/s; 170 from a bf16 cache), 2 sequences of up to 131071 of
 // the same 61 us (5.5 TB/s), 64 x 4000 of 8 over 1 of 256 28 us (4.6 TB/s). What bounds: the latencies of a warp's slice (about 800
@@ -39,9 +40,9 @@ struct PagedAttn8Args {
   int2* spans;    // [CTA] the sequence that begins in its part and ends in a later one, and that one; -1: there is none
 };
 
-constexpr float kLag = 4.f;            // how far (base 2) scores may pass their running maximum before it follows: 2^15 holds their weights
-constexpr int kWeightBits = 11;        // weights are 2^kWeightBits at the running maximum
-constexpr float kLeastScale = 7.888609052210118e-31f;   // 2^-100
+constexpr float kLag = 4.f;            // how far (base 2) scores and weights may pass their running maximum before it follows: f16 holds 2^15
+constexpr int kWeightBits = 11;        // weights are up to 2^kWeightBits where the running maximum follows
+constexpr float kLeastUnit = 7.888609052210118e-31f;   // 2^-100, of a row's weights
 
 __device__ __forceinline__ void mma16816h(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -407,7 +408,9 @@ __global__ void __launch_bounds__(kThreads, ctas8<DH, NR>()) paged_attn8_kernel(
       q[x][1] = q[x][3] = q[x + 1][1] = q[x + 1][3] = 0;
     }
   }
-  float ref = kLeastScale;   // a power of two, no value's scale so far is above it
+  float unit[2 * MT];   // of the rows' weights p sv: powers of two that no weight has passed by more than 2^kLag
+#pragma unroll
+  for (int i = 0; i < 2 * MT; ++i) unit[i] = kLeastUnit;
   const uint32_t ka = ring + (lane & 7) * DH + ((lane >> 3) ^ key_swap<DH>(lane & 7)) * 16;             // 8 keys, 64 dims
   const int vk = (lane >> 2 & 3) * 2 + (lane & 1) + (lane >> 1 & 1) * 8;
   const uint32_t va = ring + vk * DH + ((lane >> 4) ^ key_swap<DH>(vk)) * 16;                           // 16 keys, 32 dims
@@ -505,15 +508,35 @@ __global__ void __launch_bounds__(kThreads, ctas8<DH, NR>()) paged_attn8_kernel(
 
     cp_wait<SLOTS - 1>();
     __syncwarp();
-    // the values' scales: a power of two that none is above goes before the sums
-    const float own_scale = lds_f(ring + use * SLOT + SCALES + 4 * (lane & (KEYS - 1)));
-    if (__any_sync(0xffffffffu, grew || own_scale > ref)) {
-      const uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(fmaxf(own_scale, ref)));
-      const float now = __uint_as_float(min((most + 0x7fffffu) & 0xff800000u, 254u << 23)), raised = ref / now;
-      ref = now;
+    // weights p sv, of which a power of two, the row's unit, goes before the sums
+#pragma unroll
+    for (int k = 0; k < 2 * KT; ++k) {
+      const float2 w = lds_f2(ring + use * SLOT + SCALES + 32 * k + 8 * t);
 #pragma unroll
       for (int n = 0; n < NR; ++n) {
-        const float f0 = __shfl_sync(0xffffffffu, f[n], 8 * t) * raised, f1 = __shfl_sync(0xffffffffu, f[n], 8 * t + 4) * raised;
+        float* v = s[n >> 1][k] + 2 * (n & 1);   // 0 times what a row does not see is 0
+        v[0] = v[0] == 0.f ? 0.f : v[0] * w.x;
+        v[1] = v[1] == 0.f ? 0.f : v[1] * w.y;
+      }
+    }
+    float most[NR];
+#pragma unroll
+    for (int n = 0; n < NR; ++n) {
+      most[n] = 0.f;
+#pragma unroll
+      for (int k = 0; k < 2 * KT; ++k) most[n] = fmaxf(most[n], fmaxf(s[n >> 1][k][2 * (n & 1)], s[n >> 1][k][2 * (n & 1) + 1]));
+      grew |= most[n] > unit[n] * (1 << (int)kLag);
+    }
+    if (__any_sync(0xffffffffu, grew)) {
+#pragma unroll
+      for (int n = 0; n < NR; ++n) {
+        float top = most[n];
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        const float held = unit[n] * f[n], all = fmaxf(fmaxf(top, held), kLeastUnit);   // in the new maximum's terms
+        const float now = __uint_as_float(min((__float_as_uint(all) + 0x7fffffu) & 0xff800000u, 254u << 23)), kept = held / now;
+        unit[n] = now;
+        const float f0 = __shfl_sync(0xffffffffu, kept, 8 * t), f1 = __shfl_sync(0xffffffffu, kept, 8 * t + 4);
 #pragma unroll
         for (int y = 0; y < STEPS; ++y) {
           o[y][n][0] *= f0;
@@ -523,15 +546,12 @@ __global__ void __launch_bounds__(kThreads, ctas8<DH, NR>()) paged_attn8_kernel(
         }
       }
     }
-    const float per_ref = __uint_as_float(((254u + kWeightBits) << 23) - __float_as_uint(ref));   // 2^kWeightBits / ref
     uint32_t p[NR][2 * KT];
 #pragma unroll
-    for (int k = 0; k < 2 * KT; ++k) {
-      float2 w = lds_f2(ring + use * SLOT + SCALES + 32 * k + 8 * t);
-      w.x *= per_ref;
-      w.y *= per_ref;
+    for (int n = 0; n < NR; ++n) {
+      const float per_unit = __uint_as_float(((254u + kWeightBits) << 23) - __float_as_uint(unit[n]));   // 2^kWeightBits / unit
 #pragma unroll
-      for (int n = 0; n < NR; ++n) p[n][k] = pack_f16(s[n >> 1][k][2 * (n & 1)] * w.x, s[n >> 1][k][2 * (n & 1) + 1] * w.y);
+      for (int k = 0; k < 2 * KT; ++k) p[n][k] = pack_f16(s[n >> 1][k][2 * (n & 1)] * per_unit, s[n >> 1][k][2 * (n & 1) + 1] * per_unit);
     }
     // Where rows see different keys, a value that one of them does not see must not reach it, not even as 0 times NaN:
     // NaN codes of such a slice are left out here and added row by row below.
@@ -607,12 +627,12 @@ __global__ void __launch_bounds__(kThreads, ctas8<DH, NR>()) paged_attn8_kernel(
   const bool alone = !EVEN && a.warp_heads;
   if (!alone) common_rows(end);
   float* so = reinterpret_cast<float*>(smem) + warp * (S::kBytes / 4);
-  const float unit = ref * (1.f / (1 << kWeightBits));
 #pragma unroll
   for (int n = 0; n < NR; ++n) {
     const int r = 8 * n + 2 * t;
-    const float f0 = alone ? unit : unit * weight(end->m[warp][r], common_max(end, r));
-    const float f1 = alone ? unit : unit * weight(end->m[warp][r + 1], common_max(end, r + 1));
+    const float u = unit[n] * (1.f / (1 << kWeightBits)), u0 = __shfl_sync(0xffffffffu, u, 8 * t), u1 = __shfl_sync(0xffffffffu, u, 8 * t + 4);
+    const float f0 = alone ? u0 : u0 * weight(end->m[warp][r], common_max(end, r));
+    const float f1 = alone ? u1 : u1 * weight(end->m[warp][r + 1], common_max(end, r + 1));
     float* dst = so + r * S::kPitch + g;
 #pragma unroll
     for (int x = 0; x < STEPS; ++x) {
