@@ -12,10 +12,12 @@
 //   access (key_swap), the first eight or every second pair;
 // - queries: f16 after a power of two that takes each row's largest value to 2^13..2^14: bf16 has fewer bits, and what falls below
 //   f16's least is 2^-38 of the largest;
-// - scales come through the ring beside the codes. A key's multiplies its scores; a value's multiplies the weights, which are f16
-//   of 2^11 p sv / r: r is a power of two of the row, the largest p sv so far, as m is its largest score so far (p is 2^(score - m)): keys that the row does
-//   not see, or gives no weight, have no part in it, whatever their scale. Rounding weights to f16 is an
-//   error of 2^-11 at most, an eighth of what the output's own rounding to bf16 is, and 2^-35 of the row's largest for small ones.
+// - scales come through the ring beside the codes. A key's multiplies its scores; a value's multiplies the weights, 2^11 p sv / r:
+//   r is a power of two of the row, the largest p sv so far, as m is its largest score so far (p is 2^(score - m)): keys that the row does
+//   not see, or gives no weight, have no part in it, whatever their scale. A weight goes in as two f16, its upper 11 bits and the rest: a second MMA
+//   for an error of 2^-21, and 2^-34 of the row's largest weight for small ones, where one f16 has 2^-11, an eighth of what the
+//   output's own rounding to bf16 is (one / two, in us: 64 x 4000 keys of 32 heads over 8 of 128 93 / 95, of 8 over 1 of 256 28 / 29, with 4 new tokens
+//   60 / 67; 16 x 4000 with 8 new tokens of 32 over 8 of 128 60 / 74, where the MMAs of four tiles of rows count).
 //
 // One new token: 64 x 4000 keys of 32 heads over 8 of 128 take 95 us (524 MB, 5.5 TB/s; 170 from a bf16 cache), 2 sequences of up to 131071 of
 // the same 61 us (5.5 TB/s), 64 x 4000 of 8 over 1 of 256 28 us (4.6 TB/s). What bounds: the latencies of a warp's slice (about 800
@@ -546,12 +548,18 @@ __global__ void __launch_bounds__(kThreads, ctas8<DH, NR>()) paged_attn8_kernel(
         }
       }
     }
-    uint32_t p[NR][2 * KT];
+    // as two f16: the upper 11 bits and the rest
+    uint32_t hi[NR][2 * KT], lo[NR][2 * KT];
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
       const float per_unit = __uint_as_float(((254u + kWeightBits) << 23) - __float_as_uint(unit[n]));   // 2^kWeightBits / unit
 #pragma unroll
-      for (int k = 0; k < 2 * KT; ++k) p[n][k] = pack_f16(s[n >> 1][k][2 * (n & 1)] * per_unit, s[n >> 1][k][2 * (n & 1) + 1] * per_unit);
+      for (int k = 0; k < 2 * KT; ++k) {
+        const float p0 = s[n >> 1][k][2 * (n & 1)] * per_unit, p1 = s[n >> 1][k][2 * (n & 1) + 1] * per_unit;
+        const float h0 = __uint_as_float(__float_as_uint(p0) & 0xffffe000u), h1 = __uint_as_float(__float_as_uint(p1) & 0xffffe000u);
+        hi[n][k] = pack_f16(h0, h1);
+        lo[n][k] = pack_f16(p0 - h0, p1 - h1);
+      }
     }
     // Where rows see different keys, a value that one of them does not see must not reach it, not even as 0 times NaN:
     // NaN codes of such a slice are left out here and added row by row below.
@@ -575,14 +583,18 @@ __global__ void __launch_bounds__(kThreads, ctas8<DH, NR>()) paged_attn8_kernel(
 #pragma unroll
           for (int j = 0; j < 4; ++j) v[j] &= ~nan_bytes(v[j]);
         }
+        uint32_t fr[2][4];
 #pragma unroll
         for (int y = 0; y < 2; ++y) {
-          uint32_t fr[4];
-          e4m3_f16x4(v[2 * y], &fr[0], &fr[2]);
-          e4m3_f16x4(v[2 * y + 1], &fr[1], &fr[3]);
+          e4m3_f16x4(v[2 * y], &fr[y][0], &fr[y][2]);
+          e4m3_f16x4(v[2 * y + 1], &fr[y][1], &fr[y][3]);
 #pragma unroll
-          for (int n = 0; n < NR; ++n) mma16816h(o[x + y][n], fr, p[n][2 * u], p[n][2 * u + 1]);
+          for (int n = 0; n < NR; ++n) mma16816h(o[x + y][n], fr[y], hi[n][2 * u], hi[n][2 * u + 1]);
         }
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+#pragma unroll
+          for (int n = 0; n < NR; ++n) mma16816h(o[x + y][n], fr[y], lo[n][2 * u], lo[n][2 * u + 1]);
       }
     if (odd) {
 #pragma unroll 1

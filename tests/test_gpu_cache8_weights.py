@@ -138,3 +138,38 @@ def test_scales_that_a_row_does_not_see_may_hold_anything(heads, value):
         outs.append((out, lse))
     rows = [0, 1, 2, 3, 9, 10]   # positions 11 to 14, 698 and 699
     assert torch.equal(outs[0][0][rows], outs[1][0][rows]) and torch.equal(outs[0][1][rows], outs[1][1][rows])
+
+
+TWO_F16 = 2.0 ** -20
+
+
+def test_weights_have_more_than_one_f16():
+    """Two tokens of nearly opposite contributions: what is left of them is 2^-9 and less of each, which one f16 a weight misses by up to an eighth."""
+    n = 300
+    c = Case8((1, 1, 64), 1, [2] * n, [1] * n, 16, seed=13)
+    x = paged8.encode((c.rng.normal(size=(n, 64)) * 100).clip(-448, 448))
+    q = torch.zeros((c.rows, 64), device="cuda", dtype=torch.bfloat16)
+    q[:, 0] = 1.0
+    for b in range(n):
+        one, two = c.table[b]
+        for pg, score in ((one, 0.0), (two, c.rng.uniform(-2, 0))):   # one dim alone: scores whose own error is small
+            c.codes[0][pg] = 0
+            c.codes[0][pg, 0, 0, 0] = paged8.encode(np.float64(1.0 if score else 0.0))
+            c.scales[0][pg] = np.float32(abs(score) or 1.0)
+        c.codes[1][one, 0, 0], c.codes[1][two, 0, 0] = x[b], x[b] ^ 0x80
+        c.scales[1][one] = np.float32(c.rng.uniform(0.5, 1))
+        # the second token's weight e^score: as large as the first one's contribution, but for 2^-9
+        c.scales[1][two] = np.float32(c.scales[1][one] * math.exp(-float(c.scales[0][two, 0, 0])) * (1 + 2.0 ** -9))
+    q, out, lse, status = run_attention(c, q=q, scale=1.0)
+    assert status == 0
+    check_near(c, q, out, lse, scale=1.0, weights=TWO_F16)
+
+
+@pytest.mark.parametrize("heads", HEADS, ids=lambda h: "x".join(map(str, h)))
+def test_weights_of_drafts_have_more_than_one_f16(heads):
+    c = Case8(heads, 16, [33, 300, 9], [5, 3, 9], 16, seed=14)
+    c.scales[1] *= 2.0 ** c.rng.integers(-9, 9, c.scales[1].shape)
+    for causal in (True, False):
+        q, out, lse, status = run_attention(c, causal)
+        assert status == 0
+        check_near(c, q, out, lse, causal, weights=TWO_F16)
