@@ -434,7 +434,7 @@ int uad_paged_attention_sinks(const uad_kv_pages* pages, const uad_kv_seqs* seqs
                               size_t workspace_bytes, int32_t* status, void* stream);
 
 /* The same over an 8-bit cache; q and out are bf16. Products of codes and queries (as f16 with a power of two a row: exact down to 2^-30 of the row's largest query) are exact, sums and softmax
- * in fp32, a key's probability times its values' scale as the sum of two f16 (2^-21; those below 2^-14 of the row's largest 2^-34 of that). The largest offset of a code, in units of the largest power of two that divides the three strides, and of a
+ * in fp32, a key's probability times its values' scale as the sum of two f16 (2^-21; those below 2^-14 of the row's largest 2^-34 of that). The largest offset of a code, in units of the largest power of two up to 2^31 that divides the three strides, and of a
  * scale, in elements, stay below 2^32 - 1 (64 GiB of codes at least; 256 GiB with heads next to each other): UAD_EINVAL. */
 int64_t uad_paged_attention8_workspace(const uad_kv_pages8* pages, const uad_kv_seqs* seqs, const uad_attn* attn, int32_t sinks);
 int uad_paged_attention8(const uad_kv_pages8* pages, const uad_kv_seqs* seqs, const uad_attn* attn, int32_t sinks, void* workspace,

@@ -35,7 +35,7 @@ namespace {
 struct PagedAttn8Args {
   PagedAttnArgs a;
   Scales sc;
-  // Places in 32 bits: of codes in units of the largest power of two that divides all strides (at least 16), of scales in elements.
+  // Places in 32 bits: of codes in units of the largest power of two that divides all strides (at least 16, at most 2^31), of scales in elements.
   // 64-bit sums and shuffles take 1 to 4% longer with heads of 64 and 128.
   uint32_t unit, page_units, slot_units, head_units, scale_page, scale_block, scale_head;
   int parts;      // into how many the sequences' chunks are cut evenly; 0: as attn_plan has it
@@ -824,8 +824,8 @@ int attn8_args(const uad_kv_pages8* pages, const uad_kv_seqs* seqs, const uad_at
   int rc = pages8_args(pages, seqs, t->n_rows, device, &a->a.p, &a->sc);
   if (rc) return rc;
   const uad_kv_pages& g = pages->pages;
-  // offsets in 32 bits: of codes in units of the strides, of scales in elements
-  const int64_t any = g.page_stride | g.slot_stride | g.head_stride, unit = any & -any, top = 0xffffffffll;
+  // offsets in 32 bits: of codes in units of the strides (which are 32 bits themselves), of scales in elements
+  const int64_t any = g.page_stride | g.slot_stride | g.head_stride, unit = std::min<int64_t>(any & -any, 1ll << 31), top = 0xffffffffll;
   const int blocks = (g.page_size + pages->block - 1) / pages->block;
   if (g.page_stride / unit > top || g.slot_stride / unit > top || g.head_stride / unit > top || pages->scale_page_stride > top ||
       pages->scale_block_stride > top || pages->scale_head_stride > top)

@@ -156,6 +156,20 @@ def test_offsets_of_32_bits():
     assert need(dict(n_pages=1 << 21), scale_page_stride=1 << 12) == uad.UAD_EINVAL
 
 
+def test_units_of_offsets_are_32_bits_themselves():
+    """Strides that share a power of two past 2^31: places are counted in units of 2^31, and what those do not hold is refused."""
+    def need(n_pages, stride):
+        return uad.uad_paged_attention8_workspace(pages8(dict(n_pages=n_pages, page_size=1, n_kv_heads=1, page_stride=stride, slot_stride=stride, head_stride=stride)),
+                                                  seqs(), attn(n_heads=4), 0)
+
+    assert need((1 << 31) - 1, 1 << 31) == 0
+    for shift in (33, 34, 40, 47):
+        assert need(1 << 63 - shift, 1 << shift) == 0   # the last page's place is 2^32 - 2^(shift - 31)
+        assert need((1 << 63 - shift) + 1, 1 << shift) == uad.UAD_EINVAL
+    assert need(2, 1 << 62) == 0
+    assert need(3, 1 << 62) == uad.UAD_EINVAL
+
+
 def test_a_workspace_without_a_window_holds_for_every_window_and_sinks():
     rng = np.random.default_rng(0)
     heads = [(8, 1, 256), (4, 1, 128), (8, 2, 64), (24, 24, 64), (32, 8, 128), (4, 2, 64)]
