@@ -453,7 +453,8 @@ typedef struct uad_page_pool {
 /* Sequence b has len[b] tokens and shall have want[b]. The arrays are device memory, aligned to their elements. */
 typedef struct uad_kv_wanted {
   int32_t* table;          /* [n_seqs][table_stride], of which table_width entries: pages that a sequence takes are written behind those that it
-                              has; those that it gives back stay where they are */
+                              has; those that it gives back stay where they are. -1 among them is no page: a program may give the pages
+                              between the sinks and a window back itself, before the sequence ends */
   const int32_t* len;
   const int32_t* want;     /* [n_seqs], 0..table_width * page_size */
   int32_t* len_out;        /* [n_seqs] after the call: want, or len where nothing was done; may be len or want */
@@ -470,9 +471,11 @@ typedef struct uad_kv_wanted {
 /* More findings for the status word: */
 #define UAD_KV_NO_ROOM 4  /* no page or no row for a sequence that shall grow: it stays as it was */
 #define UAD_KV_BAD_POOL 8 /* state outside of the ring, or more pages given back than it has places: they are dropped */
+/* and UAD_KV_BAD_PAGE: an entry given back is neither a page nor -1 (it is left out), or one that is taken from the ring is no page. */
 
 /* Give each sequence the pages of want[b] tokens, from the front of the ring in the order of the sequences, or its last pages back to
- * the end of the ring (want below len: a rejected draft, an episode's end); pages that others share must not be given back. With it the lengths,
+ * the end of the ring (want below len: a rejected draft, an episode's end; entries that are no pages do not come onto it); pages that others share
+ * must not be given back. What lies at the ring's free places is not defined. With it the lengths,
  * first rows and slot maps of the step, so that a captured graph needs nothing from the host. Sequences are served in order: one whose pages,
  * summed with those asked for before it, are more than were free before the call, or whose rows likewise do not fit n_rows, stays as it was
  * (UAD_KV_NO_ROOM). A sequence with a length or want outside its table stays as it was too (UAD_KV_BAD_SEQ). Whole numbers, the same in

@@ -77,7 +77,7 @@ def append(codes, scales, table, lens, start, page, block, rows, theta=None, dim
 
 def resize(ring, state, table, lens, want, page, rows):
     """The pages' bookkeeping, sequence after sequence: (ring, state, table, lens, start, [(slot, sequence, position)], found), all new.
-    found: "no room", "bad sequence"."""
+    found: "no room", "bad sequence", "bad page" (-1, no page, apart), "bad pool"."""
     ring, table, out = ring.copy(), table.copy(), np.array(lens).copy()
     n, width = len(ring), table.shape[1]
     first, count = (int(x) for x in state)
@@ -96,13 +96,21 @@ def resize(ring, state, table, lens, want, page, rows):
                 found.add("no room")
             else:
                 table[b, held:needed] = free[taken:taken + needed - held]
+                if any(not 0 <= x < n for x in free[taken:taken + needed - held]):
+                    found.add("bad page")
                 taken += needed - held
                 out[b] = shall
                 made += [(int(table[b, p // page]) * page + p % page, b, p) for p in range(have, shall)]
         else:
-            back += [int(x) for x in table[b, -(-shall // page):-(-have // page)]]
+            given = [int(x) for x in table[b, -(-shall // page):-(-have // page)]]
+            back += [x for x in given if 0 <= x < n]
+            if any(x >= n or x < -1 for x in given):
+                found.add("bad page")
             out[b] = shall
         start.append(len(made))
+    if len(back) > n - count:
+        found.add("bad pool")
+        back = back[:n - count]
     for i, p in enumerate(back):
         ring[(first + count + i) % n] = p
     return ring, ((first + taken) % n, count - taken + len(back)), table, out, start, made, found

@@ -510,7 +510,7 @@ class PagePool:
         the pool's new state go (None: in place). slot int64, row_seq and row_pos int32 [rows]: each new token's place in the cache
         (page * page_size + slot), sequence and position, -1 behind the last one. rows: what the token tensors hold (None: the
         slot maps' length; without one, no limit). Sequences that find no page or row stay as they were (UAD_KV_NO_ROOM in `status`);
-        want below length gives pages back."""
+        want below length gives pages back, but for entries of the table that are -1 (given back before by the program itself)."""
         g, n, whole, shape = self._gpu, length.numel(), _dtypes["int32"], table.shape
         # the usual tensors checked at once, which takes a third of what one by one does; where a check fails, _tensor says which or finds
         # them sound

@@ -27,6 +27,7 @@ struct ResizeArgs {
   FastDiv page;
   int n_seqs, capacity, n_rows, n_pages;
   int fill, update;   // what this launch writes: tables, ring and rows; lengths and the ring's state
+  int settle;         // 1: the only block, which answers for what is given back; 0: a launch behind this one does
   int maps, wide;     // whether slot maps are wanted; whether they are 16-byte aligned
 };
 
@@ -101,8 +102,12 @@ __device__ __forceinline__ void put_rows(const ResizeArgs& a, int r, int from, i
 // them out for itself, which spares an exchange. The items (pages taken, pages given back, rows in fours) are then spread evenly
 // over all blocks' threads, each finding its owner by bisection, so that one long sequence costs no more than many short ones. T: what
 // the sums of a chunk fit in.
-// A decoding step of 64 sequences takes 5.4 us, a launch and a chain of three loads; 4000 sequences of which 2800 get 1 to 816 tokens 16 us
-// (26 MB of slot maps, 1.6 TB/s): sums of two chunks, then the rows, at 0.6 instructions a cycle and scheduler.
+// Places of a table that hold no page (an episode behind a window) do not come onto the ring when they are given back. The lengths do not tell of them, and
+// there are none most of the time: pages given back are put onto the ring as if there were none, and where one is found (or they
+// were more than fit) one block puts them there again, without gaps. Several blocks leave that to a second launch of one, which reads what they have put
+// (1.5 us, and 3 more for 88000 pages given back; a cluster of eight takes 2.8 and 5 in all).
+// A decoding step of 64 sequences takes 5.7 us, a launch and two rounds of dependent loads; 4000 sequences of which 2800 get 1 to 816 tokens 19 us
+// (26 MB of slot maps, 1.3 TB/s): sums of two chunks, then the rows, at 0.6 instructions a cycle and scheduler, 16 us; then the second launch.
 template <typename T>
 __global__ void __launch_bounds__(kThreads) resize_kernel(const ResizeArgs a) {
   __shared__ int take_at[kChunk], give_at[kChunk], row_at[kChunk], had[kChunk], kept[kChunk];   // kept: pages that it shall have
@@ -127,7 +132,7 @@ __global__ void __launch_bounds__(kThreads) resize_kernel(const ResizeArgs a) {
   const bool sound = first >= 0 && first < n && full >= 0 && full <= n;
   const int count = sound ? full : 0, room = sound ? n - full : 0;   // pages, and free places of the ring
   int64_t asked_pages = 0, asked_rows = 0, given = 0;   // of the chunks before
-  int rows = 0, taken = 0;
+  int rows = 0, taken = 0, placed = 0;                  // placed: of those given back, the pages on the ring (settle)
   int report = sound ? 0 : UAD_KV_BAD_POOL;
   const int chunk = (int)blockDim.x * kOwn;
   // Chunks are worked out by every block in turn, and filled in by a share of the blocks each, at about the same time.
@@ -138,8 +143,38 @@ __global__ void __launch_bounds__(kThreads) resize_kernel(const ResizeArgs a) {
     const uint32_t x = (uint32_t)first + i;
     return x >= (uint32_t)n ? x - n : x;
   };
+  // Whether one of the n_put entries `from` places behind the first is no page, of those that this thread reads.
+  const auto no_page = [&](int from, int n_put) {
+    unsigned most = 0;
+    for (int at = (int)on_ring((uint32_t)from); n_put > 0; at = 0) {   // to the ring's end, then from its beginning
+      const int run = min(n_put, n - at), *p = a.ring + at, skip = min(run, (int)(-(reinterpret_cast<uintptr_t>(p) / 4) & 3)), fours = (run - skip) / 4;
+      const int ends = run - 4 * fours;   // before and behind them, 6 at the most
+      if ((int)threadIdx.x < ends) most = max(most, (unsigned)p[(int)threadIdx.x < skip ? threadIdx.x : 4 * fours + threadIdx.x]);
+      const int4* p4 = reinterpret_cast<const int4*>(p + skip);
+      for (int i0 = threadIdx.x; i0 < fours; i0 += 8 * (int)blockDim.x) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int i = i0 + j * (int)blockDim.x;
+          if (i < fours) {
+            const int4 x = p4[i];
+            most = max(max(most, max((unsigned)x.x, (unsigned)x.y)), max((unsigned)x.z, (unsigned)x.w));
+          }
+        }
+      }
+      n_put -= run;
+    }
+    return most >= (unsigned)n;
+  };
   const auto pages_of = [&](int tokens) { return tokens > 0 ? (int)a.page.div(tokens - 1) + 1 : 0; };
   if (a.n_seqs == 0) __syncthreads();   // the state has been read
+  if (a.settle && !a.fill && !a.update) {   // the launch before has written its state: is it right?
+    const int head = a.state_out[0], left = a.state_out[1];
+    if (!sound) return;
+    if (head >= 0) {   // everything had a place
+      const int gone = head >= first ? head - first : head - first + n, put = room > 0 ? left - count + gone : 0;
+      if (!__syncthreads_or(no_page(count, put))) return;
+    }
+  }
   uint32_t turn = 0;
   for (int base = 0; base < a.n_seqs; base += chunk) {
     T v[3] = {0, 0, 0}, total[3];   // pages to take, pages to give back, rows
@@ -165,7 +200,6 @@ __global__ void __launch_bounds__(kThreads) resize_kernel(const ResizeArgs a) {
     // Places are counted from the chunk's beginning.
     const bool everybody = asked_pages + total[0] <= count && asked_rows + total[2] <= a.n_rows && asked_rows == rows;
     const T pages_left = (T)max(min(count - asked_pages, most_of_t), (int64_t)-1), rows_left = (T)max(min(a.n_rows - asked_rows, most_of_t), (int64_t)-1);
-    const T room_left = (T)max(room - given, (int64_t)-1);
     T served[1] = {0}, all_served = total[2];
     bool ok[kOwn];
     int most = 0;
@@ -187,7 +221,6 @@ __global__ void __launch_bounds__(kThreads) resize_kernel(const ResizeArgs a) {
         else served[0] += add;
         if (ok[i] && need[i] > held[i]) most = (int)v[0];
       }
-      if (held[i] > need[i] && v[1] > room_left) report |= UAD_KV_BAD_POOL;
     }
     if (!everybody) {   // rows and pages once more, of those who are served
       most = (int)__reduce_max_sync(0xffffffffu, (unsigned)most);
@@ -217,16 +250,26 @@ __global__ void __launch_bounds__(kThreads) resize_kernel(const ResizeArgs a) {
     __syncthreads();   // places and taken_here
     load(base + chunk);   // the next chunk, on its way meanwhile
     const int m = min(chunk, a.n_seqs - base), n_rows = (int)all_served, n_taken = everybody ? (int)total[0] : taken_here;
-    const int n_given = (int)max(min((int64_t)total[1], (int64_t)room_left), (int64_t)0);
+    // pages given back that are put behind those before as if all of them were pages
+    const int put_at = a.settle ? placed : (int)min(given, (int64_t)room);
+    const int n_given = (int)min((int64_t)total[1], (int64_t)(room - put_at));
+    const auto given_page = [&](int i) {
+      const int k = owner_of(give_at, m, i), page = a.table[(base + k) * a.table_stride + kept[k] + i - give_at[k]];
+      if (page < -1 || page >= n) report |= UAD_KV_BAD_PAGE;
+      return page;
+    };
+    bool odd = false;   // an entry of this thread's is no page
     if (a.fill && turn == share) {
       // Rows, pages taken and pages given back begin with different threads, so that few of each are worked on at the same time.
       for (uint32_t i = step - 1 - id; i < (uint32_t)n_taken; i += step) {
-        const int k = owner_of(take_at, m, (int)i);
-        a.table[(base + k) * a.table_stride + pages_of(had[k]) + (int)i - take_at[k]] = a.ring[on_ring(taken + i)];
+        const int k = owner_of(take_at, m, (int)i), page = a.ring[on_ring(taken + i)];
+        a.table[(base + k) * a.table_stride + pages_of(had[k]) + (int)i - take_at[k]] = page;
+        if ((unsigned)page >= (unsigned)n) report |= UAD_KV_BAD_PAGE;
       }
       for (uint32_t i = id < step / 2 ? id + step / 2 : id - step / 2; i < (uint32_t)n_given; i += step) {
-        const int k = owner_of(give_at, m, (int)i);
-        a.ring[on_ring(count + (uint32_t)given + i)] = a.table[(base + k) * a.table_stride + kept[k] + (int)i - give_at[k]];
+        const int page = given_page((int)i);
+        a.ring[on_ring((uint32_t)(count + put_at) + i)] = page;
+        odd |= (unsigned)page >= (unsigned)n;
       }
       if (a.maps) {
         for (uint32_t i = (uint32_t)rows / 4 + id; i < ((uint32_t)(rows + n_rows) + 3) / 4; i += step) {
@@ -257,6 +300,26 @@ __global__ void __launch_bounds__(kThreads) resize_kernel(const ResizeArgs a) {
         }
       }
     }
+    if (a.settle && sound && total[1] > 0) {
+      bool again = (int64_t)total[1] > n_given || (!a.fill && placed != given);
+      if (!again) again = __syncthreads_or(a.fill ? odd : no_page(count + placed, n_given));
+      if (!again) {
+        placed += n_given;
+      } else {
+        const uint32_t items = (uint32_t)min((int64_t)total[1], (int64_t)0x7fffffff);
+        for (uint32_t i0 = 0; i0 < items; i0 += blockDim.x) {
+          const uint32_t i = i0 + threadIdx.x;
+          const int page = i < items ? given_page((int)i) : -1;
+          const bool is = (unsigned)page < (unsigned)n;
+          T at[1] = {is}, all[1];
+          block_scan<1, T>(at, all, row_sums);
+          if (is && at[0] < room - placed) a.ring[on_ring((uint32_t)(count + placed) + (uint32_t)at[0])] = page;
+          if (all[0] > room - placed) report |= UAD_KV_BAD_POOL;
+          placed = (int)min((int64_t)placed + all[0], (int64_t)room);
+          __syncthreads();   // the sums have been read
+        }
+      }
+    }
     turn = turn + 1 >= shares ? 0 : turn + 1;
     asked_pages += total[0];
     given += total[1];
@@ -270,13 +333,13 @@ __global__ void __launch_bounds__(kThreads) resize_kernel(const ResizeArgs a) {
       for (uint32_t i = (uint32_t)rows / 4 + blockIdx.x * blockDim.x + threadIdx.x; i < ((uint32_t)a.n_rows + 3) / 4; i += gridDim.x * blockDim.x) put_rows(a, (int)i * 4, rows, a.n_rows, none);
     }
     if (lead && threadIdx.x == 0) a.start[a.n_seqs] = rows;
-    // what the lengths say is every block's finding: one tells it
-    if (!lead) report &= UAD_KV_BAD_PAGE;
-    if (report && a.status) atomicOr(a.status, report);
   }
-  if (a.update && lead && threadIdx.x == 0) {
-    const int head = sound ? (int)on_ring(taken) : first, left = sound ? count - taken + (int)min(given, (int64_t)room) : full;
-    a.state_out[0] = head;
+  // what the lengths say is every block's finding: one tells it
+  if (!lead) report &= UAD_KV_BAD_PAGE;
+  if (report && a.status) atomicOr(a.status, report);
+  if ((a.update || a.settle) && lead && threadIdx.x == 0) {
+    const int head = sound ? (int)on_ring(taken) : first, left = sound ? count - taken + (a.settle ? placed : (int)min(given, (int64_t)room)) : full;
+    a.state_out[0] = !a.settle && sound && given > room ? -1 : head;   // -1: for the launch behind, which settles it
     a.state_out[1] = left;
   }
 }
@@ -312,15 +375,19 @@ extern "C" int uad_kv_resize(const uad_page_pool* pool, const uad_kv_wanted* w, 
   const bool maps = w->slot || w->row_seq || w->row_pos;
   a.maps = maps;
   a.wide = (reinterpret_cast<uintptr_t>(w->slot) | reinterpret_cast<uintptr_t>(w->row_seq) | reinterpret_cast<uintptr_t>(w->row_pos)) % 16 == 0;
-  const int blocks = std::max(1, std::min(152, maps ? (int)(((int64_t)w->n_rows + 4095) / 4096) : w->n_seqs / 64));
-  // In place, blocks would read lengths or a state that another has already replaced: a launch of its own replaces them.
+  // Without maps, one block spares 128 to 255 sequences the second launch: a token more for 200 in place 6.6 us against 9.9 (4.1 against 5.5 not in
+  // place), whole prompts 10.1 against 11.3 (7.3 against 6.4); for 500 prompts it is 15.1 against 11.1.
+  const int blocks = std::max(1, std::min(152, maps ? (int)(((int64_t)w->n_rows + 4095) / 4096) : w->n_seqs < 256 ? 1 : w->n_seqs / 64));
+  // In place, blocks would read lengths or a state that another has already replaced: the second launch replaces them.
   const bool apart = blocks > 1 && (w->len_out == w->len || w->len_out == w->want || pool->state_out == pool->state);
   a.fill = 1;
   a.update = !apart;
+  a.settle = blocks == 1;
   cudaError_t e = launch_resize(a, blocks, s);
-  if (e == cudaSuccess && apart) {
+  if (e == cudaSuccess && blocks > 1) {
     a.fill = 0;
-    a.update = 1;
+    a.update = apart;
+    a.settle = 1;
     e = launch_resize(a, 1, s);
   }
   return launched(e);
