@@ -277,6 +277,7 @@ int uad::pages8_args(const uad_kv_pages8* g, const uad_kv_seqs* s, int n_rows, b
   if (reinterpret_cast<uintptr_t>(g->k_scale) % 4 || reinterpret_cast<uintptr_t>(g->v_scale) % 4) return UAD_EINVAL;
   const int rc = paged_args(&g->pages, s, n_rows, device, p, true);
   if (rc) return rc;
+  if (device && s->n_seqs > 0 && n_rows > 0 && (!on_current_device(g->k_scale) || !on_current_device(g->v_scale))) return UAD_EINVAL;
   sc->k = g->k_scale; sc->v = g->v_scale;
   sc->page = g->scale_page_stride; sc->block = g->scale_block_stride; sc->head = g->scale_head_stride;
   sc->log_block = log2_of(g->block);

@@ -133,7 +133,7 @@ int uad::paged_args(const uad_kv_pages* g, const uad_kv_seqs* s, int n_rows, boo
   if (n_rows < 0 || (!s->start && n_rows < s->n_seqs)) return UAD_EINVAL;
   if (device && s->n_seqs > 0 && n_rows > 0) {
     if (!s->table || !s->len) return UAD_EINVAL;
-    if (!on_current_device(g->k)) return UAD_EINVAL;
+    if (!on_current_device(g->k) || !on_current_device(g->v)) return UAD_EINVAL;
   }
   p->k = g->k; p->v = g->v;
   p->page_stride = g->page_stride; p->slot_stride = g->slot_stride; p->head_stride = g->head_stride;
