@@ -460,7 +460,7 @@ __global__ void __launch_bounds__(kThreads, ctas8<DH, NR>()) paged_attn8_kernel(
       for (int n = 0; n < 2 * KT; ++n)
 #pragma unroll
         for (int e = 0; e < (NR > 1 ? 4 : 2); ++e) {
-          const float v = s[mt][n][e] * rf[2 * mt + (e >> 1)] * (e & 1 ? ks[n].y : ks[n].x);
+          const float v = s[mt][n][e] * (rf[2 * mt + (e >> 1)] * (e & 1 ? ks[n].y : ks[n].x));   // a large query's factor and a small scale first
           s[mt][n][e] = max_nan(v, kLeast);
         }
     if (mixed || bits != (0xffffffffu >> (32 - KEYS))) {
