@@ -419,7 +419,7 @@ typedef struct uad_kv_pages8 {
  * of their block's scale: the least power of two s (2^-100 at the least) with 448 s >= the largest of the block's new values, for keys
  * that are rotated twice the largest before the rotation (which grows no value by more than sqrt(2)). Infinities and NaN do not count
  * and are stored as NaN (a finite value that a rotation takes past fp32's largest as the largest code). Where the block holds earlier tokens of the sequence, its scale does not fall below theirs (nor below the power of two above it), and where
- * it grows they are rounded to it: exactly but for values 2^-15 of the block's largest and below, so that what a cache holds hardly depends on how many
+ * it grows they are rounded to it: exactly but for values below 2^-6 of the new scale (up to 2^-13.8 of the block's largest, of rotated keys 2^-12.8), so that what a cache holds hardly depends on how many
  * calls wrote it. A block that is written therefore belongs to one sequence: it must not stand in another table of the same append, nor
  * be read meanwhile; whole blocks before it may be shared. Errors: UAD_EINVAL (arguments), UAD_ECUDA. */
 int uad_kv_append8(const uad_kv_pages8* pages, const uad_kv_seqs* seqs, const uad_kv_rows* rows, const uad_rope* rope,

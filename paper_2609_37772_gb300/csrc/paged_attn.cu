@@ -65,8 +65,8 @@ Split split_keys(int64_t keys, int64_t units, int64_t slots, int64_t least, int6
   return cut_keys(keys, n, units, slots, 64);
 }
 // warp_smem: shared memory of a CTA whose warps have heads of their own (0: there is no such form). round: keys that the warps of a CTA take at
-// once, of which the pieces of a small call are multiples (8-bit caches, 128 / 64 in us: 1 x 817 of 8 heads over 1 of 256 7.0 / 7.5, 1 x 100 of 24
-// heads of 64 3.7 / 5.1).
+// once, of which the pieces of a small call are multiples (8-bit caches, 128 / 64 in us: 1 x 817 of 8 heads over 1 of 256 7.1 / 7.5, 1 x 100 of 24
+// heads of 64 4.0 / 5.0).
 void attn_plan(const uad_kv_seqs* s, int ctas_per_sm, size_t warp_smem, int round, PagedAttnArgs* a) {
   const int64_t all = s->max_len > 0 && s->max_len < a->p.capacity ? s->max_len : a->p.capacity;
   const int64_t near = (int64_t)a->window + a->sinks + a->p.max_new - 1;

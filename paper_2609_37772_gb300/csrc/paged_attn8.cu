@@ -19,11 +19,11 @@
 //   output's own rounding to bf16 is (one / two, in us: 64 x 4000 keys of 32 heads over 8 of 128 93 / 95, of 8 over 1 of 256 28 / 29, with 4 new tokens
 //   60 / 67; 16 x 4000 with 8 new tokens of 32 over 8 of 128 60 / 74, where the MMAs of four tiles of rows count).
 //
-// One new token: 64 x 4000 keys of 32 heads over 8 of 128 take 95 us (524 MB, 5.5 TB/s; 170 from a bf16 cache), 2 sequences of up to 131071 of
-// the same 61 us (5.5 TB/s), 64 x 4000 of 8 over 1 of 256 28 us (4.6 TB/s). What bounds: the latencies of a warp's slice (about 800
-// instructions for 32 keys of 128 dims, of which the conversions of codes are 190; 0.45 issued a cycle and scheduler) with the two to four
-// warps a scheduler that registers allow. Slices of 16 keys with four CTAs an SM take 99 us for the first, four slots of the ring in place
-// of three 96; of 256 dims, slices of 16 keys 30 us for the last.
+// One new token: 64 x 4000 keys of 32 heads over 8 of 128 take 96 us (524 MB, 5.5 TB/s; 170 from a bf16 cache), 2 sequences of up to 131071 of
+// the same 63 us (5.3 TB/s), 64 x 4000 of 8 over 1 of 256 29 us (4.5 TB/s). What bounds: the latencies of a warp's slice (about 860
+// instructions for 32 keys of 128 dims, of which the conversions of codes are 190; 0.44 issued a cycle and scheduler) with the two to four
+// warps a scheduler that registers allow. Slices of 16 keys with four CTAs an SM take 111 us for the first, four slots of the ring in place
+// of three 97; of 256 dims, slices of 16 keys 31 us for the last.
 #include "kv_pages8.cuh"
 #include "paged_attn.cuh"
 
@@ -150,7 +150,7 @@ __device__ __forceinline__ Place place_of(const PagedAttn8Args& g, const Piece& 
 // Sharing evenly. A sequence's keys are chunks of four slices; the sequences' chunks one behind the other are cut into as many parts as
 // there are CTAs for each key/value head and block of rows (blockIdx.x: the part, .y: the head, .z: the rows), whatever the
 // lengths. Parts are the same for all heads, which so read a token's keys at about the same time: they lie next to each other in most caches, and
-// reading one head's alone takes up to 1.6 times as long (64 x 1000 keys of 24 heads of 64: 75 us against 46). A CTA takes the pieces of its part
+// reading one head's alone takes up to 1.6 times as long (64 x 1000 keys of 24 heads of 64: 75 us against 46, with one f16 a weight). A CTA takes the pieces of its part
 // in turn. A sequence that lies in one part is done there. Otherwise its pieces go to the workspace (a CTA has two at most: one
 // of a sequence that began before its part, one of a sequence that goes on behind it), and a second kernel joins them.
 constexpr int kEvenSeqs = 1024;   // sequences that a CTA sums up
@@ -698,7 +698,7 @@ template <int DH, int NR>
 __global__ void __launch_bounds__(kThreads) paged_join8_kernel(const PagedAttn8Args args) {
   const PagedAttnArgs& a = args.a;
   // No early start for the kernel behind it: where this one's CTAs are still there, an SM does not take as many of the next attention's as it
-  // could, and the one wave of those becomes two (64 x 4000 keys of 32 heads over 8 of 128, call after call: 137 us against 96).
+  // could, and the one wave of those becomes two (64 x 4000 keys of 32 heads over 8 of 128, call after call: 137 us against 96 with one f16 a weight).
   pdl_wait();
   constexpr int FOURS = 8 * NR / kWarps;
   const int head = blockIdx.y / (DH / 64), column = blockIdx.y % (DH / 64), block = blockIdx.z / FOURS;
@@ -803,11 +803,12 @@ int64_t attn8_bytes(const PagedAttn8Args& a) {
 // Into how many parts the chunks are cut; 0: not evenly. Evenly, a call costs about 6 us more (the sums, a second kernel) and a CTA about 4 us for each further sequence, and it gains what SMs idle otherwise: pieces in waves of which the last
 // is part-filled, and lengths that differ. So the CTAs' shares have to last some 24 us at the rates (keys a microsecond and CTA) at
 // which they come, and to be half a sequence long at least. In us, evenly / as attn_plan has it, for equal lengths and for a
-// quarter of the longest and more:
-//   64 x 4000 keys, 32 heads over 8 of 128:  96 / 107 and 68 / 75      64 x 2000, the same:            55 / 65 and 43 / 45
-//   64 x 4000, 4 new tokens, 8 over 1 of 256: 61 / 58 and 46 / 59      16 x 4000, 8 new, 32 / 8 of 128: 61 / 56 and 46 / 56
-//   32768 and 131071, 32 over 8 of 128:      63 / 74                   64 x 1000, 24 heads of 64:      51 / 45 and 40 / 36
-//   64 x 4000, 8 over 1 of 256:              33 / 27 and 27 / 25       16 x 1000, 32 / 8 of 128:       18 / 13 and 16 / 12
+// quarter of the longest and more (which of the two the host cannot know: batches of several new tokens pay 6 to 7% where lengths are
+// equal for 20% where they are not):
+//   64 x 4000 keys, 32 heads over 8 of 128:  96 / 111 and 67 / 79      64 x 2000, the same:            54 / 67 and 42 / 47
+//   64 x 4000, 4 new tokens, 8 over 1 of 256: 67 / 63 and 50 / 64      16 x 4000, 8 new, 32 / 8 of 128: 74 / 70 and 55 / 69
+//   32768 and 131071, 32 over 8 of 128:      67 / 80                   64 x 1000, 24 heads of 64:      53 / 48 and 41 / 38
+//   64 x 4000, 8 over 1 of 256:              34 / 29 and 29 / 27       16 x 1000, 32 / 8 of 128:       19 / 13 and 17 / 12
 int even_parts(const PagedAttnArgs& a, const uad_kv_seqs* s, int ctas) {
   const int64_t all = s->max_len > 0 && s->max_len < a.p.capacity ? s->max_len : a.p.capacity;
   const int64_t near = (int64_t)a.window + a.sinks + a.p.max_new - 1, keys = a.window > 0 && near < all ? near : all;

@@ -5,9 +5,9 @@ nearest ones, exactly. A rotated value is off by (|a| + |b|) 2^-22 before it is 
 sum by 2^-24 each); its code is then within half a step of e4m3 of that: 2^(e - 4) for a value of exponent e, 2^(-10) of the scale
 at the least.
 Attention: as for bf16 caches a score is off by d = dh 2^-23 scale sum |q k| (products of f16 are exact, the tensor cores truncate), and by
-three more roundings for the scales: 2^-22 of it. Probabilities are off by e^d twice, by 2^-20 of exp, sums of n terms by n 2^-23; the weights are rounded
-to f16: 2^-11 relative at most (half a step is 2^-12, of the mantissa's 1 to 2), and 2^-36 of the largest weight where they are small. The output is off by
-that much of sum p |v|, then by bf16's half step.
+three more roundings for the scales: 2^-22 of it. Probabilities are off by e^d twice, by 2^-20 of exp, sums of n terms by n 2^-23; the weights are the sum of
+two f16, 2^-21 relative and 2^-34 of the row's largest where they are small; allowed are 2^-11 and 2^-36 of the values' sum (test_gpu_cache8_weights has the
+closer bounds). The output is off by that much of sum p |v|, then by bf16's half step.
 """
 import math
 
