@@ -146,3 +146,40 @@ def test_a_windowed_episode_from_its_begin_to_its_end():
     step(0, 30)
     held = table[1].tolist()
     assert len(set(held[:2])) == 2 and min(held[:2]) >= 0
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("rows", [40, 9000])
+def test_a_captured_call_meets_other_tables(rows, in_place):
+    """One graph, replayed over tables with and without places that hold no page, and over a ring that they do not fit."""
+    rng = np.random.default_rng(rows)
+    seqs, width, page, n = 300, 20, 4, 6000
+    up = lambda x: torch.from_numpy(np.ascontiguousarray(x)).cuda()  # noqa: E731
+    whole = lambda *s: torch.full(s, -9, dtype=torch.int32, device="cuda")  # noqa: E731
+    ring, state, table, lens, want, start, status = whole(n), whole(2), whole(seqs, width), whole(seqs), whole(seqs), whole(seqs + 1), whole(1)
+    slot, seq, pos = torch.zeros(rows, dtype=torch.int64, device="cuda"), whole(rows), whole(rows)
+    out, state_out = (lens, state) if in_place else (whole(seqs), whole(2))
+    pool, st = uad.PagePool(ring, state, page), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=st):
+        pool.resize(table, lens, want, start, length_out=None if in_place else out, state_out=None if in_place else state_out, slot=slot, row_seq=seq,
+                    row_pos=pos, status=status, stream=st)
+    for turn in range(6):
+        now = rng.integers(20, 60, seqs)
+        p = Pool(now.tolist(), width, page, 0, seed=turn)
+        spare = n - p.n
+        p.ring = np.concatenate([np.arange(p.n, n), np.full(p.n, -1)]).astype(np.int32)
+        p.n, p.state = n, np.array([0, spare], np.int32)
+        if turn % 2:
+            hide(p, 0.5, rng)
+        if turn == 4:
+            p.state[1] = n - 500   # more than there are: not everything finds a place
+        shall = np.where(rng.random(seqs) < 0.5, 0, now + rng.integers(0, 9, seqs))
+        for t, x in ((ring, p.ring), (state, p.state), (table, p.table), (lens, p.lens), (want, shall.astype(np.int32)), (status, np.zeros(1, np.int32))):
+            t.copy_(up(x))
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        check_ring(p, shall, rows, dict(ring=ring.cpu().numpy(), state=state_out.cpu().numpy(), table=table.cpu().numpy(), lens=out.cpu().numpy(), start=start.cpu().numpy(),
+                                        slot=slot.cpu().numpy(), seq=seq.cpu().numpy(), pos=pos.cpu().numpy(), status=int(status)))
